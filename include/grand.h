@@ -315,6 +315,153 @@ grand_status grand_reset_stats(grand_index *h);
 /* Text of the last error on this handle ("" if none). */
 const char *grand_last_error(const grand_index *h);
 
+/* ------------------------------------------------------------------------
+ * Key/value caches: the operators with which a language model's attention
+ * uses pools of slots beside an index of its keys.  A query's search in a
+ * GRAND_MIPS index returns the slots to attend to (grand_cache_attend_ids),
+ * the newest tokens are attended to where they lie (grand_cache_attend),
+ * and the slots that draw the least attention leave (grand_cache_evict); the
+ * freed ids are what grand_delete_batch takes.
+ *
+ * A pool holds n_pages pages of page_size slots; a slot holds one token's
+ * key and value rows of every key/value head.  A sequence's tokens lie in
+ * the pages that its row of the page table names, in order.  With
+ * page_size 1 a page is a slot and page ids are slot ids.
+ *
+ * Conventions of grand_cache_* beside those at the top of this file
+ *  - Every pointer to data is device memory of the cache's GPU, and the
+ *    calls only enqueue work on the cache's stream: they return before it
+ *    is done, and the memory must live until then.  A handle keeps
+ *    workspaces, no results; calls on one handle are ordered by its stream.
+ *  - A workspace grows when a call needs more than any call before it (the
+ *    growth waits for the device).  A stream capture does not allow that:
+ *    run the call once before the capture, else it fails with
+ *    GRAND_E_CAPACITY and nothing is done.
+ *  - Sizes, strides, alignment and the extent of device buffers are checked
+ *    before anything is enqueued.  What lies in device memory (page ids,
+ *    lengths, chunk starts, slot ids) is checked by the kernels: nothing is
+ *    read or written outside the buffers, the results of the sequence
+ *    concerned are unspecified, and grand_cache_check reports it.
+ *  - Strides are in elements.  The elements of one head's row are
+ *    contiguous; rows start at multiples of 16 bytes (8 elements).
+ */
+typedef struct grand_cache grand_cache;
+enum { GRAND_BF16 = 2, GRAND_F16 = 3 };
+
+typedef struct {
+  uint32_t struct_size;  /* sizeof(grand_cache_params) */
+  int32_t dtype;         /* of queries, keys, values and results: GRAND_BF16 | GRAND_F16 */
+  uint32_t q_heads;      /* a multiple of kv_heads */
+  uint32_t kv_heads;
+  uint32_t head_dim;     /* a multiple of 8, 8..256 */
+  uint32_t page_size;    /* slots of a page, a power of two, 1..1024 */
+  int32_t device;
+  void *stream;
+} grand_cache_params;
+
+/* A pool.  keys and values have the same strides. */
+typedef struct {
+  void *k, *v;
+  uint32_t n_pages;
+  int64_t page_stride, slot_stride, head_stride;
+} grand_pages;
+
+/* Rows by (token, head). */
+typedef struct {
+  void *p;
+  int64_t token_stride, head_stride;
+} grand_rows;
+
+/* Sums of attention weight by (sequence, key/value head, token), fp32. */
+typedef struct {
+  float *p;
+  int64_t seq_stride, head_stride;
+} grand_weights;
+
+/* The sequences of a call.  The new tokens of sequence b are rows
+ * q_start[b] .. q_start[b + 1] - 1 of the call's n_tokens rows (q_start
+ * null: row b only, n_tokens = n_seq); lens[b] tokens are cached, the new ones
+ * included (they are the last).  max_q and max_k bound the new and the
+ * cached tokens of a sequence: work is laid out by them. */
+typedef struct {
+  uint32_t n_seq, n_tokens, max_q, max_k;
+  const uint32_t *table;   /* n_seq rows of max_pages page ids, table_stride apart */
+  int64_t table_stride;
+  uint32_t max_pages;
+  const uint32_t *q_start; /* n_seq + 1, or null */
+  const uint32_t *lens;    /* n_seq */
+} grand_seqs;
+
+/* bf16, 32 query heads, 8 key/value heads of 128 elements, pages of 16. */
+void grand_default_cache_params(grand_cache_params *p);
+grand_status grand_cache_create(const grand_cache_params *p, grand_cache **out);
+grand_status grand_cache_destroy(grand_cache *h);
+/* Waits for the old stream's work, as the workspaces are shared. */
+grand_status grand_cache_set_stream(grand_cache *h, void *stream);
+/* Waits for the stream and reports what kernels found wrong in device memory
+ * since the last check: GRAND_E_ID (a page or slot id outside the pool) or
+ * GRAND_E_ARG (lengths or chunk starts out of range), else GRAND_OK. */
+grand_status grand_cache_check(grand_cache *h);
+const char *grand_cache_last_error(const grand_cache *h);
+
+/* Writes the new tokens' keys and values (n_tokens rows by kv_heads) to their
+ * places in the pages: new token i of sequence b is cached token
+ * lens[b] - chunk length + i.  No other slot is touched. */
+grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand_rows *k, const grand_rows *v,
+                                const grand_pages *pages);
+
+/* Attention of the new tokens over the cached ones, which hold the new ones
+ * already (grand_cache_append).  Row i of sequence b has position
+ * p = lens[b] - chunk length + i and sees the cached tokens j < lens[b] with
+ * j <= p if causal, and j > p - window if window > 0.  With
+ * s_j = scale <q, k_j>, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and
+ * lse = ln sum_j exp(s_j), by (token, q_head); a row that sees nothing has
+ * out = 0 and lse = -inf.  Hidden tokens have no influence, whatever their
+ * keys and values hold.  Query head h uses key/value head
+ * h / (q_heads / kv_heads).  scale > 0.
+ * lse: n_tokens x q_heads, or null.
+ * weights_in, weights_out: null, or rows of at least max_k entries: entry j
+ * of weights_out becomes entry j of weights_in plus the softmax weight that
+ * the new tokens give to cached token j, summed over them and the query
+ * heads of the key/value head; entries from lens[b] on are not written.
+ * The two may be one buffer, but not overlap otherwise. */
+grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages,
+                                float scale, int causal, uint32_t window, const grand_rows *out, float *lse,
+                                const grand_weights *weights_in, const grand_weights *weights_out);
+
+/* Attention of one token per sequence (n_seq rows) over listed slots: row
+ * (b, query head h) over the k ids at ids + b * ids_seq_stride +
+ * h * ids_head_stride, in any order; GRAND_INVALID entries are passed over,
+ * so the lists may be a search's results (a stride of 0 shares a list).
+ * Slot id i is slot i % page_size of page i / page_size.  A repeated id
+ * counts each time.
+ * prior, prior_lse: null, or another attention's result of the same rows
+ * over other tokens (out and lse of grand_cache_attend): the call returns
+ * what attention over both would.  lse: n_seq x q_heads, or null. */
+grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_rows *q, const grand_pages *pages,
+                                    const uint32_t *ids, uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride,
+                                    float scale, const grand_rows *prior, const float *prior_lse,
+                                    const grand_rows *out, float *lse);
+
+/* Eviction by accumulated weight, in pages.  Of the n = ceil(lens[b] /
+ * page_size) pages of sequence b stay: the first `sinks`, the last
+ * max(recent, 1 if the last page is not full), and of the others those with
+ * the largest score, up to budget[b] pages in all (more only if the fixed
+ * ones are more).  A page's score is the fp32 sum, head by head and in a
+ * head token by token, of its entries of `weights` (`heads` heads, rows of
+ * `cap` entries); equal scores stay lowest index first, NaN counts as
+ * -inf.  The order of the pages is kept.
+ * Outputs, which overlap no input: out_table (n_seq x max_pages, packed; the
+ * kept pages, then GRAND_INVALID), out_weights (`cap` entries a row: the
+ * kept tokens' weights, then zeros), out_lens, freed (n_seq x max_pages: the
+ * freed page ids in table order, then GRAND_INVALID), n_freed.  The pages'
+ * keys and values stay where they are.  q_start, max_q and n_tokens of s are
+ * not used. */
+grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t heads, uint32_t cap,
+                               const grand_weights *weights, const uint32_t *budget, uint32_t sinks, uint32_t recent,
+                               uint32_t *out_table, const grand_weights *out_weights, uint32_t *out_lens,
+                               uint32_t *freed, uint32_t *n_freed);
+
 #ifdef __cplusplus
 }
 #endif

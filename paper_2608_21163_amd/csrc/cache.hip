@@ -1,0 +1,484 @@
+// cache.hip -- the host side of the key/value-cache operators: checks of
+// arguments, plans, workspaces and launches.  No call here waits for the GPU
+// unless a workspace grows.
+#include "cache.h"
+
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+
+#include "../../include/grand.h"
+
+using namespace gr;
+
+struct grand_cache {
+  grand_cache_params p;
+  hipStream_t stream = nullptr;
+  bool poisoned = false;
+  uint32_t shift = 0;       // log2 of the page size
+  uint8_t *ws = nullptr;    // workspace
+  size_t ws_bytes = 0;
+  CacheErr *err = nullptr;  // device
+  char msg[256] = "";
+};
+
+namespace {
+
+grand_status fail(grand_cache *h, grand_status code, const char *fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(h->msg, sizeof h->msg, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+grand_status fail_dev(grand_cache *h, hipError_t e, const char *what) {
+  (void)hipGetLastError();  // the error stays with this handle
+  h->poisoned = true;
+  return fail(h, GRAND_E_DEVICE, "HIP error in %s: %s", what, hipGetErrorString(e));
+}
+
+#define HCHK(h, x)                                      \
+  do {                                                  \
+    hipError_t e_ = (x);                                \
+    if (e_ != hipSuccess) return fail_dev((h), e_, #x); \
+  } while (0)
+#define TRY(x)                            \
+  do {                                    \
+    const grand_status s_ = (x);          \
+    if (s_ != GRAND_OK) return s_;        \
+  } while (0)
+
+grand_status check_usable(grand_cache *h) {
+  if (!h) return GRAND_E_ARG;
+  if (h->poisoned) return GRAND_E_STATE;
+  h->msg[0] = 0;
+  return GRAND_OK;
+}
+
+// A buffer must lie in this GPU's memory, and its allocation must hold it.
+grand_status check_mem(grand_cache *h, const char *name, const void *p, uint64_t bytes, size_t align) {
+  if (!p) return fail(h, GRAND_E_ARG, "%s is null", name);
+  if ((uintptr_t)p % align) return fail(h, GRAND_E_ARG, "%s is not aligned to %zu bytes", name, align);
+  hipPointerAttribute_t a{};
+  if (hipPointerGetAttributes(&a, p) != hipSuccess || a.type != hipMemoryTypeDevice || a.device != h->p.device) {
+    (void)hipGetLastError();
+    return fail(h, GRAND_E_ARG, "%s is not memory of GPU %d", name, h->p.device);
+  }
+  hipDeviceptr_t base = nullptr;
+  size_t size = 0;
+  if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(h, GRAND_E_ARG, "%s has no device allocation", name);
+  }
+  const uint64_t room = (uint64_t)((uintptr_t)base + size - (uintptr_t)p);
+  if (bytes > room) return fail(h, GRAND_E_ARG, "%s is shorter than the call needs", name);
+  return GRAND_OK;
+}
+
+// Elements up to which rows n0 x n1 x n2 at these strides reach; false when
+// a stride is negative or the extent does not fit 62 bits.
+bool extent(uint64_t n0, int64_t s0, uint64_t n1, int64_t s1, uint64_t n2, int64_t s2, uint64_t row, uint64_t *out) {
+  if (s0 < 0 || s1 < 0 || s2 < 0) return false;
+  const __uint128_t e = (__uint128_t)(n0 - 1) * s0 + (__uint128_t)(n1 - 1) * s1 + (__uint128_t)(n2 - 1) * s2 + row;
+  if (e >> 62) return false;
+  *out = (uint64_t)e;
+  return true;
+}
+
+grand_status check_rows(grand_cache *h, const char *name, const grand_rows *r, uint64_t tokens, uint32_t heads, bool written,
+                        RowsView *out) {
+  if (!r) return fail(h, GRAND_E_ARG, "%s is null", name);
+  uint64_t e = 0;
+  if (r->token_stride % 8 || r->head_stride % 8 || !extent(tokens, r->token_stride, heads, r->head_stride, 1, 0, h->p.head_dim, &e))
+    return fail(h, GRAND_E_ARG, "strides of %s must be multiples of 8 elements, not negative", name);
+  // rows that are written must not overlap: one head's rows lie inside the
+  // other stride
+  if (written) {
+    const uint64_t d = h->p.head_dim, ts = (uint64_t)r->token_stride, hs = (uint64_t)r->head_stride;
+    const bool ok = (heads == 1 || hs >= d) && (tokens == 1 || ts >= d) &&
+                    (tokens == 1 || heads == 1 || ts >= (heads - 1) * hs + d || hs >= (tokens - 1) * ts + d);
+    if (!ok) return fail(h, GRAND_E_ARG, "rows of %s overlap", name);
+  }
+  TRY(check_mem(h, name, r->p, e * 2, 16));
+  out->p = static_cast<uint8_t *>(r->p);
+  out->token = r->token_stride * 2;
+  out->head = r->head_stride * 2;
+  return GRAND_OK;
+}
+
+grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
+  if (!g) return fail(h, GRAND_E_ARG, "pages is null");
+  uint64_t e = 0;
+  if (g->n_pages == 0) return fail(h, GRAND_E_ARG, "the pool has no pages");
+  if ((uint64_t)g->n_pages << h->shift > 0xFFFFFFFFull) return fail(h, GRAND_E_CAPACITY, "a pool holds fewer than 2^32 slots");
+  if (g->page_stride % 8 || g->slot_stride % 8 || g->head_stride % 8 ||
+      !extent(g->n_pages, g->page_stride, h->p.page_size, g->slot_stride, h->p.kv_heads, g->head_stride, h->p.head_dim, &e))
+    return fail(h, GRAND_E_ARG, "strides of pages must be multiples of 8 elements, not negative");
+  TRY(check_mem(h, "pages.k", g->k, e * 2, 16));
+  TRY(check_mem(h, "pages.v", g->v, e * 2, 16));
+  out->k = static_cast<const uint8_t *>(g->k);
+  out->v = static_cast<const uint8_t *>(g->v);
+  out->page = g->page_stride * 2;
+  out->slot = g->slot_stride * 2;
+  out->head = g->head_stride * 2;
+  out->n_pages = g->n_pages;
+  out->shift = h->shift;
+  return GRAND_OK;
+}
+
+grand_status check_seqs(grand_cache *h, const grand_seqs *s, bool chunks, SeqsView *out) {
+  if (!s) return fail(h, GRAND_E_ARG, "seqs is null");
+  if (s->n_seq > 65535) return fail(h, GRAND_E_CAPACITY, "at most 65535 sequences a call");
+  if (s->table_stride < (int64_t)s->max_pages) return fail(h, GRAND_E_ARG, "table_stride is below max_pages");
+  if (s->max_k > (uint64_t)s->max_pages << h->shift) return fail(h, GRAND_E_ARG, "max_k tokens do not fit max_pages pages");
+  if (s->max_k >= 1u << 31) return fail(h, GRAND_E_CAPACITY, "max_k must be below 2^31");
+  if (chunks) {
+    if (!s->q_start && (s->n_tokens != s->n_seq || s->max_q != 1))
+      return fail(h, GRAND_E_ARG, "without q_start every sequence has one new token (n_tokens = n_seq, max_q = 1)");
+    if (s->q_start) TRY(check_mem(h, "q_start", s->q_start, ((uint64_t)s->n_seq + 1) * 4, 4));
+  }
+  uint64_t e = 0;
+  if (!extent(s->n_seq, s->table_stride, 1, 0, 1, 0, s->max_pages, &e)) return fail(h, GRAND_E_ARG, "table_stride is too large");
+  if (s->max_pages) TRY(check_mem(h, "table", s->table, e * 4, 4));
+  TRY(check_mem(h, "lens", s->lens, (uint64_t)s->n_seq * 4, 4));
+  out->table = s->table;
+  out->table_stride = s->table_stride;
+  out->q_start = s->q_start;
+  out->lens = s->lens;
+  out->n_seq = s->n_seq;
+  out->n_tokens = s->n_tokens;
+  out->max_pages = s->max_pages;
+  out->max_q = std::min(s->max_q, s->n_tokens);
+  out->max_k = s->max_k;
+  return GRAND_OK;
+}
+
+grand_status check_weights(grand_cache *h, const char *name, const grand_weights *w, uint32_t n_seq, uint32_t heads, uint32_t cap,
+                           bool written, WeightsView *out) {
+  if (!w) return fail(h, GRAND_E_ARG, "%s is null", name);
+  uint64_t e = 0;
+  if (!extent(n_seq, w->seq_stride, heads, w->head_stride, 1, 0, cap, &e)) return fail(h, GRAND_E_ARG, "strides of %s are negative", name);
+  if (written) {
+    const uint64_t ss = (uint64_t)w->seq_stride, hs = (uint64_t)w->head_stride, c = cap;
+    const bool ok = (heads == 1 || hs >= c) && (n_seq == 1 || ss >= c) &&
+                    (n_seq == 1 || heads == 1 || ss >= (heads - 1) * hs + c || hs >= (n_seq - 1) * ss + c);
+    if (!ok) return fail(h, GRAND_E_ARG, "rows of %s overlap", name);
+  }
+  TRY(check_mem(h, name, w->p, e * 4, 4));
+  out->p = w->p;
+  out->seq = w->seq_stride;
+  out->head = w->head_stride;
+  return GRAND_OK;
+}
+
+// A workspace of parts of these sizes, each 256-byte aligned.
+struct Parts {
+  size_t at[8] = {}, total = 0;
+  int n = 0;
+  int add(uint64_t bytes) {
+    at[n] = total;
+    total += (bytes + 255) / 256 * 256;
+    return n++;
+  }
+};
+grand_status ensure_ws(grand_cache *h, size_t bytes) {
+  if (bytes <= h->ws_bytes) return GRAND_OK;
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  HCHK(h, hipStreamIsCapturing(h->stream, &cs));
+  if (cs != hipStreamCaptureStatusNone)
+    return fail(h, GRAND_E_CAPACITY, "the workspace must grow to %zu bytes: run the call once before the capture", bytes);
+  HCHK(h, hipStreamSynchronize(h->stream));
+  if (h->ws) (void)hipFree(h->ws);
+  h->ws = nullptr;
+  h->ws_bytes = 0;
+  const size_t want = bytes + bytes / 4;
+  if (hipMalloc((void **)&h->ws, want) != hipSuccess) {
+    (void)hipGetLastError();
+    h->ws = nullptr;
+    return fail(h, GRAND_E_OOM, "no memory for a workspace of %zu bytes", want);
+  }
+  h->ws_bytes = want;
+  return GRAND_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+void grand_default_cache_params(grand_cache_params *p) {
+  if (!p) return;
+  memset(p, 0, sizeof *p);
+  p->struct_size = sizeof(grand_cache_params);
+  p->dtype = GRAND_BF16;
+  p->q_heads = 32;
+  p->kv_heads = 8;
+  p->head_dim = 128;
+  p->page_size = 16;
+}
+
+grand_status grand_cache_create(const grand_cache_params *p, grand_cache **out) {
+  if (!out) return GRAND_E_ARG;
+  *out = nullptr;
+  const char *why = nullptr;
+  if (!p || p->struct_size != sizeof(grand_cache_params)) why = "struct_size does not match";
+  else if (p->dtype != GRAND_BF16 && p->dtype != GRAND_F16) why = "dtype must be GRAND_BF16 or GRAND_F16";
+  else if (!p->kv_heads || !p->q_heads || p->q_heads % p->kv_heads) why = "q_heads must be a multiple of kv_heads";
+  else if (p->q_heads > 1024) why = "at most 1024 query heads";
+  else if (!p->head_dim || p->head_dim % 8 || p->head_dim > 256) why = "head_dim must be a multiple of 8 up to 256";
+  else if (!p->page_size || p->page_size > 1024 || (p->page_size & (p->page_size - 1))) why = "page_size must be a power of two up to 1024";
+  if (why) {
+    fprintf(stderr, "grand_cache_create: %s\n", why);
+    return GRAND_E_ARG;
+  }
+  grand_cache *h = new (std::nothrow) grand_cache();
+  if (!h) return GRAND_E_OOM;
+  h->p = *p;
+  h->stream = (hipStream_t)p->stream;
+  while ((1u << h->shift) < p->page_size) h->shift++;
+  if (hipSetDevice(p->device) != hipSuccess) {
+    (void)hipGetLastError();
+    delete h;
+    return GRAND_E_DEVICE;
+  }
+  if (hipMalloc((void **)&h->err, sizeof(CacheErr)) != hipSuccess) {
+    (void)hipGetLastError();
+    delete h;
+    return GRAND_E_OOM;
+  }
+  if (hipMemset(h->err, 0, sizeof(CacheErr)) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
+    (void)hipGetLastError();
+    (void)hipFree(h->err);
+    delete h;
+    return GRAND_E_DEVICE;
+  }
+  *out = h;
+  return GRAND_OK;
+}
+
+grand_status grand_cache_destroy(grand_cache *h) {
+  if (!h) return GRAND_OK;
+  (void)hipSetDevice(h->p.device);
+  if (!h->poisoned) (void)hipStreamSynchronize(h->stream);
+  if (h->ws) (void)hipFree(h->ws);
+  if (h->err) (void)hipFree(h->err);
+  delete h;
+  return GRAND_OK;
+}
+
+grand_status grand_cache_set_stream(grand_cache *h, void *stream) {
+  TRY(check_usable(h));
+  if ((hipStream_t)stream == h->stream) return GRAND_OK;
+  HCHK(h, hipStreamSynchronize(h->stream));
+  h->stream = (hipStream_t)stream;
+  return GRAND_OK;
+}
+
+grand_status grand_cache_check(grand_cache *h) {
+  TRY(check_usable(h));
+  HCHK(h, hipSetDevice(h->p.device));
+  CacheErr e{};
+  HCHK(h, hipMemcpyAsync(&e, h->err, sizeof e, hipMemcpyDeviceToHost, h->stream));
+  HCHK(h, hipStreamSynchronize(h->stream));
+  if (e.code == kCacheOk) return GRAND_OK;
+  HCHK(h, hipMemsetAsync(h->err, 0, sizeof e, h->stream));
+  HCHK(h, hipStreamSynchronize(h->stream));
+  switch (e.code) {
+    case kCachePage: return fail(h, GRAND_E_ID, "a page id of sequence %u is outside the pool", e.where);
+    case kCacheId: return fail(h, GRAND_E_ID, "a slot id of sequence %u is outside the pool", e.where);
+    case kCacheLen: return fail(h, GRAND_E_ARG, "the length of sequence %u is above max_k or below its chunk's", e.where);
+    default: return fail(h, GRAND_E_ARG, "the chunk of sequence %u is not within n_tokens rows and max_q", e.where);
+  }
+}
+
+const char *grand_cache_last_error(const grand_cache *h) { return h ? h->msg : "null handle"; }
+
+grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand_rows *k, const grand_rows *v,
+                                const grand_pages *pages) {
+  TRY(check_usable(h));
+  if (s && (s->n_seq == 0 || s->n_tokens == 0 || s->max_q == 0)) return GRAND_OK;
+  HCHK(h, hipSetDevice(h->p.device));
+  AppendArgs a{};
+  TRY(check_seqs(h, s, true, &a.s));
+  TRY(check_pages(h, pages, &a.pg));
+  TRY(check_rows(h, "k", k, s->n_tokens, h->p.kv_heads, false, &a.k));
+  TRY(check_rows(h, "v", v, s->n_tokens, h->p.kv_heads, false, &a.v));
+  if ((uint64_t)a.s.max_q * h->p.kv_heads * (h->p.head_dim / 8) >= 1ull << 31)
+    return fail(h, GRAND_E_CAPACITY, "max_q is too large");
+  a.kv_heads = h->p.kv_heads;
+  a.dim = h->p.head_dim;
+  a.err = h->err;
+  HCHK(h, launch_append(a, h->stream));
+  return GRAND_OK;
+}
+
+grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages, float scale,
+                                int causal, uint32_t window, const grand_rows *out, float *lse, const grand_weights *weights_in,
+                                const grand_weights *weights_out) {
+  TRY(check_usable(h));
+  if (s && (s->n_seq == 0 || ((s->n_tokens == 0 || s->max_q == 0) && !weights_out))) return GRAND_OK;
+  HCHK(h, hipSetDevice(h->p.device));
+  const grand_cache_params &p = h->p;
+  AttendArgs a{};
+  TRY(check_seqs(h, s, true, &a.s));
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
+  if (!weights_in != !weights_out) return fail(h, GRAND_E_ARG, "weights_in and weights_out come together");
+  TRY(check_pages(h, pages, &a.pg));
+  if (s->n_tokens) {
+    TRY(check_rows(h, "q", q, s->n_tokens, p.q_heads, false, &a.q));
+    TRY(check_rows(h, "out", out, s->n_tokens, p.q_heads, true, &a.out));
+    if (lse) TRY(check_mem(h, "lse", lse, (uint64_t)s->n_tokens * p.q_heads * 4, 4));
+  }
+  if (weights_out) {
+    TRY(check_weights(h, "weights_in", weights_in, s->n_seq, p.kv_heads, s->max_k, false, &a.win));
+    TRY(check_weights(h, "weights_out", weights_out, s->n_seq, p.kv_heads, s->max_k, true, &a.wout));
+  }
+  a.lse = lse;
+  a.q_heads = p.q_heads;
+  a.kv_heads = p.kv_heads;
+  a.group = p.q_heads / p.kv_heads;
+  a.dim = p.head_dim;
+  a.scale = scale;
+  a.c = scale * 1.44269504088896341f;
+  a.causal = causal != 0;
+  a.window = window ? window : 0xFFFFFFFFu;
+  a.err = h->err;
+
+  const uint64_t rows = (uint64_t)a.s.max_q * a.group;
+  if (rows >= 1u << 30) return fail(h, GRAND_E_CAPACITY, "max_q is too large");
+  const int mode = rows <= kKeysTileRows ? kKeys : kRows;
+  const uint32_t tile_rows = mode == kKeys ? kKeysTileRows : kRowsTileRows;
+  a.row_tiles = (uint32_t)((rows + tile_rows - 1) / tile_rows);
+  // Keys a row tile sees at most, and the splits that give every CU work.
+  const uint64_t span = std::min<uint64_t>(s->max_k, window ? (uint64_t)window + std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) + 31 : s->max_k);
+  const uint64_t base = std::max<uint64_t>(1, (uint64_t)p.kv_heads * a.row_tiles * s->n_seq);
+  const uint64_t want = mode == kKeys ? (1024 + base - 1) / base : (512 + base - 1) / base;
+  const uint64_t least = mode == kKeys ? 2 * kKeysStep : 512;
+  uint64_t split = std::max<uint64_t>(least, (span + want - 1) / want);
+  split = (split + kKeysStep - 1) / kKeysStep * kKeysStep;
+  a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
+  if (span <= split) a.n_splits = 1, split = span + 31;
+  a.split = (uint32_t)split;
+  if (base / s->n_seq * a.n_splits >= 1ull << 31) return fail(h, GRAND_E_CAPACITY, "max_q is too large");
+
+  Parts w;
+  const uint64_t all_rows = (uint64_t)s->n_tokens * p.q_heads;
+  const int w_part = a.n_splits > 1 ? w.add(all_rows * a.n_splits * p.head_dim * 4) : -1;
+  const int w_ml = a.n_splits > 1 ? w.add(all_rows * a.n_splits * 8) : -1;
+  int w_lse = -1, w_scores = -1;
+  if (weights_out) {
+    w_lse = w.add(all_rows * 4);
+    // scores of a few rows are kept (4 bytes a row and key, against half of
+    // the cache to compute them again)
+    const uint64_t keys = ((uint64_t)s->max_k + 31) / 32 * 32;
+    const uint64_t bytes = (uint64_t)s->n_seq * p.kv_heads * rows * keys * 4;
+    if (mode == kKeys && bytes <= 256ull << 20) {
+      w_scores = w.add(bytes);
+      a.score_rows = (uint32_t)rows;
+      a.score_keys = (uint32_t)keys;
+    }
+  }
+  TRY(ensure_ws(h, w.total));
+  if (w_part >= 0) a.part = (float *)(h->ws + w.at[w_part]);
+  if (w_ml >= 0) a.part_ml = (float2 *)(h->ws + w.at[w_ml]);
+  if (w_lse >= 0) a.lse2 = (float *)(h->ws + w.at[w_lse]);
+  if (w_scores >= 0) a.scores = (float *)(h->ws + w.at[w_scores]);
+  const bool f16 = p.dtype == GRAND_F16;
+  if (s->n_tokens && s->max_q) {
+    HCHK(h, launch_attend(mode, f16, a, h->stream));
+    if (a.n_splits > 1) HCHK(h, launch_attend_join(f16, a, tile_rows, h->stream));
+  }
+  if (weights_out && s->max_k) HCHK(h, launch_attend_weights(f16, a, h->stream));
+  return GRAND_OK;
+}
+
+grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_rows *q, const grand_pages *pages, const uint32_t *ids,
+                                    uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride, float scale, const grand_rows *prior,
+                                    const float *prior_lse, const grand_rows *out, float *lse) {
+  TRY(check_usable(h));
+  if (n_seq == 0) return GRAND_OK;
+  HCHK(h, hipSetDevice(h->p.device));
+  const grand_cache_params &p = h->p;
+  IdsArgs a{};
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
+  if (!prior != !prior_lse) return fail(h, GRAND_E_ARG, "prior and prior_lse come together");
+  if ((uint64_t)n_seq * p.q_heads >= 1u << 31) return fail(h, GRAND_E_CAPACITY, "too many rows");
+  if (k >= 1u << 30) return fail(h, GRAND_E_CAPACITY, "lists are too long");
+  TRY(check_pages(h, pages, &a.pg));
+  TRY(check_rows(h, "q", q, n_seq, p.q_heads, false, &a.q));
+  TRY(check_rows(h, "out", out, n_seq, p.q_heads, true, &a.out));
+  if (prior) {
+    TRY(check_rows(h, "prior", prior, n_seq, p.q_heads, false, &a.prior));
+    TRY(check_mem(h, "prior_lse", prior_lse, (uint64_t)n_seq * p.q_heads * 4, 4));
+  }
+  uint64_t e = 0;
+  if (!extent(n_seq, ids_seq_stride, p.q_heads, ids_head_stride, 1, 0, k, &e)) return fail(h, GRAND_E_ARG, "strides of ids are negative");
+  if (k) TRY(check_mem(h, "ids", ids, e * 4, 4));
+  if (lse) TRY(check_mem(h, "lse", lse, (uint64_t)n_seq * p.q_heads * 4, 4));
+  a.prior_lse = prior_lse;
+  a.lse = lse;
+  a.ids = ids;
+  a.ids_seq = ids_seq_stride;
+  a.ids_head = ids_head_stride;
+  a.n_seq = n_seq;
+  a.k = k;
+  a.q_heads = p.q_heads;
+  a.group = p.q_heads / p.kv_heads;
+  a.dim = p.head_dim;
+  a.c = scale * 1.44269504088896341f;
+  a.err = h->err;
+  HCHK(h, launch_attend_ids(p.dtype == GRAND_F16, a, h->stream));
+  return GRAND_OK;
+}
+
+grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t heads, uint32_t cap, const grand_weights *weights,
+                               const uint32_t *budget, uint32_t sinks, uint32_t recent, uint32_t *out_table,
+                               const grand_weights *out_weights, uint32_t *out_lens, uint32_t *freed, uint32_t *n_freed) {
+  TRY(check_usable(h));
+  if (s && s->n_seq == 0) return GRAND_OK;
+  HCHK(h, hipSetDevice(h->p.device));
+  EvictArgs a{};
+  TRY(check_seqs(h, s, false, &a.s));
+  if (heads == 0 || heads > 65535) return fail(h, GRAND_E_ARG, "heads must be 1..65535");
+  if (s->max_k > cap) return fail(h, GRAND_E_ARG, "max_k is above cap");
+  if (cap >= 1u << 31) return fail(h, GRAND_E_CAPACITY, "cap must be below 2^31");
+  if (cap) {
+    TRY(check_weights(h, "weights", weights, s->n_seq, heads, cap, false, &a.win));
+    TRY(check_weights(h, "out_weights", out_weights, s->n_seq, heads, cap, true, &a.wout));
+  }
+  TRY(check_mem(h, "budget", budget, (uint64_t)s->n_seq * 4, 4));
+  const uint64_t cells = (uint64_t)s->n_seq * s->max_pages;
+  if (s->max_pages) {
+    TRY(check_mem(h, "out_table", out_table, cells * 4, 4));
+    TRY(check_mem(h, "freed", freed, cells * 4, 4));
+  }
+  TRY(check_mem(h, "out_lens", out_lens, (uint64_t)s->n_seq * 4, 4));
+  TRY(check_mem(h, "n_freed", n_freed, (uint64_t)s->n_seq * 4, 4));
+  Parts w;
+  const int w_keys = w.add(cells * 4), w_map = w.add(cells * 4);
+  TRY(ensure_ws(h, w.total));
+  a.keys = (uint32_t *)(h->ws + w.at[w_keys]);
+  a.map = (uint32_t *)(h->ws + w.at[w_map]);
+  a.heads = heads;
+  a.page = h->p.page_size;
+  a.shift = h->shift;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.budget = budget;
+  a.out_table = out_table;
+  a.out_table_stride = s->max_pages;
+  a.out_lens = out_lens;
+  a.freed = freed;
+  a.freed_stride = s->max_pages;
+  a.n_freed = n_freed;
+  a.cap = cap;
+  a.err = h->err;
+  HCHK(h, launch_evict(a, h->stream));
+  return GRAND_OK;
+}
+
+}  // extern "C"

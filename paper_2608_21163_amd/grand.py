@@ -20,6 +20,7 @@ INVALID = 0xFFFFFFFF
 OK, E_ARG, E_ID, E_CAPACITY, E_DEVICE, E_OOM, E_STATE = 0, -1, -2, -3, -4, -5, -6
 VAMANA, CAGRA = 0, 1
 F32, U8 = 0, 1
+BF16, F16 = 2, 3
 L2, IP, MIPS = 0, 1, 2
 ALPHA_ON_DIST, ALPHA_ON_L2 = 0, 1
 CAS_GROUPED, CAS_RACING = 0, 1
@@ -33,7 +34,9 @@ PHASES = ["validate", "stage", "search_insert", "bootstrap", "prune_fwd", "group
 EXPORTED = ["grand_default_params", "grand_create", "grand_destroy", "grand_set_stream", "grand_insert_batch",
             "grand_build_cagra", "grand_delete_batch", "grand_search", "grand_search_static", "grand_count_in_edges", "grand_reader_create",
             "grand_reader_search", "grand_reader_destroy", "grand_reader_last_error", "grand_export_graph", "grand_import_graph", "grand_set_timing",
-            "grand_set_counting", "grand_stats", "grand_reset_stats", "grand_last_error"]
+            "grand_set_counting", "grand_stats", "grand_reset_stats", "grand_last_error",
+            "grand_default_cache_params", "grand_cache_create", "grand_cache_destroy", "grand_cache_set_stream", "grand_cache_check",
+            "grand_cache_last_error", "grand_cache_append", "grand_cache_attend", "grand_cache_attend_ids", "grand_cache_evict"]
 
 
 class GrandError(RuntimeError):
@@ -64,6 +67,31 @@ class Stats(ctypes.Structure):
                 ("repair_rows", ctypes.c_uint64), ("repair_records", ctypes.c_uint64),
                 ("search_distinct", ctypes.c_uint64 * 3), ("search_capped", ctypes.c_uint64 * 3),
                 ("phase_ms", ctypes.c_double * len(PHASES)), ("phase_calls", ctypes.c_uint64 * len(PHASES))]
+
+
+class CacheParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("q_heads", ctypes.c_uint32),
+                ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("page_size", ctypes.c_uint32),
+                ("device", ctypes.c_int32), ("stream", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_uint32),
+                ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Weights(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Seqs(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_uint32), ("n_tokens", ctypes.c_uint32), ("max_q", ctypes.c_uint32),
+                ("max_k", ctypes.c_uint32), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_uint32), ("q_start", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
 
 
 _lib = None
@@ -111,8 +139,21 @@ def load_library(path: str = LIB_PATH):
     lib.grand_reset_stats.argtypes = [P]
     lib.grand_last_error.argtypes = [P]
     lib.grand_last_error.restype = ctypes.c_char_p
+    lib.grand_default_cache_params.argtypes = [P]
+    lib.grand_cache_create.argtypes = [P, P]
+    lib.grand_cache_destroy.argtypes = [P]
+    lib.grand_cache_set_stream.argtypes = [P, P]
+    lib.grand_cache_check.argtypes = [P]
+    lib.grand_cache_last_error.argtypes = [P]
+    lib.grand_cache_last_error.restype = ctypes.c_char_p
+    F, I64 = ctypes.c_float, ctypes.c_int64
+    lib.grand_cache_append.argtypes = [P, P, P, P, P]
+    lib.grand_cache_attend.argtypes = [P, P, P, P, F, I32, U32, P, P, P, P]
+    lib.grand_cache_attend_ids.argtypes = [P, U32, P, P, P, U32, I64, I64, F, P, P, P, P]
+    lib.grand_cache_evict.argtypes = [P, P, U32, U32, P, P, U32, U32, P, P, P, P, P]
     for name in EXPORTED:
-        if name not in ("grand_default_params", "grand_last_error", "grand_reader_last_error"):
+        if name not in ("grand_default_params", "grand_last_error", "grand_reader_last_error",
+                        "grand_default_cache_params", "grand_cache_last_error"):
             getattr(lib, name).restype = I32
     _lib = lib
     return lib
@@ -362,3 +403,209 @@ class GrandIndex:
         out["phase_ms"] = {n: s.phase_ms[i] for i, n in enumerate(PHASES)}
         out["phase_calls"] = {n: s.phase_calls[i] for i, n in enumerate(PHASES)}
         return out
+
+
+class Sequences:
+    """The sequences of cache calls (grand_seqs); holds the tensors it names."""
+
+    def __init__(self, table, lens, q_start, n_tokens: int, max_q: int, max_k: int):
+        self.tensors = (table, lens, q_start)
+        self.n_seq, self.max_pages, self.n_tokens = table.shape[0], table.shape[1], n_tokens
+        self.max_q, self.max_k = max_q, max_k
+        self.c = Seqs(table.shape[0], n_tokens, max_q, max_k, table.data_ptr(), table.stride(0), table.shape[1],
+                      None if q_start is None else q_start.data_ptr(), lens.data_ptr())
+
+
+class Cache:
+    """The key/value-cache operators on one GPU (grand_cache_create ...
+    grand_cache_destroy).  Every tensor is a torch tensor of that GPU; the
+    calls enqueue work on the cache's stream and return.
+
+    Queries, results, new keys and values are (tokens, heads, head_dim), pages
+    (pages, page_size, kv_heads, head_dim) views of any layout whose rows are
+    contiguous and 16-byte aligned.  Ids, lengths and starts are 32-bit
+    integers; INVALID is -1 in an int32 tensor."""
+
+    def __init__(self, dtype: str = "bf16", q_heads: int = 32, kv_heads: int = 8, head_dim: int = 128, page_size: int = 16,
+                 device: int = 0, stream: Optional[int] = None):
+        import torch
+        self.lib = load_library()
+        p = CacheParams()
+        self.lib.grand_default_cache_params(ctypes.byref(p))
+        try:
+            p.dtype, self.torch_dtype = {"bf16": (BF16, torch.bfloat16), "f16": (F16, torch.float16)}[dtype]
+        except KeyError:
+            raise ValueError(f"dtype must be 'bf16' or 'f16', not {dtype!r}") from None
+        p.q_heads, p.kv_heads, p.head_dim, p.page_size, p.device = q_heads, kv_heads, head_dim, page_size, device
+        p.stream = stream
+        self.params = p
+        h = ctypes.c_void_p()
+        rc = self.lib.grand_cache_create(ctypes.byref(p), ctypes.byref(h))
+        if rc != OK:
+            raise GrandError(rc, "grand_cache_create failed")
+        self.h = h
+        self._torch = torch
+        self._q, self._kv, self._dim, self._page = q_heads, kv_heads, head_dim, page_size
+        self._int = (torch.int32, torch.uint32)
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.lib.grand_cache_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc: int) -> int:
+        if rc != OK:
+            raise GrandError(rc, self.last_error())
+        return rc
+
+    def last_error(self) -> str:
+        return self.lib.grand_cache_last_error(self.h).decode()
+
+    def set_stream(self, stream: int):
+        self._check(self.lib.grand_cache_set_stream(self.h, ctypes.c_void_p(stream)))
+
+    def check(self):
+        """Waits for the stream; raises if a kernel found an id, a length or
+        a start out of range since the last check."""
+        self._check(self.lib.grand_cache_check(self.h))
+
+    # ------------------------------------------------------------ arguments
+    def _ints(self, name, x, shape):
+        if x.dtype not in self._int or not x.is_cuda or tuple(x.shape) != shape:
+            raise ValueError(f"{name} must be a 32-bit integer tensor {shape} on the GPU")
+        if x.shape and x.shape[-1] > 1 and x.stride(-1) != 1:
+            raise ValueError(f"{name} must be contiguous along its last axis")
+
+    def _rows(self, name, x, heads, tokens=None):
+        if x.dtype != self.torch_dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self._dim or not x.is_cuda:
+            raise ValueError(f"{name} must be (tokens, {heads}, {self._dim}) {self.torch_dtype} on the GPU")
+        if x.stride(2) != 1:
+            raise ValueError(f"{name} must be contiguous along its last axis")
+        if tokens is not None and x.shape[0] != tokens:
+            raise ValueError(f"{name} must have {tokens} tokens")
+        return Rows(x.data_ptr(), x.stride(0), x.stride(1))
+
+    def _pages(self, k, v):
+        shape = (k.shape[0], self._page, self._kv, self._dim)
+        for name, x in (("k_pages", k), ("v_pages", v)):
+            if x.dtype != self.torch_dtype or tuple(x.shape) != shape or not x.is_cuda or x.stride(3) != 1:
+                raise ValueError(f"{name} must be (pages, {self._page}, {self._kv}, {self._dim}) {self.torch_dtype} on the "
+                                 "GPU, contiguous along its last axis")
+        if k.stride() != v.stride():
+            raise ValueError("k_pages and v_pages must have the same strides")
+        return Pages(k.data_ptr(), v.data_ptr(), k.shape[0], k.stride(0), k.stride(1), k.stride(2))
+
+    def _weights(self, name, w, n_seq, least, heads=None):
+        if (w.dtype != self._torch.float32 or w.dim() != 3 or w.shape[0] != n_seq or not w.is_cuda or w.shape[2] < least
+                or (heads is not None and w.shape[1] != heads) or (w.shape[2] > 1 and w.stride(2) != 1)):
+            raise ValueError(f"{name} must be ({n_seq}, heads, at least {least}) float32 on the GPU, contiguous along its last axis")
+        return Weights(w.data_ptr(), w.stride(0), w.stride(1))
+
+    def _lse(self, lse, tokens):
+        if lse is None:
+            return self._torch.empty((tokens, self._q), dtype=self._torch.float32, device=f"cuda:{self.params.device}")
+        if lse.dtype != self._torch.float32 or tuple(lse.shape) != (tokens, self._q) or not lse.is_contiguous() or not lse.is_cuda:
+            raise ValueError(f"lse must be a contiguous ({tokens}, {self._q}) float32 tensor on the GPU")
+        return lse
+
+    # ------------------------------------------------------------ operators
+    def sequences(self, table, lens, q_start=None, n_tokens: Optional[int] = None, max_q: int = 1,
+                  max_k: Optional[int] = None) -> Sequences:
+        """Describes the sequences of the calls that follow: table (sequences,
+        pages) page ids, lens cached tokens (new ones included), q_start
+        (sequences + 1) the new tokens' rows, or None for one each; max_q and
+        max_k bound new and cached tokens of a sequence.  n_tokens (the rows
+        of q) is taken from the rows themselves if not given."""
+        n = int(lens.shape[0])
+        self._ints("lens", lens, (n,))
+        if table.dim() != 2 or table.shape[0] != n:
+            raise ValueError("table must have a row for every sequence")
+        self._ints("table", table, tuple(table.shape))
+        if q_start is not None:
+            self._ints("q_start", q_start, (n + 1,))
+        if max_k is None:
+            max_k = int(table.shape[1]) * self._page
+        return Sequences(table, lens, q_start, n if q_start is None else (n_tokens or 0), max_q, max_k)
+
+    @staticmethod
+    def _tokens(s: Sequences, rows) -> int:
+        if s.tensors[2] is not None:
+            s.c.n_tokens = s.n_tokens = int(rows.shape[0])
+        return s.n_tokens
+
+    def append(self, seqs: Sequences, k, v, k_pages, v_pages):
+        """grand_cache_append: the new tokens' keys and values go into their pages."""
+        n = self._tokens(seqs, k)
+        rk, rv = self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n)
+        pg = self._pages(k_pages, v_pages)
+        self._check(self.lib.grand_cache_append(self.h, ctypes.byref(seqs.c), ctypes.byref(rk), ctypes.byref(rv),
+                                                ctypes.byref(pg)))
+
+    def attend(self, seqs: Sequences, q, k_pages, v_pages, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+               weights=None, weights_out=None, out=None, lse=None):
+        """grand_cache_attend: (out, lse), and with weights (sequences,
+        kv_heads, at least max_k) also weights_out (weights itself if not given)."""
+        n = self._tokens(seqs, q)
+        rq = self._rows("q", q, self._q, n)
+        if out is None:
+            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=q.device)
+        ro = self._rows("out", out, self._q, n)
+        lse = self._lse(lse, n)
+        pg = self._pages(k_pages, v_pages)
+        wi = wo = None
+        if weights is not None:
+            weights_out = weights if weights_out is None else weights_out
+            wi = self._weights("weights", weights, seqs.n_seq, seqs.max_k, self._kv)
+            wo = self._weights("weights_out", weights_out, seqs.n_seq, seqs.max_k, self._kv)
+        elif weights_out is not None:
+            raise ValueError("weights_out needs weights")
+        self._check(self.lib.grand_cache_attend(
+            self.h, ctypes.byref(seqs.c), ctypes.byref(rq), ctypes.byref(pg), self._dim ** -0.5 if scale is None else scale,
+            1 if causal else 0, window, ctypes.byref(ro), lse.data_ptr(), wi and ctypes.byref(wi), wo and ctypes.byref(wo)))
+        return (out, lse) if weights is None else (out, lse, weights_out)
+
+    def attend_ids(self, q, k_pages, v_pages, ids, scale: Optional[float] = None, prior=None, out=None, lse=None):
+        """grand_cache_attend_ids: one token per sequence over ids (sequences,
+        q_heads, k), e.g. the results of GrandIndex.search; prior: (out, lse)
+        of the same rows over other tokens.  Returns (out, lse)."""
+        n = int(q.shape[0])
+        rq = self._rows("q", q, self._q, n)
+        if ids.dim() != 3:
+            raise ValueError("ids must be (sequences, q_heads, k)")
+        self._ints("ids", ids, (n, self._q, ids.shape[2]))
+        if out is None:
+            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=q.device)
+        ro = self._rows("out", out, self._q, n)
+        lse = self._lse(lse, n)
+        pg = self._pages(k_pages, v_pages)
+        rp = zp = None
+        if prior is not None:
+            rp = self._rows("prior", prior[0], self._q, n)
+            zp = self._lse(prior[1], n).data_ptr()
+        self._check(self.lib.grand_cache_attend_ids(
+            self.h, n, ctypes.byref(rq), ctypes.byref(pg), ids.data_ptr(), ids.shape[2], ids.stride(0), ids.stride(1),
+            self._dim ** -0.5 if scale is None else scale, rp and ctypes.byref(rp), zp, ctypes.byref(ro), lse.data_ptr()))
+        return out, lse
+
+    def evict(self, seqs: Sequences, weights, budget, sinks: int = 0, recent: int = 0):
+        """grand_cache_evict: (table, weights, lens, freed, n_freed), the kept
+        pages of each sequence and the freed ones; budget is in pages."""
+        n, pages = seqs.n_seq, seqs.max_pages
+        wi = self._weights("weights", weights, n, seqs.max_k)
+        self._ints("budget", budget, (n,))
+        heads, cap = weights.shape[1], weights.shape[2]
+        empty, i32, dev = self._torch.empty, self._torch.int32, weights.device
+        table, freed = empty((n, pages), dtype=i32, device=dev), empty((n, pages), dtype=i32, device=dev)
+        lens, n_freed = empty(n, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
+        new = empty((n, heads, cap), dtype=self._torch.float32, device=dev)
+        wo = Weights(new.data_ptr(), new.stride(0), new.stride(1))
+        self._check(self.lib.grand_cache_evict(
+            self.h, ctypes.byref(seqs.c), heads, cap, ctypes.byref(wi), budget.data_ptr(), sinks, recent, table.data_ptr(),
+            ctypes.byref(wo), lens.data_ptr(), freed.data_ptr(), n_freed.data_ptr()))
+        return table, new, lens, freed, n_freed
