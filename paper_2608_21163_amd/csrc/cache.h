@@ -20,7 +20,7 @@ __device__ __forceinline__ void cache_err(CacheErr *e, uint32_t code, uint32_t w
 
 struct PagesView {
   const uint8_t *k, *v;
-  int64_t page, slot, head;  // strides in bytes
+  uint32_t page, slot, head; // strides in bytes; a page's rows lie within 2^32 bytes of its start
   uint32_t n_pages;
   uint32_t shift;            // log2 of the page size
 };
@@ -52,7 +52,7 @@ struct AttendArgs {
   uint32_t q_heads, kv_heads, group, dim;
   float scale;               // of the scores
   float c;                   // scale * log2(e)
-  uint32_t window;           // keys a row sees, its own included; 0xFFFFFFFF: all
+  uint32_t window;           // keys a row sees, its own included; 0: all; below 2^31
   int causal;
   // plan
   uint32_t row_tiles;        // row tiles of the longest chunk
@@ -106,13 +106,12 @@ struct EvictArgs {
   CacheErr *err;
 };
 
-// ROWS: the waves of a workgroup take different rows and share key tiles;
-// KEYS: they take the same rows and different keys.
-enum { kRows = 0, kKeys = 1 };
-constexpr uint32_t kKeysTileRows = 32, kRowsTileRows = 128;
-constexpr uint32_t kKeysStep = 128;  // keys a KEYS workgroup takes at once (four waves of 32)
+// Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
+// 128, its waves taking different rows.
+constexpr uint32_t kFewRows = 32, kRowsTileRows = 128;
+constexpr uint32_t kKeysStep = 128;  // keys that a workgroup of few rows takes at once (four waves of 32)
 
-hipError_t launch_attend(int mode, bool f16, const AttendArgs &a, hipStream_t st);
+hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);
 hipError_t launch_attend_join(bool f16, const AttendArgs &a, uint32_t tile_rows, hipStream_t st);
 hipError_t launch_attend_weights(bool f16, const AttendArgs &a, hipStream_t st);
 hipError_t launch_attend_ids(bool f16, const IdsArgs &a, hipStream_t st);
@@ -123,7 +122,7 @@ hipError_t launch_evict(const EvictArgs &a, hipStream_t st);
 // brought into range.
 struct Chunk {
   uint32_t r0, ql, kl;  // first token, chunk length, cached length
-  int64_t p0;           // position of the first new token (kl - ql; negative if it has no history)
+  int p0;               // position of the first new token (kl - ql; negative if the chunk is longer than the cache)
 };
 __device__ __forceinline__ Chunk chunk_of(const SeqsView &s, uint32_t b, CacheErr *err) {
   Chunk c;
@@ -141,7 +140,7 @@ __device__ __forceinline__ Chunk chunk_of(const SeqsView &s, uint32_t b, CacheEr
   c.r0 = r0;
   c.ql = r1 - r0;
   c.kl = kl;
-  c.p0 = (int64_t)kl - (int64_t)c.ql;
+  c.p0 = (int)kl - (int)c.ql;
   return c;
 }
 

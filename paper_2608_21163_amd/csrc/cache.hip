@@ -119,13 +119,18 @@ grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
   if (g->page_stride % 8 || g->slot_stride % 8 || g->head_stride % 8 ||
       !extent(g->n_pages, g->page_stride, h->p.page_size, g->slot_stride, h->p.kv_heads, g->head_stride, h->p.head_dim, &e))
     return fail(h, GRAND_E_ARG, "strides of pages must be multiples of 8 elements, not negative");
+  // offsets inside a page are computed in 32 bits
+  uint64_t in_page = 0;
+  if (!extent(1, 0, h->p.page_size, g->slot_stride, h->p.kv_heads, g->head_stride, h->p.head_dim, &in_page) || in_page >= 1ull << 31 ||
+      g->page_stride >= 1ll << 31 || g->slot_stride >= 1ll << 31 || g->head_stride >= 1ll << 31)
+    return fail(h, GRAND_E_CAPACITY, "a page and its strides must stay below 2^31 elements");
   TRY(check_mem(h, "pages.k", g->k, e * 2, 16));
   TRY(check_mem(h, "pages.v", g->v, e * 2, 16));
   out->k = static_cast<const uint8_t *>(g->k);
   out->v = static_cast<const uint8_t *>(g->v);
-  out->page = g->page_stride * 2;
-  out->slot = g->slot_stride * 2;
-  out->head = g->head_stride * 2;
+  out->page = (uint32_t)g->page_stride * 2;
+  out->slot = (uint32_t)g->slot_stride * 2;
+  out->head = (uint32_t)g->head_stride * 2;
   out->n_pages = g->n_pages;
   out->shift = h->shift;
   return GRAND_OK;
@@ -345,20 +350,24 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   a.scale = scale;
   a.c = scale * 1.44269504088896341f;
   a.causal = causal != 0;
-  a.window = window ? window : 0xFFFFFFFFu;
+  a.window = window < s->max_k ? window : 0;  // a window as long as the cache hides nothing
   a.err = h->err;
 
   const uint64_t rows = (uint64_t)a.s.max_q * a.group;
   if (rows >= 1u << 30) return fail(h, GRAND_E_CAPACITY, "max_q is too large");
-  const int mode = rows <= kKeysTileRows ? kKeys : kRows;
-  const uint32_t tile_rows = mode == kKeys ? kKeysTileRows : kRowsTileRows;
+  const bool few = rows <= kFewRows;
+  const uint32_t tile_rows = rows <= 16 ? 16 : few ? 32 : kRowsTileRows;
   a.row_tiles = (uint32_t)((rows + tile_rows - 1) / tile_rows);
-  // Keys a row tile sees at most, and the splits that give every CU work.
-  const uint64_t span = std::min<uint64_t>(s->max_k, window ? (uint64_t)window + std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) + 31 : s->max_k);
+  // Keys a row tile sees at most, and the splits of them.  A split costs a
+  // workgroup's start and end (about 6 us, behind the others' loads) and a
+  // row of sums to join; too few leave the last workgroups alone.  64 single
+  // tokens over 1 to 8,192 cached ones, 8 heads: 1,024 workgroups 222 us,
+  // 4,096 212 us, 8,192 216 us; two over 131,072: 211, 215, 222 us.  Chunks
+  // of 512 over up to 8,192: 512 workgroups 187 us, 1,024 162 us.
+  const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) + 31 : s->max_k);
   const uint64_t base = std::max<uint64_t>(1, (uint64_t)p.kv_heads * a.row_tiles * s->n_seq);
-  const uint64_t want = mode == kKeys ? (1024 + base - 1) / base : (512 + base - 1) / base;
-  const uint64_t least = mode == kKeys ? 2 * kKeysStep : 512;
-  uint64_t split = std::max<uint64_t>(least, (span + want - 1) / want);
+  const uint64_t want = ((few ? 4096 : 1024) + base - 1) / base;
+  uint64_t split = std::max<uint64_t>(256, (span + want - 1) / want);
   split = (split + kKeysStep - 1) / kKeysStep * kKeysStep;
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   if (span <= split) a.n_splits = 1, split = span + 31;
@@ -376,7 +385,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
     // the cache to compute them again)
     const uint64_t keys = ((uint64_t)s->max_k + 31) / 32 * 32;
     const uint64_t bytes = (uint64_t)s->n_seq * p.kv_heads * rows * keys * 4;
-    if (mode == kKeys && bytes <= 256ull << 20) {
+    if (few && bytes <= 256ull << 20) {
       w_scores = w.add(bytes);
       a.score_rows = (uint32_t)rows;
       a.score_keys = (uint32_t)keys;
@@ -389,7 +398,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   if (w_scores >= 0) a.scores = (float *)(h->ws + w.at[w_scores]);
   const bool f16 = p.dtype == GRAND_F16;
   if (s->n_tokens && s->max_q) {
-    HCHK(h, launch_attend(mode, f16, a, h->stream));
+    HCHK(h, launch_attend(tile_rows, f16, a, h->stream));
     if (a.n_splits > 1) HCHK(h, launch_attend_join(f16, a, tile_rows, h->stream));
   }
   if (weights_out && s->max_k) HCHK(h, launch_attend_weights(f16, a, h->stream));

@@ -27,18 +27,31 @@ struct Bf16 {
   typedef __bf16 T;
   typedef v8bf V;
   static __device__ __forceinline__ v16f mul(V a, V b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ v4f mul16(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
   static constexpr uint32_t kExp = 0x7C007C00u, kExpLow = 0x04000400u, kInf = 0x7C00u;
   typedef _Float16 T;
   typedef v8h V;
   static __device__ __forceinline__ v16f mul(V a, V b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ v4f mul16(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+// Both halves of the wave (both rows of 16 of each half) in every lane.
+template <class F> __device__ __forceinline__ float halves(float x, F f) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <class F> __device__ __forceinline__ float rows16(float x, F f) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float fadd2(float a, float b) { return a + b; }
 
 // The LDS writes of this workgroup (or wave) are visible after these; loads
 // from global memory stay in flight.
@@ -81,20 +94,35 @@ struct TileLoad {
       const uint32_t slot = min(key0 + row(i, t), end - 1) & mask;
       bad |= page[i] >= a.pg.n_pages;
       const uint32_t p = min(page[i], a.pg.n_pages - 1);
-      const int64_t off = (int64_t)p * a.pg.page + (int64_t)slot * a.pg.slot + (int64_t)kvh * a.pg.head + col(i, t) * 16;
-      if (DP == 64 || col(i, t) * 8 < (int)a.dim || (DP & (DP - 1)) == 0) {
-        const bool in = col(i, t) * 8 < (int)a.dim;
-        const int64_t o = in ? off : off - col(i, t) * 16;
-        k[i] = *(const v4u *)(a.pg.k + o);
-        v[i] = *(const v4u *)(a.pg.v + o);
-        if (!in) k[i] = v[i] = v4u{0, 0, 0, 0};
-      } else {
-        k[i] = v[i] = v4u{0, 0, 0, 0};
-      }
+      const bool in = col(i, t) * 8 < (int)a.dim;
+      const uint64_t off = (uint64_t)p * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head + (in ? col(i, t) * 16 : 0));
+      k[i] = *(const v4u *)(a.pg.k + off);
+      v[i] = *(const v4u *)(a.pg.v + off);
     }
     if (bad) cache_err(a.err, kCachePage, seq);
   }
-  __device__ __forceinline__ void store(uint8_t *lk, uint8_t *lv, int t) {
+  // Infinite and NaN values become 0; returns whether there were any.
+  template <class E>
+  __device__ __forceinline__ bool clear_non_finite() {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const uint32_t odd = ((v[i][j] & E::kExp) + E::kExpLow) & 0x80008000u;  // the sign bits of such elements
+        any |= odd;
+        v[i][j] &= ~((odd >> 15) * 0xFFFFu);
+      }
+    return any != 0;
+  }
+  // Elements past dim: the keys' are zeros, as the queries' are, the values'
+  // are whatever was loaded, as their sums are not written.
+  __device__ __forceinline__ void store(const AttendArgs &a, uint8_t *lk, uint8_t *lv, int t) {
+    if (a.dim != DP) {
+#pragma unroll
+      for (int i = 0; i < N; i++)
+        if (col(i, t) * 8 >= (int)a.dim) k[i] = v4u{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int i = 0; i < N; i++) {
       *(v4u *)(lk + row(i, t) * k_row<DP>() + col(i, t) * 16) = k[i];
@@ -108,7 +136,7 @@ template <class E, int DP>
 struct RowState {
   typename E::V q[DP / 16];
   v16f o[DP / 32];
-  float m, l;  // maximum (raw score units) and this lane's share of the sum
+  float m, l;  // what scores are taken against (log2 units; -inf: no key seen), this lane's share of the sum
 
   __device__ __forceinline__ void init(const AttendArgs &a, bool valid, uint32_t token, uint32_t head, int half) {
     m = neg_inf();
@@ -135,20 +163,30 @@ __device__ __forceinline__ v8s v_operand(const uint8_t *lv, int t, int d, int la
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Whether a value of the tile is infinite or NaN.  A hidden key's weight of
-// zero would make NaN of it.
-template <class E, int DP, int KT>
-__device__ __forceinline__ bool has_non_finite(const uint8_t *lv, int lane) {
-  uint32_t any = 0;
-  constexpr int NCH = DP / 8;
-#pragma unroll 4
-  for (int i = 0; i < KT * NCH / 64; i++) {
-    const int x = i * 64 + lane;
-    const v4u v = *(const v4u *)(lv + x / NCH * v_row<DP>() + x % NCH * 16);
+// Adds the infinite and NaN values of the keys [begin, end) (blocks of 32,
+// `step` apart) to the rows that see them.  Tiles with a key that is hidden
+// from some row hold zeros in their place, as a hidden key's weight of zero
+// would make NaN of them; in other tiles the product took them already, and
+// adding them again changes nothing.
+template <class E, int DP>
+__device__ __forceinline__ void add_non_finite(const AttendArgs &a, const uint32_t *table, uint32_t kvh, uint32_t begin, uint32_t end,
+                                               uint32_t step, int first, int last, int half, v16f *o) {
+  for (uint32_t k0 = begin; k0 < end; k0 += step)
+    for (uint32_t key = k0; key < min(k0 + 32, end); key++) {
+      const uint32_t page = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & ((1u << a.pg.shift) - 1);
+      const uint8_t *p = a.pg.v + (uint64_t)page * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head);
+      const bool see = (int)key >= first && (int)key <= last;
 #pragma unroll
-    for (int j = 0; j < 4; j++) any |= ((v[j] & E::kExp) + E::kExpLow) & 0x80008000u;
-  }
-  return __ballot(any != 0) != 0;
+      for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+          const int at = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
+          if (at < (int)a.dim) {
+            const uint16_t u = *(const uint16_t *)(p + at * 2);
+            if (see && (u & E::kInf) == E::kInf) o[d][i] += (float)__builtin_bit_cast(typename E::T, u);
+          }
+        }
+    }
 }
 
 // One tile of KT keys: scores, running softmax, weighted values.
@@ -157,7 +195,7 @@ __device__ __forceinline__ bool has_non_finite(const uint8_t *lv, int lane) {
 // hidden from some row of the wave.  emit(kb, s): sees the scores of block kb.
 template <class E, int DP, int KT, class F>
 __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk, const uint8_t *lv, float c, uint32_t key0,
-                                          bool masked, int64_t first, int64_t last, int lane, F emit) {
+                                          bool masked, int first, int last, int lane, F emit) {
   const int col = lane & 31, half = lane >> 5;
   v16f s[KT / 32];
 #pragma unroll
@@ -171,28 +209,39 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
     s[kb] = acc;
   }
   if (masked) {
+    // (opaque, or the compiler computes every comparison in every tile)
+    uint32_t k0 = key0;
+    asm volatile("" : "+s"(k0));
 #pragma unroll
     for (int kb = 0; kb < KT / 32; kb++)
 #pragma unroll
       for (int i = 0; i < 16; i++) {
-        const int64_t key = (int64_t)key0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        const int key = (int)k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
         if (key < first || key > last) s[kb][i] = neg_inf();
       }
   }
   emit(s);
-  float mx = st.m;
+  float mx = s[0][0];
 #pragma unroll
   for (int kb = 0; kb < KT / 32; kb++)
 #pragma unroll
     for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[kb][i]);
-  mx = fmaxf(mx, other_half(mx));
-  const float base = mx == neg_inf() ? 0.f : mx * c;
-  const float scale = ex2(st.m == neg_inf() ? neg_inf() : st.m * c - base);
+  mx = halves(mx, fmax2);
+  // The maximum that scores are taken against follows the true one only
+  // when that passes it by 2^8 for some row: sums and values then stay below
+  // 2^8 times what they would be, which loses nothing in floating point, and
+  // most tiles need no rescaling.
+  if (__ballot(mx * c > st.m + 8.f)) {
+    const float mn = fmaxf(st.m, mx * c);
+    const float scale = st.m == neg_inf() ? 0.f : ex2(st.m - mn);
 #pragma unroll
-  for (int d = 0; d < DP / 32; d++)
+    for (int d = 0; d < DP / 32; d++)
 #pragma unroll
-    for (int i = 0; i < 16; i++) st.o[d][i] *= scale;
-  st.m = mx;
+      for (int i = 0; i < 16; i++) st.o[d][i] *= scale;
+    st.l *= scale;
+    st.m = mn;
+  }
+  const float base = st.m == neg_inf() ? 0.f : st.m;
   // a tile's sum first: the running sum then takes one rounding a tile
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -203,36 +252,7 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
       s[kb][i] = p;
       sum[i % 4] += p;
     }
-  st.l = __builtin_fmaf(st.l, scale, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-  if (masked && has_non_finite<E, DP, KT>(lv, lane)) {
-    // finite values as ever, then the infinities and NaN one key at a time,
-    // to the rows that see it
-#pragma unroll
-    for (int t = 0; t < KT / 16; t++) {
-      typename E::V p;
-#pragma unroll
-      for (int j = 0; j < 8; j++) p[j] = (typename E::T)s[t / 2][(t % 2) * 8 + j];
-#pragma unroll
-      for (int d = 0; d < DP / 32; d++) {
-        v8s v = v_operand<E, DP>(lv, t, d, lane);
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = ((uint16_t)v[j] & E::kInf) == E::kInf ? (short)0 : v[j];
-        st.o[d] = E::mul(__builtin_bit_cast(typename E::V, v), p, st.o[d]);
-      }
-    }
-#pragma unroll 1
-    for (int k = 0; k < KT; k++) {
-      const bool see = (int64_t)key0 + k >= first && (int64_t)key0 + k <= last;
-#pragma unroll
-      for (int d = 0; d < DP / 32; d++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-          const uint16_t u = *(const uint16_t *)(lv + k * v_row<DP>() + (d * 32 + (i / 4) * 8 + half * 4 + i % 4) * 2);
-          if (see && (u & E::kInf) == E::kInf) st.o[d][i] += (float)__builtin_bit_cast(typename E::T, u);
-        }
-    }
-    return;
-  }
+  st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
   for (int t = 0; t < KT / 16; t++) {
     // the probabilities enter the product in 16 bits, as the values are; the
@@ -249,11 +269,11 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
 // The keys that rows [first token, last token] of a chunk see.
 __device__ __forceinline__ void key_range(const AttendArgs &a, const Chunk &c, uint32_t t0, uint32_t t1, uint32_t align,
                                           uint32_t &lo, uint32_t &hi) {
-  int64_t l = 0, h = c.kl;
-  if (a.causal) h = min(h, c.p0 + (int64_t)t1 + 1);
-  if (a.window != 0xFFFFFFFFu) l = max((int64_t)0, c.p0 + (int64_t)t0 - (int64_t)a.window + 1);
+  int l = 0, h = (int)c.kl;
+  if (a.causal) h = min(h, c.p0 + (int)t1 + 1);
+  if (a.window) l = max(0, c.p0 + (int)t0 - (int)a.window + 1);
   lo = (uint32_t)l / align * align;
-  hi = (uint32_t)max(h, (int64_t)lo);
+  hi = (uint32_t)max(h, (int)lo);
 }
 
 template <class E, int DP>
@@ -276,7 +296,7 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, const v16f *o, fl
         }
       }
     if (half == 0) {
-      const float z = l > 0.f || l != l ? m * a.c + lg2(l) : neg_inf();
+      const float z = l > 0.f || l != l ? m + lg2(l) : neg_inf();
       if (a.lse) a.lse[row] = z * kLn2;
       if (a.lse2) a.lse2[row] = z;
     }
@@ -289,7 +309,7 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, const v16f *o, fl
         const int at = d * 32 + (i / 4) * 8 + half * 4;
         if (at < (int)a.dim) *(v4f *)(p + at) = v4f{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
       }
-    if (half == 0) a.part_ml[row * a.n_splits + split] = make_float2(l > 0.f || l != l ? m * a.c : neg_inf(), l);
+    if (half == 0) a.part_ml[row * a.n_splits + split] = make_float2(l > 0.f || l != l ? m : neg_inf(), l);
   }
 }
 
@@ -308,21 +328,25 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
   const bool direct = a.n_splits == 1;
   const uint32_t begin = lo + split * a.split, end = min(hi, begin + a.split);
   if (split && begin >= hi) return;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, half = lane >> 5;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
   const uint32_t r = r0 + wave * 32 + (lane & 31), tok = min(r, r1) / a.group;
   const bool valid = r < rows;
   const uint32_t head = kvh * a.group + min(r, r1) % a.group;
   RowState<E, DP> st;
   st.init(a, valid, ch.r0 + tok, head, half);
-  const int64_t pos = ch.p0 + tok;
-  const int64_t last = a.causal ? min(pos, (int64_t)ch.kl - 1) : (int64_t)ch.kl - 1;
-  const int64_t first = a.window != 0xFFFFFFFFu ? pos - (int64_t)a.window + 1 : 0;
+  const int pos = ch.p0 + (int)tok;
+  const int last = a.causal ? min(pos, (int)ch.kl - 1) : (int)ch.kl - 1;
+  const int first = a.window ? pos - (int)a.window + 1 : 0;
   // positions of the wave's first and last row
   const uint32_t wr0 = min(r0 + wave * 32, r1), wr1 = min(r0 + wave * 32 + 31, r1);
-  const int64_t wfirst = a.window != 0xFFFFFFFFu ? ch.p0 + wr1 / a.group - (int64_t)a.window + 1 : 0;
-  const int64_t wlast = a.causal ? min(ch.p0 + wr0 / a.group, (int64_t)ch.kl - 1) : (int64_t)ch.kl - 1;
+  const int wfirst = a.window ? ch.p0 + (int)(wr1 / a.group) - (int)a.window + 1 : 0;
+  const int wlast = a.causal ? min(ch.p0 + (int)(wr0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
   if (begin < end) {
     const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
+    // the whole workgroup's rows see every key from all0 to all1
+    const int all0 = a.window ? ch.p0 + (int)(r1 / a.group) - (int)a.window + 1 : 0;
+    const int all1 = a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
+    bool odd = false;
     TileLoad<DP, KT, 256> ld;
     ld.pages(a, table, begin, end, t);
     ld.rows(a, begin, end, kvh, t, b);
@@ -330,120 +354,315 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
     int buf = 0;
     for (uint32_t key0 = begin; key0 < end; key0 += KT, buf ^= 1) {
       uint8_t *lk = smem + buf * tile_bytes<DP, KT>(), *lv = lk + KT * k_row<DP>();
-      ld.store(lk, lv, t);
+      if ((int)key0 < all0 || (int)key0 + KT - 1 > all1) odd |= ld.template clear_non_finite<E>();
+      ld.store(a, lk, lv, t);
       if (key0 + KT < end) {
         ld.rows(a, key0 + KT, end, kvh, t, b);
         ld.pages(a, table, min(key0 + 2 * KT, end - 1), end, t);
       }
       lds_barrier();
-      const bool masked = (int64_t)key0 < wfirst || (int64_t)key0 + KT - 1 > wlast || key0 + KT > end;
-      tile_step<E, DP, KT>(st, lk, lv, a.c, key0, masked, first, min(last, (int64_t)end - 1), lane, [](v16f *) {});
+      const bool masked = (int)key0 < wfirst || (int)key0 + KT - 1 > wlast || key0 + KT > end;
+      tile_step<E, DP, KT>(st, lk, lv, a.c, key0, masked, first, min(last, (int)end - 1), lane, [](v16f *) {});
     }
+    if (__syncthreads_or(odd)) add_non_finite<E, DP>(a, table, kvh, begin, end, 32, first, last, half, st.o);
   }
-  st.l += other_half(st.l);
+  st.l = halves(st.l, fadd2);
   if (valid) write_row<E, DP>(a, st.o, st.m, st.l, ch.r0 + tok, head, split, direct, half);
 }
 
-// Four waves of the same 32 rows, each over tiles of 32 keys of its own;
-// their sums are joined at the end.
-template <class E, int DP>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_keys(AttendArgs a) {
-  extern __shared__ uint8_t smem[];
-  __shared__ float2 ml[4][32];
-  const uint32_t kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const uint32_t rt = rest % a.row_tiles, split = rest / a.row_tiles, b = blockIdx.y;
+// Four waves of the same 16 NB rows, each over every fourth tile of 32 keys;
+// their sums are joined at the end.  For the few rows of single tokens and
+// short chunks: the time is that of the cache's bytes, so what counts is how
+// many loads are in flight and that each takes whole cache lines, past which
+// the caches are told not to keep them (an instruction reads whole rows of 2
+// to 8 keys).  A tile's keys, then its values pass through the same LDS.
+template <class E, int DP, int NB>
+__global__ __launch_bounds__(256, DP > 192 ? 1 : DP > 128 || NB > 1 ? 2 : 3) void k_attend_few(AttendArgs a) {
+  typedef typename E::V V;
+  constexpr int NS = DP / 32, KROW = k_row<DP>(), VROW = v_row<DP>(), ROWS = 16 * NB;
+  constexpr int LPR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;  // lanes that load a row, 16 bytes each (96, 192: some idle)
+  constexpr int N = LPR / 2;                               // consecutive keys of a tile that a lane loads a piece of
+  constexpr int kSum = DP + 4;  // floats of a row of the waves' sums
+  constexpr int kTiles = 4 * 32 * (VROW > KROW ? VROW : KROW), kSums = 4 * 16 * kSum * 4;
+  __shared__ __align__(16) uint8_t smem[kTiles > kSums ? kTiles : kSums];
+  __shared__ float2 ml[4][16];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, c = lane & 15;
+  // Workgroups go to the eight XCDs in turn.  A unit (sequence, row tile,
+  // split) has all its heads on one of them, one after the other: a slot's
+  // heads lie side by side, and an XCD that had one head only would read
+  // through an eighth of its L2 channels.
+  const uint32_t unit = blockIdx.x / (8 * a.kv_heads) * 8 + blockIdx.x % 8, kvh = blockIdx.x / 8 % a.kv_heads;
+  const uint32_t b = unit % a.s.n_seq, rt = unit / a.s.n_seq % a.row_tiles, split = unit / a.s.n_seq / a.row_tiles;
+  if (split >= a.n_splits) return;
+  const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
+  const int piece = lane % LPR, krow = lane / LPR * N;
+  const bool in = piece * 8 < (int)a.dim;
+  // pages of at least N slots hold all N keys
+  const bool one_page = a.pg.shift >= (DP <= 64 ? 2 : DP <= 128 ? 3 : 4);
+  // the first page ids are asked for together with the lengths where the
+  // split's first key does not depend on them
+  uint32_t page[N];
+  auto pages = [&](uint32_t key0) {
+    if (one_page) {
+      page[0] = table[min((key0 + krow) >> a.pg.shift, a.s.max_pages - 1)];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i++) page[i] = table[min((key0 + krow + i) >> a.pg.shift, a.s.max_pages - 1)];
+    }
+  };
+  pages(split * a.split + wave * 32);
   const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t rows = ch.ql * a.group, r0 = rt * kKeysTileRows;
+  const uint32_t rows = ch.ql * a.group, r0 = rt * ROWS;
   if (r0 >= rows) return;
-  const uint32_t r1 = min(rows, r0 + kKeysTileRows) - 1;
+  const uint32_t r1 = min(rows, r0 + ROWS) - 1;
   uint32_t lo, hi;
   key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
-  const bool direct = a.n_splits == 1;
   const uint32_t begin = lo + split * a.split, end = min(hi, begin + a.split);
   if (split && begin >= hi) return;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, half = lane >> 5;
-  const uint32_t r = r0 + (lane & 31), tok = min(r, r1) / a.group;
-  const bool valid = r < rows;
-  const uint32_t head = kvh * a.group + min(r, r1) % a.group;
-  RowState<E, DP> st;
-  st.init(a, valid, ch.r0 + tok, head, half);
-  const int64_t pos = ch.p0 + tok;
-  const int64_t last = a.causal ? min(pos, (int64_t)ch.kl - 1) : (int64_t)ch.kl - 1;
-  const int64_t first = a.window != 0xFFFFFFFFu ? pos - (int64_t)a.window + 1 : 0;
-  const int64_t wfirst = a.window != 0xFFFFFFFFu ? ch.p0 + r1 / a.group - (int64_t)a.window + 1 : 0;
-  const int64_t wlast = a.causal ? min(ch.p0 + r0 / a.group, (int64_t)ch.kl - 1) : (int64_t)ch.kl - 1;
-  uint8_t *lk = smem + wave * tile_bytes<DP, 32>(), *lv = lk + 32 * k_row<DP>();
+  if (lo) pages(begin + wave * 32);
+
+  V q[NB][NS];
+  int first[NB], last[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++) {
+    const uint32_t r = min(r0 + nb * 16 + c, r1), tok = r / a.group;
+    const uint8_t *p = a.q.p + (int64_t)(ch.r0 + tok) * a.q.token + (int64_t)(kvh * a.group + r % a.group) * a.q.head;
+#pragma unroll
+    for (int s = 0; s < NS; s++) {
+      v4u x{0, 0, 0, 0};
+      if ((s * 4 + g) * 8 < (int)a.dim) x = *(const v4u *)(p + (s * 4 + g) * 16);
+      q[nb][s] = __builtin_bit_cast(V, x);
+    }
+    const int pos = ch.p0 + (int)tok;
+    last[nb] = min(a.causal ? min(pos, (int)ch.kl - 1) : (int)ch.kl - 1, (int)end - 1);
+    first[nb] = a.window ? pos - (int)a.window + 1 : 0;
+  }
+  // every row sees the keys from all0 to all1
+  const int all0 = a.window ? ch.p0 + (int)(r1 / a.group) - (int)a.window + 1 : 0;
+  const int all1 = a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
+
+  v4f o[NB][DP / 16];
+  float m[NB], l[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++) {
+    m[nb] = neg_inf();
+    l[nb] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DP / 16; d++) o[nb][d] = v4f{0, 0, 0, 0};
+  }
+  // keys and values of the lane's N keys of a tile; a key at or past `end`
+  // reads some slot of the pool and is hidden
+  v4u kx[N], vx[N];
+  uint64_t off[N];
+  bool odd = false;
+  auto offsets = [&](uint32_t key0) {
+    bool bad = false;
+    const uint32_t mask = (1u << a.pg.shift) - 1, in_head = kvh * a.pg.head + (in ? piece * 16 : 0);
+    if (one_page) {
+      bad = page[0] >= a.pg.n_pages && key0 + krow < end;
+      off[0] = (uint64_t)min(page[0], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow) & mask) * a.pg.slot + in_head);
+#pragma unroll
+      for (int i = 1; i < N; i++) off[i] = off[i - 1] + a.pg.slot;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end;
+        off[i] = (uint64_t)min(page[i], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow + i) & mask) * a.pg.slot + in_head);
+      }
+    }
+    if (bad) cache_err(a.err, kCachePage, b);
+  };
+  auto load_k = [&] {
+#pragma unroll
+    for (int i = 0; i < N; i++) kx[i] = __builtin_nontemporal_load((const v4u *)(a.pg.k + off[i]));
+  };
+  auto load_v = [&] {
+#pragma unroll
+    for (int i = 0; i < N; i++) vx[i] = __builtin_nontemporal_load((const v4u *)(a.pg.v + off[i]));
+  };
+  uint8_t *lt = smem + wave * (kTiles / 4);
   uint32_t key0 = begin + wave * 32;
   if (key0 < end) {
-    const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
-    TileLoad<DP, 32, 64> ld;
-    ld.pages(a, table, key0, end, lane);
-    ld.rows(a, key0, end, kvh, lane, b);
-    ld.pages(a, table, min(key0 + kKeysStep, end - 1), end, lane);
+    offsets(key0);
+    load_k();
+    load_v();
+    pages(key0 + kKeysStep);
     for (; key0 < end; key0 += kKeysStep) {
-      lds_wave_fence();
-      ld.store(lk, lv, lane);
-      if (key0 + kKeysStep < end) {
-        ld.rows(a, key0 + kKeysStep, end, kvh, lane, b);
-        ld.pages(a, table, min(key0 + 2 * kKeysStep, end - 1), end, lane);
+      const bool masked = (int)key0 < all0 || (int)key0 + 31 > min(all1, (int)end - 1), more = key0 + kKeysStep < end;
+      if (a.dim != DP && !in) {
+#pragma unroll
+        for (int i = 0; i < N; i++) kx[i] = v4u{0, 0, 0, 0};
       }
       lds_wave_fence();
-      const bool masked = (int64_t)key0 < wfirst || (int64_t)key0 + 31 > wlast || key0 + 32 > end;
-      tile_step<E, DP, 32>(st, lk, lv, a.c, key0, masked, first, min(last, (int64_t)end - 1), lane, [&](v16f *s) {
-        if (a.scores && valid) {
-          float *p = a.scores + (((size_t)b * a.kv_heads + kvh) * a.score_rows + r) * a.score_keys + key0 + half * 4;
+      if (LPR * 8 == DP || piece * 8 < DP) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *(v4f *)(p + i * 2) = v4f{s[0][i] * a.c, s[0][i + 1] * a.c, s[0][i + 2] * a.c, s[0][i + 3] * a.c};
+        for (int i = 0; i < N; i++) *(v4u *)(lt + (krow + i) * KROW + piece * 16) = kx[i];
+      }
+      lds_wave_fence();
+      v4f sc[NB][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) {
+#pragma unroll
+        for (int nb = 0; nb < NB; nb++) sc[nb][kb] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < NS; s++) {
+          const v4u x = *(const v4u *)(lt + (kb * 16 + c) * KROW + (s * 4 + g) * 16);
+#pragma unroll
+          for (int nb = 0; nb < NB; nb++) sc[nb][kb] = E::mul16(__builtin_bit_cast(V, x), q[nb][s], sc[nb][kb]);
         }
-      });
+      }
+      if (masked) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const uint32_t bits = ((vx[i][j] & E::kExp) + E::kExpLow) & 0x80008000u;
+            if (key0 + krow + i < end) any |= bits;
+            vx[i][j] &= ~((bits >> 15) * 0xFFFFu);
+          }
+        odd |= any != 0;
+      }
+      lds_wave_fence();
+      if (LPR * 8 == DP || piece * 8 < DP) {
+#pragma unroll
+        for (int i = 0; i < N; i++) *(v4u *)(lt + (krow + i) * VROW + piece * 16) = vx[i];
+      }
+      if (more) {
+        offsets(key0 + kKeysStep);
+        load_k();
+        load_v();
+        pages(key0 + 2 * kKeysStep);
+      }
+      lds_wave_fence();
+      if (masked) {
+        uint32_t k0 = key0;
+        asm volatile("" : "+s"(k0));
+#pragma unroll
+        for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+          for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+              const int key = (int)k0 + kb * 16 + g * 4 + i;
+              if (key < first[nb] || key > last[nb]) sc[nb][kb][i] = neg_inf();
+            }
+      }
+      V p[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; nb++) {
+        if (a.scores && r0 + nb * 16 + c <= r1) {
+          float *to = a.scores + (((size_t)b * a.kv_heads + kvh) * a.score_rows + r0 + nb * 16 + c) * a.score_keys + key0 + g * 4;
+          *(v4f *)to = sc[nb][0] * a.c;
+          *(v4f *)(to + 16) = sc[nb][1] * a.c;
+        }
+        float mx = fmaxf(fmaxf(fmaxf(sc[nb][0][0], sc[nb][0][1]), fmaxf(sc[nb][0][2], sc[nb][0][3])),
+                         fmaxf(fmaxf(sc[nb][1][0], sc[nb][1][1]), fmaxf(sc[nb][1][2], sc[nb][1][3])));
+        mx = halves(rows16(mx, fmax2), fmax2) * a.c;
+        if (__ballot(mx > m[nb] + 8.f)) {  // as in tile_step
+          const float mn = fmaxf(m[nb], mx), scale = m[nb] == neg_inf() ? 0.f : ex2(m[nb] - mn);
+#pragma unroll
+          for (int d = 0; d < DP / 16; d++) o[nb][d] *= scale;
+          l[nb] *= scale;
+          m[nb] = mn;
+        }
+        const float base = m[nb] == neg_inf() ? 0.f : m[nb];
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float x = ex2(__builtin_fmaf(sc[nb][j / 4][j % 4], a.c, -base));
+          sum += x;
+          p[nb][j] = (typename E::T)x;
+        }
+        l[nb] += sum;
+      }
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) {
+        typedef __attribute__((address_space(3))) v4s *P;
+        const uint8_t *at = lt + (g * 4 + (c >> 2)) * VROW + (d * 16 + (c & 3) * 4) * 2;
+        const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)at), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 16 * VROW));
+        const V v = __builtin_bit_cast(V, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int nb = 0; nb < NB; nb++) o[nb][d] = E::mul16(v, p[nb], o[nb][d]);
+      }
+    }
+    if (__ballot(odd)) {  // as add_non_finite
+      for (uint32_t k0 = begin + wave * 32; k0 < end; k0 += kKeysStep)
+        for (uint32_t key = k0; key < min(k0 + 32, end); key++) {
+          const uint32_t pg = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & ((1u << a.pg.shift) - 1);
+          const uint8_t *p = a.pg.v + (uint64_t)pg * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head);
+#pragma unroll
+          for (int d = 0; d < DP / 16; d++) {
+            if (d * 16 + g * 4 < (int)a.dim) {
+              const uint2 x = *(const uint2 *)(p + (d * 16 + g * 4) * 2);
+#pragma unroll
+              for (int i = 0; i < 4; i++) {
+                const uint16_t u = (uint16_t)((i < 2 ? x.x : x.y) >> (i % 2 * 16));
+                if ((u & E::kInf) == E::kInf) {
+#pragma unroll
+                  for (int nb = 0; nb < NB; nb++)
+                    if ((int)key >= first[nb] && (int)key <= last[nb]) o[nb][d][i] += (float)__builtin_bit_cast(typename E::T, u);
+                }
+              }
+            }
+          }
+        }
     }
   }
-  st.l += other_half(st.l);
-  if (half == 0) ml[wave][lane] = make_float2(st.m, st.l);
-  __syncthreads();  // tiles are free, the waves' maxima known
-  float m = neg_inf(), l = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; w++) m = fmaxf(m, ml[w][lane & 31].x);
-#pragma unroll
-  for (int w = 0; w < 4; w++) {
-    const float2 x = ml[w][lane & 31];
-    l += x.x == neg_inf() ? x.y : x.y * ex2((x.x - m) * a.c);
-  }
-  const float scale = st.m == neg_inf() ? 1.f : ex2((st.m - m) * a.c);
-  // waves 3, 2, 1 add to one buffer in turn, wave 0 last
   float *sum = (float *)smem;
-  constexpr int kStride = DP + 4;
-  for (int w = 3; w >= 0; w--) {
-    if (wave == w) {
-      float *p = sum + (lane & 31) * kStride + half * 4;
 #pragma unroll
-      for (int d = 0; d < DP / 32; d++)
+  for (int nb = 0; nb < NB; nb++) {
+    __syncthreads();  // the tiles, or the sums of the rows before, are free
+    l[nb] = halves(rows16(l[nb], fadd2), fadd2);
+    if (g == 0) ml[wave][c] = make_float2(m[nb], l[nb]);
+    if (r0 + nb * 16 + c <= r1) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          v4f x{st.o[d][i] * scale, st.o[d][i + 1] * scale, st.o[d][i + 2] * scale, st.o[d][i + 3] * scale};
-          if (w < 3) {
-            const v4f y = *(v4f *)(p + d * 32 + i * 2);
-            x += y;
-          }
-          if (w > 0) {
-            *(v4f *)(p + d * 32 + i * 2) = x;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; j++) st.o[d][i + j] = x[j];
-          }
-        }
+      for (int d = 0; d < DP / 16; d++) *(v4f *)(sum + (wave * 16 + c) * kSum + d * 16 + g * 4) = o[nb][d];
     }
-    if (w) __syncthreads();
+    __syncthreads();
+    const uint32_t quads = a.dim / 4, rb = r0 + nb * 16, n = rb > r1 ? 0 : (min(r1, rb + 15) - rb + 1) * quads;
+    for (uint32_t x = t; x < n; x += 256) {
+      const uint32_t row = x / quads, d = x % quads * 4, r = rb + row;
+      float mm = neg_inf(), ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; w++) mm = fmaxf(mm, ml[w][row].x);
+      v4f v{0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < 4; w++) {
+        const float2 y = ml[w][row];
+        const float f = y.x == neg_inf() ? 1.f : ex2(y.x - mm);
+        ll += y.y * f;
+        v += *(const v4f *)(sum + (w * 16 + row) * kSum + d) * f;
+      }
+      const bool some = ll > 0.f || ll != ll;
+      const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
+      const size_t at = (size_t)token * a.q_heads + head;
+      if (a.n_splits == 1) {
+        const float inv = some ? 1.f / ll : 0.f;
+        typename E::T y[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) y[j] = (typename E::T)(v[j] * inv);
+        *(uint2 *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + d * 2) = *(uint2 *)y;
+        if (d == 0) {
+          const float z = some ? mm + lg2(ll) : neg_inf();
+          if (a.lse) a.lse[at] = z * kLn2;
+          if (a.lse2) a.lse2[at] = z;
+        }
+      } else {
+        *(v4f *)(a.part + (at * a.n_splits + split) * a.dim + d) = v;
+        if (d == 0) a.part_ml[at * a.n_splits + split] = make_float2(some ? mm : neg_inf(), ll);
+      }
+    }
   }
-  if (wave == 0 && valid) write_row<E, DP>(a, st.o, m, l, ch.r0 + tok, head, split, direct, half);
 }
 
-// Joins the splits of one row: four waves, every fourth split each.
-template <class E>
+// Joins the splits of one row: LQ lanes read one split's sums, 16 bytes each.
+template <class E, int LQ>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile_rows) {
+  constexpr int G = 256 / LQ, CHUNK = 1024;
   __shared__ float2 ml[4];
-  __shared__ float acc[4][256];
+  __shared__ float factor[CHUNK];
+  __shared__ v4f acc[256];
   const uint32_t b = blockIdx.y;
   const Chunk ch = chunk_of(a.s, b, a.err);
   const uint32_t kvh = blockIdx.x % a.kv_heads, r = blockIdx.x / a.kv_heads, rows = ch.ql * a.group;
@@ -454,10 +673,11 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile
   const uint32_t n = max(1u, (hi - lo + a.split - 1) / a.split);
   const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
   const size_t row = (size_t)token * a.q_heads + head;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float2 *parts = a.part_ml + row * a.n_splits;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   float m = neg_inf(), l = 0.f;
-  for (uint32_t s = wave * 64 + lane; s < n; s += 256) {
-    const float2 x = a.part_ml[row * a.n_splits + s];
+  for (uint32_t s = t; s < n; s += 256) {
+    const float2 x = parts[s];
     const float mn = fmaxf(m, x.x);
     l = (m == neg_inf() ? l : l * ex2(m - mn)) + (x.x == neg_inf() ? x.y : x.y * ex2(x.x - mn));
     m = mn;
@@ -476,49 +696,116 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile
 #pragma unroll
   for (int w = 0; w < 4; w++) l += ml[w].x == neg_inf() ? ml[w].y : ml[w].y * ex2(ml[w].x - m);
   v4f o{0, 0, 0, 0};
-  if (lane * 4 < (int)a.dim) {
-    for (uint32_t s = wave; s < n; s += 4) {
-      const float x = a.part_ml[row * a.n_splits + s].x;
-      const float f = x == neg_inf() ? 1.f : ex2(x - m);
-      o += *(const v4f *)(a.part + (row * a.n_splits + s) * a.dim + lane * 4) * f;
+  const int g = t / LQ, c = t % LQ;
+  for (uint32_t s0 = 0; s0 < n; s0 += CHUNK) {
+    const uint32_t m1 = min(n - s0, (uint32_t)CHUNK);
+    if (s0) __syncthreads();
+    for (uint32_t s = t; s < m1; s += 256) {
+      const float x = parts[s0 + s].x;
+      factor[s] = x == neg_inf() ? 1.f : ex2(x - m);
+    }
+    __syncthreads();
+    if (c * 4 < (int)a.dim) {
+      const float *p = a.part + (row * a.n_splits + s0) * a.dim + c * 4;
+#pragma unroll 4
+      for (uint32_t s = g; s < m1; s += G) o += *(const v4f *)(p + (size_t)s * a.dim) * factor[s];
     }
   }
-  *(v4f *)&acc[wave][lane * 4] = o;
+  acc[t] = o;
   __syncthreads();
-  const int d = threadIdx.x;
   const bool some = l > 0.f || l != l;
-  if (d < (int)a.dim) {
-    const float x = acc[0][d] + acc[1][d] + acc[2][d] + acc[3][d];
-    *(typename E::T *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + d * 2) =
-        (typename E::T)(some ? x / l : 0.f);
+  if (t < LQ && t * 4 < (int)a.dim) {
+    for (int i = 1; i < G; i++) o += acc[i * LQ + t];
+    const float inv = some ? 1.f / l : 0.f;
+    typename E::T y[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = (typename E::T)(o[j] * inv);
+    *(uint2 *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + t * 8) = *(uint2 *)y;
   }
-  if (d == 0) {
+  if (t == 0) {
     const float z = some ? m + lg2(l) : neg_inf();
     if (a.lse) a.lse[row] = z * kLn2;
     if (a.lse2) a.lse2[row] = z;
   }
 }
 
-// Weights from stored scores: a thread sums one key's weights over the rows.
-__global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
-  const uint32_t b = blockIdx.z, kvh = blockIdx.y;
+// The same for few splits and many rows: LQ lanes a row.
+constexpr uint32_t kShortSplits = 8;
+template <class E, int LQ>
+__global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_t tile_rows) {
+  const uint32_t b = blockIdx.y;
   const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t key = blockIdx.x * 256 + threadIdx.x;
-  if (key >= ch.kl) return;
-  float sum = a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key];
-  const uint32_t rows = ch.ql * a.group;
-  for (uint32_t r0 = 0; r0 < rows; r0 += kKeysTileRows) {
-    const uint32_t r1 = min(rows, r0 + kKeysTileRows);
-    uint32_t lo, hi;
-    key_range(a, ch, r0 / a.group, (r1 - 1) / a.group, 32, lo, hi);
-    if (key < lo || key >= hi) continue;
-    for (uint32_t r = r0; r < r1; r++) {
-      const float z = a.lse2[(size_t)(ch.r0 + r / a.group) * a.q_heads + kvh * a.group + r % a.group];
-      const float s = a.scores[(((size_t)b * a.kv_heads + kvh) * a.score_rows + r) * a.score_keys + key];
-      sum += z == neg_inf() ? 0.f : ex2(s - z);
-    }
+  const uint32_t x = blockIdx.x * (256 / LQ) + threadIdx.x / LQ, c = threadIdx.x % LQ, rows = ch.ql * a.group;
+  const uint32_t kvh = x % a.kv_heads, r = x / a.kv_heads;
+  if (r >= rows || c * 4 >= a.dim) return;
+  const uint32_t r0 = r / tile_rows * tile_rows, r1 = min(rows, r0 + tile_rows) - 1;
+  uint32_t lo, hi;
+  key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
+  const uint32_t n = min(max(1u, (hi - lo + a.split - 1) / a.split), kShortSplits);
+  const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
+  const size_t row = (size_t)token * a.q_heads + head;
+  float2 ml[kShortSplits];
+  v4f part[kShortSplits];
+  float m = neg_inf(), l = 0.f;
+#pragma unroll
+  for (uint32_t s = 0; s < kShortSplits; s++) {
+    ml[s] = s < n ? a.part_ml[row * a.n_splits + s] : make_float2(neg_inf(), 0.f);
+    part[s] = s < n ? *(const v4f *)(a.part + (row * a.n_splits + s) * a.dim + c * 4) : v4f{0, 0, 0, 0};
   }
-  a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] = sum;
+#pragma unroll
+  for (uint32_t s = 0; s < kShortSplits; s++) m = fmaxf(m, ml[s].x);
+  v4f o{0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t s = 0; s < kShortSplits; s++) {
+    const float f = ml[s].x == neg_inf() ? 1.f : ex2(ml[s].x - m);
+    l += ml[s].y * f;
+    o += part[s] * f;
+  }
+  const bool some = l > 0.f || l != l;
+  const float inv = some ? 1.f / l : 0.f;
+  typename E::T y[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) y[j] = (typename E::T)(o[j] * inv);
+  *(uint2 *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + c * 8) = *(uint2 *)y;
+  if (c == 0) {
+    const float z = some ? m + lg2(l) : neg_inf();
+    if (a.lse) a.lse[row] = z * kLn2;
+    if (a.lse2) a.lse2[row] = z;
+  }
+}
+
+// Weights from stored scores: a thread sums four keys' weights over the rows.
+__global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
+  __shared__ float z[kFewRows];
+  const uint32_t b = blockIdx.z, kvh = blockIdx.y, key0 = blockIdx.x * 1024 + threadIdx.x;
+  const Chunk ch = chunk_of(a.s, b, a.err);
+  if (blockIdx.x * 1024 >= ch.kl) return;
+  const uint32_t rows = ch.ql * a.group;  // one tile: at most kFewRows
+  if (threadIdx.x < rows) {
+    const float x = a.lse2[(size_t)(ch.r0 + threadIdx.x / a.group) * a.q_heads + kvh * a.group + threadIdx.x % a.group];
+    z[threadIdx.x] = x == neg_inf() ? __builtin_inff() : x;  // a row that sees nothing gives nothing
+  }
+  const float *win = a.win.p + (int64_t)b * a.win.seq + (int64_t)kvh * a.win.head;
+  float sum[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) sum[j] = key0 + j * 256 < ch.kl ? win[key0 + j * 256] : 0.f;
+  __syncthreads();
+  if (rows) {
+    uint32_t lo, hi;
+    key_range(a, ch, 0, (rows - 1) / a.group, 32, lo, hi);
+    const float *sc = a.scores + ((size_t)b * a.kv_heads + kvh) * a.score_rows * a.score_keys;
+#pragma unroll 4
+    for (uint32_t r = 0; r < rows; r++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const uint32_t key = key0 + j * 256;
+        if (key >= lo && key < hi) sum[j] += ex2(sc[(size_t)r * a.score_keys + key] - z[r]);
+      }
+  }
+  float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head;
+#pragma unroll
+  for (int j = 0; j < 4; j++)
+    if (key0 + j * 256 < ch.kl) wout[key0 + j * 256] = sum[j];
 }
 
 // Weights from scores computed again: a wave keeps 32 keys, the rows of the
@@ -539,7 +826,7 @@ __global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
     const uint32_t key = min(key0 + wave * 32 + col, ch.kl - 1);
     uint32_t p = a.s.table[(int64_t)b * a.s.table_stride + (key >> a.pg.shift)];
     p = min(p, a.pg.n_pages - 1);
-    const uint8_t *at = a.pg.k + (int64_t)p * a.pg.page + (int64_t)(key & ((1u << a.pg.shift) - 1)) * a.pg.slot + (int64_t)kvh * a.pg.head;
+    const uint8_t *at = a.pg.k + (uint64_t)p * a.pg.page + ((key & ((1u << a.pg.shift) - 1)) * a.pg.slot + kvh * a.pg.head);
 #pragma unroll
     for (int s = 0; s < DP / 16; s++) {
       v4u x{0, 0, 0, 0};
@@ -548,10 +835,10 @@ __global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
     }
   }
   // rows that see a key of this tile
-  const int64_t klast = min((int64_t)key0 + 127, (int64_t)ch.kl - 1);
-  int64_t t_lo = a.causal ? max((int64_t)0, (int64_t)key0 - ch.p0) : 0;
-  int64_t t_hi = a.window != 0xFFFFFFFFu ? min((int64_t)ch.ql, klast + (int64_t)a.window - ch.p0) : (int64_t)ch.ql;
-  const uint32_t r_lo = (uint32_t)min(t_lo, (int64_t)ch.ql) * a.group, r_hi = (uint32_t)max(t_hi, (int64_t)0) * a.group;
+  const int klast = (int)min(key0 + 128, ch.kl) - 1;
+  const int t_lo = a.causal ? max(0, (int)key0 - ch.p0) : 0;
+  const int t_hi = a.window ? min((int)ch.ql, klast + (int)a.window - ch.p0) : (int)ch.ql;
+  const uint32_t r_lo = (uint32_t)min(t_lo, (int)ch.ql) * a.group, r_hi = (uint32_t)max(t_hi, 0) * a.group;
   v16f acc{};
   constexpr int NCH = DP / 8, N = (32 * NCH + 255) / 256;
   v4u next[N];
@@ -589,15 +876,15 @@ __global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
       s = E::mul(k[x], __builtin_bit_cast(typename E::V, q), s);
     }
     const float z = lz[buf][col];
-    const int64_t p_lo = ch.p0 + r0 / a.group, p_hi = ch.p0 + min(r0 + 31, r_hi - 1) / a.group;
-    const bool masked = (a.causal && (int64_t)key0 + wave * 32 + 31 > p_lo) ||
-                        (a.window != 0xFFFFFFFFu && (int64_t)key0 + wave * 32 <= p_hi - (int64_t)a.window);
+    const int p_lo = ch.p0 + (int)(r0 / a.group), p_hi = ch.p0 + (int)(min(r0 + 31, r_hi - 1) / a.group);
+    const bool masked = (a.causal && (int)(key0 + wave * 32 + 31) > p_lo) ||
+                        (a.window && (int)(key0 + wave * 32) <= p_hi - (int)a.window);
     if (masked) {
-      const int64_t pos = ch.p0 + min(r0 + col, r_hi - 1) / a.group;
+      const int pos = ch.p0 + (int)(min(r0 + col, r_hi - 1) / a.group);
 #pragma unroll
       for (int i = 0; i < 16; i++) {
-        const int64_t key = (int64_t)key0 + wave * 32 + (i / 4) * 8 + half * 4 + i % 4;
-        if ((a.causal && key > pos) || (a.window != 0xFFFFFFFFu && key <= pos - (int64_t)a.window)) s[i] = neg_inf();
+        const int key = (int)key0 + wave * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[i] = neg_inf();
       }
     }
 #pragma unroll
@@ -618,22 +905,33 @@ __global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
 }
 
 template <class E, int DP>
-hipError_t attend_dim(int mode, const AttendArgs &a, hipStream_t st) {
-  const dim3 grid(a.kv_heads * a.row_tiles * a.n_splits, a.s.n_seq);
-  if (mode == kRows) {
-    constexpr int KT = DP > 128 ? 32 : 64;
-    k_attend_rows<E, DP, KT><<<grid, 256, 2 * tile_bytes<DP, KT>(), st>>>(a);
-  } else {
-    k_attend_keys<E, DP><<<grid, 256, 4 * tile_bytes<DP, 32>(), st>>>(a);
-  }
+hipError_t rows_dim(const AttendArgs &a, hipStream_t st) {
+  constexpr int KT = DP > 128 ? 32 : 64;
+  k_attend_rows<E, DP, KT><<<dim3(a.kv_heads * a.row_tiles * a.n_splits, a.s.n_seq), 256, 2 * tile_bytes<DP, KT>(), st>>>(a);
+  return hipGetLastError();
+}
+
+template <class E, int DP>
+hipError_t few_dim(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
+  const uint32_t units = (a.row_tiles * a.n_splits * a.s.n_seq + 7) / 8 * 8;
+  const dim3 grid(units * a.kv_heads);
+  if (tile_rows == 16) k_attend_few<E, DP, 1><<<grid, 256, 0, st>>>(a);
+  else k_attend_few<E, DP, 2><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <class E>
-hipError_t attend_type(int mode, const AttendArgs &a, hipStream_t st) {
-  if (a.dim <= 64) return attend_dim<E, 64>(mode, a, st);
-  if (a.dim <= 128) return attend_dim<E, 128>(mode, a, st);
-  return attend_dim<E, 256>(mode, a, st);
+hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) {
+  if (tile_rows == kRowsTileRows) {
+    if (a.dim <= 64) return rows_dim<E, 64>(a, st);
+    if (a.dim <= 128) return rows_dim<E, 128>(a, st);
+    return rows_dim<E, 256>(a, st);
+  }
+  if (a.dim <= 64) return few_dim<E, 64>(a, tile_rows, st);
+  if (a.dim <= 96) return few_dim<E, 96>(a, tile_rows, st);
+  if (a.dim <= 128) return few_dim<E, 128>(a, tile_rows, st);
+  if (a.dim <= 192) return few_dim<E, 192>(a, tile_rows, st);
+  return few_dim<E, 256>(a, tile_rows, st);
 }
 
 template <class E>
@@ -647,20 +945,32 @@ hipError_t weights_type(const AttendArgs &a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_attend(int mode, bool f16, const AttendArgs &a, hipStream_t st) {
-  return f16 ? attend_type<F16>(mode, a, st) : attend_type<Bf16>(mode, a, st);
+hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st) {
+  return f16 ? attend_type<F16>(tile_rows, a, st) : attend_type<Bf16>(tile_rows, a, st);
 }
 
-hipError_t launch_attend_join(bool f16, const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
-  const dim3 grid(a.s.max_q * a.q_heads, a.s.n_seq);
-  if (f16) k_attend_join<F16><<<grid, 256, 0, st>>>(a, tile_rows);
-  else k_attend_join<Bf16><<<grid, 256, 0, st>>>(a, tile_rows);
+template <class E>
+static hipError_t join_type(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
+  const uint32_t rows = a.s.max_q * a.q_heads;
+  if (a.n_splits <= kShortSplits) {
+    if (a.dim <= 64) k_attend_join_short<E, 16><<<dim3((rows + 15) / 16, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    else if (a.dim <= 128) k_attend_join_short<E, 32><<<dim3((rows + 7) / 8, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    else k_attend_join_short<E, 64><<<dim3((rows + 3) / 4, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    return hipGetLastError();
+  }
+  const dim3 grid(rows, a.s.n_seq);
+  if (a.dim <= 64) k_attend_join<E, 16><<<grid, 256, 0, st>>>(a, tile_rows);
+  else if (a.dim <= 128) k_attend_join<E, 32><<<grid, 256, 0, st>>>(a, tile_rows);
+  else k_attend_join<E, 64><<<grid, 256, 0, st>>>(a, tile_rows);
   return hipGetLastError();
+}
+hipError_t launch_attend_join(bool f16, const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
+  return f16 ? join_type<F16>(a, tile_rows, st) : join_type<Bf16>(a, tile_rows, st);
 }
 
 hipError_t launch_attend_weights(bool f16, const AttendArgs &a, hipStream_t st) {
   if (a.scores) {
-    k_weights_stored<<<dim3((a.s.max_k + 255) / 256, a.kv_heads, a.s.n_seq), 256, 0, st>>>(a);
+    k_weights_stored<<<dim3((a.s.max_k + 1023) / 1024, a.kv_heads, a.s.n_seq), 256, 0, st>>>(a);
     return hipGetLastError();
   }
   return f16 ? weights_type<F16>(a, st) : weights_type<Bf16>(a, st);

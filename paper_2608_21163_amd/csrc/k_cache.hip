@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void k_attend_ids(IdsArgs a) {
     for (int u = 0; u < U; u++) {
       kx[u] = vx[u] = v4u{0, 0, 0, 0};
       if (id[u] != kInvalid && in) {
-        const int64_t off = (int64_t)(id[u] >> a.pg.shift) * a.pg.page + (int64_t)(id[u] & mask) * a.pg.slot + (int64_t)kvh * a.pg.head + c * 16;
+        const uint64_t off = (uint64_t)(id[u] >> a.pg.shift) * a.pg.page + ((id[u] & mask) * a.pg.slot + kvh * a.pg.head + c * 16);
         kx[u] = *(const v4u *)(a.pg.k + off);
         vx[u] = *(const v4u *)(a.pg.v + off);
       }
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   const uint32_t x = blockIdx.x * 256 + threadIdx.x;
   const uint32_t c = x % nch, head = x / nch % a.kv_heads, i = x / nch / a.kv_heads;
   if (i >= ch.ql) return;
-  const int64_t pos = ch.p0 + i;
+  const int64_t pos = (int64_t)ch.p0 + i;
   if (pos < 0) {  // a chunk longer than its cache
     cache_err(a.err, kCacheLen, b);
     return;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
     cache_err(a.err, kCachePage, b);
     return;
   }
-  const int64_t to = (int64_t)page * a.pg.page + (int64_t)(pos & ((1u << a.pg.shift) - 1)) * a.pg.slot + (int64_t)head * a.pg.head + c * 16;
+  const uint64_t to = (uint64_t)page * a.pg.page + ((uint32_t)(pos & ((1u << a.pg.shift) - 1)) * a.pg.slot + head * a.pg.head + c * 16);
   const int64_t tok = ch.r0 + i;
   *(v4u *)(const_cast<uint8_t *>(a.pg.k) + to) = *(const v4u *)(a.k.p + tok * a.k.token + (int64_t)head * a.k.head + c * 16);
   *(v4u *)(const_cast<uint8_t *>(a.pg.v) + to) = *(const v4u *)(a.v.p + tok * a.v.token + (int64_t)head * a.v.head + c * 16);
