@@ -97,14 +97,17 @@ struct EvictArgs {
   uint32_t *out_lens, *freed, *n_freed;
   int64_t freed_stride;
   uint32_t cap;              // tokens of a weights row
+  int quads;                 // pages of weights are whole, aligned groups of four floats
   // workspace
   uint32_t *keys;            // n_seq x max_pages order keys (larger: kept first)
-  uint32_t *map;             // n_seq x max_pages: kept page -> old page
-  uint32_t *state;           // n_seq x kEvictState selection state
-  uint32_t *hist;            // n_seq x 4 x 256 digit counts
-  uint32_t *blk;             // n_seq x blocks x 2 tile counts
+  // tables above kEvictSmall pages only
+  uint32_t *hist;            // n_seq x 3 x 2048 digit counts
+  uint32_t *blk;             // n_seq x tiles x 2: keys above and at the threshold
+  uint32_t *state;           // n_seq x 2: the threshold, how many equal to it stay
   CacheErr *err;
 };
+
+constexpr uint32_t kEvictSmall = 16384, kEvictTile = 2048;  // pages
 
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.

@@ -468,10 +468,21 @@ grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t hea
   TRY(check_mem(h, "out_lens", out_lens, (uint64_t)s->n_seq * 4, 4));
   TRY(check_mem(h, "n_freed", n_freed, (uint64_t)s->n_seq * 4, 4));
   Parts w;
-  const int w_keys = w.add(cells * 4), w_map = w.add(cells * 4);
+  const int w_keys = w.add(cells * 4);
+  int w_hist = -1, w_blk = -1, w_state = -1;
+  if (s->max_pages > kEvictSmall) {
+    w_hist = w.add((uint64_t)s->n_seq * 3 * 2048 * 4);
+    w_blk = w.add((uint64_t)s->n_seq * ((s->max_pages + kEvictTile - 1) / kEvictTile) * 8);
+    w_state = w.add((uint64_t)s->n_seq * 8);
+  }
   TRY(ensure_ws(h, w.total));
   a.keys = (uint32_t *)(h->ws + w.at[w_keys]);
-  a.map = (uint32_t *)(h->ws + w.at[w_map]);
+  if (w_hist >= 0) {
+    a.hist = (uint32_t *)(h->ws + w.at[w_hist]);
+    a.blk = (uint32_t *)(h->ws + w.at[w_blk]);
+    a.state = (uint32_t *)(h->ws + w.at[w_state]);
+  }
+  a.quads = h->p.page_size >= 4 && (uintptr_t)a.win.p % 16 == 0 && a.win.seq % 4 == 0 && a.win.head % 4 == 0;
   a.heads = heads;
   a.page = h->p.page_size;
   a.shift = h->shift;

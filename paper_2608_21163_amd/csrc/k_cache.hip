@@ -205,111 +205,360 @@ __device__ __forceinline__ uint32_t order_key(float s) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(256) void k_evict_score(EvictArgs a) {
-  const uint32_t b = blockIdx.y, p = blockIdx.x * 256 + threadIdx.x;
-  const EvictSeq e = evict_seq(a, b);
-  if (p >= e.n) return;
-  uint32_t key = 0xFFFFFFFFu;
-  if (p >= a.sinks && p < e.tail0) {
-    float s = 0.f;
-    for (uint32_t h = 0; h < a.heads; h++) {
-      const float *w = a.win.p + (int64_t)b * a.win.seq + (int64_t)h * a.win.head + ((size_t)p << a.shift);
-      for (uint32_t i = 0; i < a.page; i++) s += w[i];
-    }
-    key = order_key(s);
+// A page's score, in the order of the definition: head by head, token by
+// token.  A page's tokens lie side by side, so 16 bytes at a time where that
+// is aligned (a.quads), 64 tokens' loads in flight: 64 sequences of 512 pages
+// of 16 with 8 heads take 4.6 us, one float at a time 17.7.
+__device__ __forceinline__ float page_score(const EvictArgs &a, uint32_t b, uint32_t p) {
+  const float *w = a.win.p + (int64_t)b * a.win.seq + ((size_t)p << a.shift);
+  float s = 0.f;
+  if (!a.quads) {
+    for (uint32_t h = 0; h < a.heads; h++)
+      for (uint32_t i = 0; i < a.page; i++) s += w[(int64_t)h * a.win.head + i];
+    return s;
   }
-  a.keys[(size_t)b * a.s.max_pages + p] = key;
+  const uint32_t heads_at_once = a.page <= 16 ? 4 : 1, quads = a.page / 4;
+  for (uint32_t h0 = 0; h0 < a.heads; h0 += heads_at_once)
+    for (uint32_t i0 = 0; i0 < quads; i0 += 16) {
+      float4 x[16];
+#pragma unroll
+      for (uint32_t j = 0; j < 16; j++) {
+        const uint32_t h = h0 + (heads_at_once == 4 ? j / 4 : 0), i = heads_at_once == 4 ? j % 4 : i0 + j;
+        const bool ok = h < a.heads && i < quads;
+        x[j] = ok ? *(const float4 *)(w + (int64_t)h * a.win.head + i * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < 16; j++) {
+        const uint32_t h = h0 + (heads_at_once == 4 ? j / 4 : 0), i = heads_at_once == 4 ? j % 4 : i0 + j;
+        if (h < a.heads && i < quads) s = (((s + x[j].x) + x[j].y) + x[j].z) + x[j].w;
+      }
+    }
+  return s;
+}
+__device__ __forceinline__ uint32_t page_key(const EvictArgs &a, const EvictSeq &e, uint32_t b, uint32_t p) {
+  return p < a.sinks || p >= e.tail0 ? 0xFFFFFFFFu : order_key(page_score(a, b, p));
 }
 
-// One workgroup per sequence: the threshold key by four passes of eight
-// bits, then the kept and the freed pages in order.
-__global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t sh[4];
-  __shared__ uint32_t wsum[16][2];
-  const uint32_t b = blockIdx.x;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+__global__ __launch_bounds__(64) void k_evict_score(EvictArgs a) {
+  const uint32_t b = blockIdx.y, p = blockIdx.x * 64 + threadIdx.x;
   const EvictSeq e = evict_seq(a, b);
-  const uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
-  uint32_t prefix = 0, left = e.keep;  // the left-th largest key among those with this prefix
-  if (e.keep < e.n) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (t < 256) hist[t] = 0;
-      __syncthreads();
-      for (uint32_t p = t; p < e.n; p += 1024) {
-        const uint32_t k = keys[p];
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+  if (p < e.n) a.keys[(size_t)b * a.s.max_pages + p] = page_key(a, e, b, p);
+}
+
+// The digit at which the number of larger digits reaches `left`: hist holds
+// BINS counts, every thread of the workgroup calls.  left becomes the rank
+// inside that digit.
+template <int BINS, int NT>
+__device__ __forceinline__ uint32_t find_digit(const uint32_t *hist, uint32_t &left, uint32_t *tmp) {
+  constexpr int PER = (BINS + NT - 1) / NT;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  uint32_t own = 0;
+  if (t * PER < BINS) {
+#pragma unroll
+    for (int i = 0; i < PER; i++) own += hist[t * PER + i];
+  }
+  uint32_t above = own;  // inclusive sum over the lanes from this one on
+#pragma unroll
+  for (int j = 1; j < 64; j <<= 1) {
+    const uint32_t x = (uint32_t)__shfl_down((int)above, j, 64);
+    if (lane + j < 64) above += x;
+  }
+  if (lane == 0) tmp[wave] = above;
+  __syncthreads();
+  for (int w = wave + 1; w < NT / 64; w++) above += tmp[w];
+  above -= own;  // keys in later threads' digits
+  if (own && above < left && above + own >= left) {
+    uint32_t at = above;
+    for (int i = PER - 1; i >= 0; i--) {
+      const uint32_t h = hist[t * PER + i];
+      if (at + h >= left) {
+        tmp[NT / 64] = (uint32_t)(t * PER + i);
+        tmp[NT / 64 + 1] = left - at;
+        break;
       }
-      __syncthreads();
-      if (t == 0) {
-        uint32_t above = 0;
-        int d = 255;
-        for (; d > 0 && above + hist[d] < left; d--) above += hist[d];
-        sh[0] = prefix | ((uint32_t)d << shift);
-        sh[1] = left - above;
-      }
-      __syncthreads();
-      prefix = sh[0];
-      left = sh[1];
-      __syncthreads();
+      at += h;
     }
   }
-  // keys above `prefix` stay, and the first `left` equal to it
+  __syncthreads();
+  const uint32_t d = tmp[NT / 64];
+  left = tmp[NT / 64 + 1];
+  __syncthreads();
+  return d;
+}
+
+// Pages [p0, p1) of a sequence: kept ones go to their places in the table,
+// with their tokens' weights, freed ones to the list.  Keys above thr stay,
+// and the first `left` equal to it; above0 and equal0 count such keys before
+// p0.  512 threads.
+template <class Keys>
+__device__ void evict_slice(const EvictArgs &a, const EvictSeq &e, uint32_t b, uint32_t thr, uint32_t left, uint32_t p0, uint32_t p1,
+                            uint32_t above0, uint32_t equal0, Keys keys) {
+  __shared__ uint32_t list[512];
+  __shared__ uint32_t wsum[8][2];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
   uint32_t *out = a.out_table + (int64_t)b * a.out_table_stride, *freed = a.freed + (int64_t)b * a.freed_stride;
-  uint32_t *map = a.map + (size_t)b * a.s.max_pages;
-  uint32_t eq0 = 0, kept0 = 0;
-  for (uint32_t p0 = 0; p0 < a.s.max_pages; p0 += 1024) {
-    const uint32_t p = p0 + t;
-    const bool live = p < e.n;
-    const uint32_t k = live ? keys[p] : 0;
-    const bool all = e.keep >= e.n, eq = live && !all && k == prefix;
-    const uint64_t eqm = ballot(eq);
-    if (lane == 0) wsum[wave][0] = popc(eqm);
-    __syncthreads();
-    uint32_t before = eq0;
-    for (int w = 0; w < wave; w++) before += wsum[w][0];
-    const bool keep = live && (all || k > prefix || (eq && before + mbcnt(eqm) < left));
-    const uint64_t km = ballot(keep);
-    if (lane == 0) wsum[wave][1] = popc(km);
-    __syncthreads();
-    uint32_t at = kept0, eqn = 0, kn = 0;
-    for (int w = 0; w < 16; w++) {
-      if (w < wave) at += wsum[w][1];
-      eqn += wsum[w][0];
-      kn += wsum[w][1];
+  const bool all = e.keep >= e.n;
+  for (uint32_t q0 = p0; q0 < p1; q0 += 512) {
+    const uint32_t p = q0 + t;
+    const bool live = p < p1;
+    const uint32_t k = live ? keys(p) : 0;
+    const uint32_t id = live ? table[p] : 0;
+    const uint64_t am = ballot(live && (all || k > thr)), em = ballot(live && !all && k == thr);
+    if (lane == 0) {
+      wsum[wave][0] = popc(am);
+      wsum[wave][1] = popc(em);
     }
-    at += mbcnt(km);  // pages kept before p
+    __syncthreads();
+    uint32_t above = above0 + mbcnt(am), equal = equal0 + mbcnt(em), an = above0, en = equal0;
+#pragma unroll
+    for (int w = 0; w < 8; w++) {
+      if (w < wave) {
+        above += wsum[w][0];
+        equal += wsum[w][1];
+      }
+      an += wsum[w][0];
+      en += wsum[w][1];
+    }
+    const uint32_t kept0 = above0 + min(equal0, left), at = above + min(equal, left);  // kept before q0, before p
     if (live) {
+      const bool keep = all || k > thr || (k == thr && equal < left);
       if (keep) {
-        out[at] = table[p];
-        map[at] = p;
+        out[at] = id;
+        list[at - kept0] = p;
       } else {
-        freed[p - at] = table[p];
+        freed[p - at] = id;
       }
     }
-    eq0 += eqn;
-    kept0 += kn;
+    above0 = an;
+    equal0 = en;
+    const uint32_t kept1 = above0 + min(equal0, left);
     __syncthreads();
-  }
-  for (uint32_t p = kept0 + t; p < a.s.max_pages; p += 1024) out[p] = kInvalid;
-  for (uint32_t p = e.n - kept0 + t; p < a.s.max_pages; p += 1024) freed[p] = kInvalid;
-  if (t == 0) {
-    a.out_lens[b] = e.len - ((e.n - kept0) << a.shift);
-    a.n_freed[b] = e.n - kept0;
+    // the last page of the sequence may be partly filled
+    const uint32_t first = kept0 << a.shift, n = min(kept1 << a.shift, e.len - ((e.n - e.keep) << a.shift));
+    const float *win = a.win.p + (int64_t)b * a.win.seq;
+    float *wout = a.wout.p + (int64_t)b * a.wout.seq;
+    for (uint32_t j = first + t; j < n; j += 512) {
+      const size_t from = ((size_t)list[(j >> a.shift) - kept0] << a.shift) + (j & (a.page - 1));
+      for (uint32_t h0 = 0; h0 < a.heads; h0 += 8) {
+        float x[8];
+#pragma unroll
+        for (uint32_t h = 0; h < 8; h++)
+          if (h0 + h < a.heads) x[h] = win[(int64_t)(h0 + h) * a.win.head + from];
+#pragma unroll
+        for (uint32_t h = 0; h < 8; h++)
+          if (h0 + h < a.heads) wout[(int64_t)(h0 + h) * a.wout.head + j] = x[h];
+      }
+    }
+    __syncthreads();
   }
 }
 
-// Weights of the kept tokens move to their new places; zeros behind them.
-__global__ __launch_bounds__(256) void k_evict_pack(EvictArgs a) {
-  const uint32_t b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= a.cap) return;
-  float x = 0.f;
-  if (j < a.out_lens[b]) {
-    const uint32_t p = a.map[(size_t)b * a.s.max_pages + (j >> a.shift)];
-    x = a.win.p[(int64_t)b * a.win.seq + (int64_t)h * a.win.head + ((size_t)p << a.shift) + (j & (a.page - 1))];
+// What lies behind the kept pages, by `parts` workgroups of 512 threads.
+__device__ __forceinline__ void evict_tails(const EvictArgs &a, const EvictSeq &e, uint32_t b, uint32_t part, uint32_t parts) {
+  const uint32_t step = parts * 512, i0 = part * 512 + threadIdx.x, gone = e.n - e.keep, len = e.len - (gone << a.shift);
+  uint32_t *out = a.out_table + (int64_t)b * a.out_table_stride, *freed = a.freed + (int64_t)b * a.freed_stride;
+  for (uint32_t p = e.keep + i0; p < a.s.max_pages; p += step) out[p] = kInvalid;
+  for (uint32_t p = gone + i0; p < a.s.max_pages; p += step) freed[p] = kInvalid;
+  for (uint32_t h = 0; h < a.heads; h++) {
+    float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)h * a.wout.head;
+    for (uint32_t j = len + i0; j < a.cap; j += step) wout[j] = 0.f;
   }
-  a.wout.p[(int64_t)b * a.wout.seq + (int64_t)h * a.wout.head + j] = x;
+  if (i0 == 0) {
+    a.out_lens[b] = len;
+    a.n_freed[b] = gone;
+  }
+}
+
+// Tables of up to kEvictSmall pages: every workgroup of a sequence takes all
+// its keys into LDS, finds the threshold by four passes of eight bits, and
+// moves its slice of the pages.  Finding it once per slice costs no launch.
+__global__ __launch_bounds__(512) void k_evict_small(EvictArgs a) {
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t hist[256], tmp[10];
+  const uint32_t b = blockIdx.y, slice = (a.s.max_pages + gridDim.x - 1) / gridDim.x;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const EvictSeq e = evict_seq(a, b);
+  evict_tails(a, e, b, blockIdx.x, gridDim.x);
+  const uint32_t p0 = blockIdx.x * slice, p1 = min(e.n, p0 + slice);
+  if (p0 >= p1) return;
+  const uint32_t *src = a.keys + (size_t)b * a.s.max_pages;
+  for (uint32_t p = t; p < e.n; p += 512) keys[p] = src[p];
+  uint32_t thr = 0, left = e.keep;
+  if (e.keep < e.n) {
+    if (e.keep == 0) {
+      thr = 0xFFFFFFFFu;  // no key is larger
+      left = 0;
+    } else {
+      for (int shift = 24; shift >= 0; shift -= 8) {
+        if (t < 256) hist[t] = 0;
+        __syncthreads();
+        for (uint32_t p = t; p < e.n; p += 512) {
+          const uint32_t k = keys[p];
+          if (shift == 24 || (k >> (shift + 8)) == (thr >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+        }
+        __syncthreads();
+        thr |= find_digit<256, 512>(hist, left, tmp) << shift;
+      }
+    }
+  }
+  __syncthreads();
+  // keys above and at the threshold before the slice
+  uint32_t above = 0, equal = 0;
+  for (uint32_t p = t; p < p0; p += 512) {
+    above += e.keep >= e.n || keys[p] > thr;
+    equal += e.keep < e.n && keys[p] == thr;
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) {
+    above += (uint32_t)__shfl_xor((int)above, j, 64);
+    equal += (uint32_t)__shfl_xor((int)equal, j, 64);
+  }
+  if (lane == 0) {
+    hist[wave] = above;
+    hist[8 + wave] = equal;
+  }
+  __syncthreads();
+  above = equal = 0;
+#pragma unroll
+  for (int w = 0; w < 8; w++) {
+    above += hist[w];
+    equal += hist[8 + w];
+  }
+  evict_slice(a, e, b, thr, left, p0, p1, above, equal, [&](uint32_t p) { return keys[p]; });
+}
+
+// Longer tables, tiles of kEvictTile pages: digits of 11, 11 and 10 bits are
+// counted by all workgroups together, one launch a digit, then each tile's
+// keys above and at the threshold, then the tiles move.
+constexpr uint32_t kBins = 2048;
+__device__ __forceinline__ uint32_t *evict_hist(const EvictArgs &a, uint32_t b, int pass) { return a.hist + ((size_t)b * 3 + pass) * kBins; }
+
+__global__ __launch_bounds__(512) void k_evict_clear(EvictArgs a) {
+  const size_t i = (size_t)blockIdx.x * 512 + threadIdx.x;
+  if (i < (size_t)a.s.n_seq * 3 * kBins) a.hist[i] = 0;
+}
+
+// The threshold's digits of the passes before `pass`.
+__device__ __forceinline__ void evict_prefix(const EvictArgs &a, const EvictSeq &e, uint32_t b, int pass, uint32_t *tmp, uint32_t &thr,
+                                             uint32_t &left) {
+  thr = 0;
+  left = e.keep;
+  if (pass > 0) thr |= find_digit<2048, 512>(evict_hist(a, b, 0), left, tmp) << 21;
+  if (pass > 1) thr |= find_digit<2048, 512>(evict_hist(a, b, 1), left, tmp) << 10;
+  if (pass > 2) thr |= find_digit<1024, 512>(evict_hist(a, b, 2), left, tmp);
+}
+
+template <int PASS>
+__global__ __launch_bounds__(512) void k_evict_digit(EvictArgs a) {
+  __shared__ uint32_t hist[kBins], tmp[10];
+  const uint32_t b = blockIdx.y, p0 = blockIdx.x * kEvictTile;
+  const int t = threadIdx.x;
+  const EvictSeq e = evict_seq(a, b);
+  if (p0 >= e.n) return;
+  const uint32_t p1 = min(e.n, p0 + kEvictTile);
+  uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
+  uint32_t thr = 0, left = 0;
+  if (e.keep > 0 && e.keep < e.n) evict_prefix(a, e, b, PASS, tmp, thr, left);
+  for (int i = t; i < (int)kBins; i += 512) hist[i] = 0;
+  __syncthreads();
+  for (uint32_t p = p0 + t; p < p1; p += 512) {
+    uint32_t k;
+    if (PASS == 0) keys[p] = k = page_key(a, e, b, p);
+    else k = keys[p];
+    if (PASS == 0) atomicAdd(&hist[k >> 21], 1u);
+    if (PASS == 1 && (k >> 21) == (thr >> 21)) atomicAdd(&hist[(k >> 10) & 2047], 1u);
+    if (PASS == 2 && (k >> 10) == (thr >> 10)) atomicAdd(&hist[k & 1023], 1u);
+  }
+  __syncthreads();
+  uint32_t *sum = evict_hist(a, b, PASS);
+  for (int i = t; i < (int)kBins; i += 512)
+    if (hist[i]) atomicAdd(&sum[i], hist[i]);
+}
+
+__device__ __forceinline__ void evict_threshold(const EvictArgs &a, const EvictSeq &e, uint32_t b, uint32_t *tmp, uint32_t &thr, uint32_t &left) {
+  if (e.keep >= e.n) {
+    thr = 0;
+    left = e.keep;
+  } else if (e.keep == 0) {
+    thr = 0xFFFFFFFFu;
+    left = 0;
+  } else {
+    evict_prefix(a, e, b, 3, tmp, thr, left);
+  }
+}
+
+__global__ __launch_bounds__(512) void k_evict_count(EvictArgs a) {
+  __shared__ uint32_t tmp[10], sum[8][2];
+  const uint32_t b = blockIdx.y, p0 = blockIdx.x * kEvictTile;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const EvictSeq e = evict_seq(a, b);
+  if (p0 >= e.n) return;
+  uint32_t thr, left, above = 0, equal = 0;
+  evict_threshold(a, e, b, tmp, thr, left);
+  const uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
+  for (uint32_t p = p0 + t; p < min(e.n, p0 + kEvictTile); p += 512) {
+    const uint32_t k = keys[p];
+    above += e.keep >= e.n || k > thr;
+    equal += e.keep < e.n && k == thr;
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) {
+    above += (uint32_t)__shfl_xor((int)above, j, 64);
+    equal += (uint32_t)__shfl_xor((int)equal, j, 64);
+  }
+  if (lane == 0) {
+    sum[wave][0] = above;
+    sum[wave][1] = equal;
+  }
+  __syncthreads();
+  if (t == 0) {
+    above = equal = 0;
+    for (int w = 0; w < 8; w++) {
+      above += sum[w][0];
+      equal += sum[w][1];
+    }
+    uint32_t *blk = a.blk + ((size_t)b * gridDim.x + blockIdx.x) * 2;
+    blk[0] = above;
+    blk[1] = equal;
+    if (blockIdx.x == 0) {
+      a.state[b * 2] = thr;
+      a.state[b * 2 + 1] = left;
+    }
+  }
+}
+
+__global__ __launch_bounds__(512) void k_evict_move(EvictArgs a) {
+  __shared__ uint32_t sum[8][2];
+  const uint32_t b = blockIdx.y, p0 = blockIdx.x * kEvictTile;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const EvictSeq e = evict_seq(a, b);
+  evict_tails(a, e, b, blockIdx.x, gridDim.x);
+  if (p0 >= e.n) return;
+  uint32_t above = 0, equal = 0;
+  const uint32_t *blk = a.blk + (size_t)b * gridDim.x * 2;
+  for (uint32_t i = t; i < blockIdx.x; i += 512) {
+    above += blk[i * 2];
+    equal += blk[i * 2 + 1];
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) {
+    above += (uint32_t)__shfl_xor((int)above, j, 64);
+    equal += (uint32_t)__shfl_xor((int)equal, j, 64);
+  }
+  if (lane == 0) {
+    sum[wave][0] = above;
+    sum[wave][1] = equal;
+  }
+  __syncthreads();
+  above = equal = 0;
+#pragma unroll
+  for (int w = 0; w < 8; w++) {
+    above += sum[w][0];
+    equal += sum[w][1];
+  }
+  const uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
+  evict_slice(a, e, b, a.state[b * 2], a.state[b * 2 + 1], p0, min(e.n, p0 + kEvictTile), above, equal, [&](uint32_t p) { return keys[p]; });
 }
 
 template <class E>
@@ -334,9 +583,21 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t st) {
-  k_evict_score<<<dim3((a.s.max_pages + 255) / 256, a.s.n_seq), 256, 0, st>>>(a);
-  k_evict_select<<<a.s.n_seq, 1024, 0, st>>>(a);
-  k_evict_pack<<<dim3((a.cap + 255) / 256, a.heads, a.s.n_seq), 256, 0, st>>>(a);
+  if (a.s.max_pages <= kEvictSmall) {
+    if (a.s.max_pages) k_evict_score<<<dim3((a.s.max_pages + 63) / 64, a.s.n_seq), 64, 0, st>>>(a);
+    // enough slices to fill the chip, of 64 pages at least
+    const uint32_t want = (512 + a.s.n_seq - 1) / a.s.n_seq, most = (a.s.max_pages + 63) / 64;
+    const uint32_t slices = want < most ? want : most ? most : 1;
+    k_evict_small<<<dim3(slices, a.s.n_seq), 512, a.s.max_pages * 4, st>>>(a);
+    return hipGetLastError();
+  }
+  const dim3 grid((a.s.max_pages + kEvictTile - 1) / kEvictTile, a.s.n_seq);
+  k_evict_clear<<<(uint32_t)(((size_t)a.s.n_seq * 3 * kBins + 511) / 512), 512, 0, st>>>(a);
+  k_evict_digit<0><<<grid, 512, 0, st>>>(a);
+  k_evict_digit<1><<<grid, 512, 0, st>>>(a);
+  k_evict_digit<2><<<grid, 512, 0, st>>>(a);
+  k_evict_count<<<grid, 512, 0, st>>>(a);
+  k_evict_move<<<grid, 512, 0, st>>>(a);
   return hipGetLastError();
 }
 
