@@ -23,6 +23,10 @@ struct grand_cache {
   uint8_t *ws = nullptr;    // workspace
   size_t ws_bytes = 0;
   CacheErr *err = nullptr;  // device
+  // allocations that buffers of the present call were found in: small
+  // tensors share theirs, and asking for one takes 0.6 us
+  struct { uintptr_t base, end; } seen[4];
+  int n_seen = 0;
   char msg[256] = "";
 };
 
@@ -57,6 +61,7 @@ grand_status check_usable(grand_cache *h) {
   if (!h) return GRAND_E_ARG;
   if (h->poisoned) return GRAND_E_STATE;
   h->msg[0] = 0;
+  h->n_seen = 0;
   return GRAND_OK;
 }
 
@@ -64,6 +69,9 @@ grand_status check_usable(grand_cache *h) {
 grand_status check_mem(grand_cache *h, const char *name, const void *p, uint64_t bytes, size_t align) {
   if (!p) return fail(h, GRAND_E_ARG, "%s is null", name);
   if ((uintptr_t)p % align) return fail(h, GRAND_E_ARG, "%s is not aligned to %zu bytes", name, align);
+  for (int i = 0; i < h->n_seen; i++)
+    if ((uintptr_t)p >= h->seen[i].base && (uintptr_t)p < h->seen[i].end)
+      return bytes <= h->seen[i].end - (uintptr_t)p ? GRAND_OK : fail(h, GRAND_E_ARG, "%s is shorter than the call needs", name);
   hipPointerAttribute_t a{};
   if (hipPointerGetAttributes(&a, p) != hipSuccess || a.type != hipMemoryTypeDevice || a.device != h->p.device) {
     (void)hipGetLastError();
@@ -75,6 +83,7 @@ grand_status check_mem(grand_cache *h, const char *name, const void *p, uint64_t
     (void)hipGetLastError();
     return fail(h, GRAND_E_ARG, "%s has no device allocation", name);
   }
+  if (h->n_seen < 4) h->seen[h->n_seen++] = {(uintptr_t)base, (uintptr_t)base + size};
   const uint64_t room = (uint64_t)((uintptr_t)base + size - (uintptr_t)p);
   if (bytes > room) return fail(h, GRAND_E_ARG, "%s is shorter than the call needs", name);
   return GRAND_OK;

@@ -414,6 +414,7 @@ class Sequences:
         self.max_q, self.max_k = max_q, max_k
         self.c = Seqs(table.shape[0], n_tokens, max_q, max_k, table.data_ptr(), table.stride(0), table.shape[1],
                       None if q_start is None else q_start.data_ptr(), lens.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
 
 class Cache:
@@ -444,9 +445,13 @@ class Cache:
         if rc != OK:
             raise GrandError(rc, "grand_cache_create failed")
         self.h = h
-        self._torch = torch
+        self._torch, self._device = torch, torch.device("cuda", device)
         self._q, self._kv, self._dim, self._page = q_heads, kv_heads, head_dim, page_size
         self._int = (torch.int32, torch.uint32)
+        # argument structs, filled anew by every call
+        self._args = {n: Rows() for n in ("q", "out", "k", "v", "prior")}
+        self._args.update(pages=Pages(), weights=Weights(), weights_out=Weights())
+        self._refs = {n: ctypes.byref(a) for n, a in self._args.items()}
 
     def close(self):
         if getattr(self, "h", None):
@@ -482,34 +487,39 @@ class Cache:
         if x.shape and x.shape[-1] > 1 and x.stride(-1) != 1:
             raise ValueError(f"{name} must be contiguous along its last axis")
 
-    def _rows(self, name, x, heads, tokens=None):
-        if x.dtype != self.torch_dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self._dim or not x.is_cuda:
-            raise ValueError(f"{name} must be (tokens, {heads}, {self._dim}) {self.torch_dtype} on the GPU")
-        if x.stride(2) != 1:
-            raise ValueError(f"{name} must be contiguous along its last axis")
-        if tokens is not None and x.shape[0] != tokens:
-            raise ValueError(f"{name} must have {tokens} tokens")
-        return Rows(x.data_ptr(), x.stride(0), x.stride(1))
+    def _rows(self, name, x, heads, tokens):
+        stride = x.stride()
+        if x.dtype != self.torch_dtype or tuple(x.shape) != (tokens, heads, self._dim) or not x.is_cuda or stride[2] != 1:
+            raise ValueError(f"{name} must be ({tokens}, {heads}, {self._dim}) {self.torch_dtype} on the GPU, contiguous "
+                             "along its last axis")
+        r = self._args[name]
+        r.p, r.token_stride, r.head_stride = x.data_ptr(), stride[0], stride[1]
+        return self._refs[name]
 
     def _pages(self, k, v):
-        shape = (k.shape[0], self._page, self._kv, self._dim)
-        for name, x in (("k_pages", k), ("v_pages", v)):
-            if x.dtype != self.torch_dtype or tuple(x.shape) != shape or not x.is_cuda or x.stride(3) != 1:
-                raise ValueError(f"{name} must be (pages, {self._page}, {self._kv}, {self._dim}) {self.torch_dtype} on the "
-                                 "GPU, contiguous along its last axis")
-        if k.stride() != v.stride():
+        shape, stride = k.shape, k.stride()
+        if (k.dtype != self.torch_dtype or v.dtype != self.torch_dtype or tuple(shape[1:]) != (self._page, self._kv, self._dim)
+                or v.shape != shape or not k.is_cuda or not v.is_cuda or stride[3] != 1):
+            raise ValueError(f"k_pages and v_pages must be (pages, {self._page}, {self._kv}, {self._dim}) {self.torch_dtype} on the "
+                             "GPU, contiguous along their last axis")
+        if v.stride() != stride:
             raise ValueError("k_pages and v_pages must have the same strides")
-        return Pages(k.data_ptr(), v.data_ptr(), k.shape[0], k.stride(0), k.stride(1), k.stride(2))
+        g = self._args["pages"]
+        g.k, g.v, g.n_pages = k.data_ptr(), v.data_ptr(), shape[0]
+        g.page_stride, g.slot_stride, g.head_stride = stride[:3]
+        return self._refs["pages"]
 
     def _weights(self, name, w, n_seq, least, heads=None):
         if (w.dtype != self._torch.float32 or w.dim() != 3 or w.shape[0] != n_seq or not w.is_cuda or w.shape[2] < least
                 or (heads is not None and w.shape[1] != heads) or (w.shape[2] > 1 and w.stride(2) != 1)):
             raise ValueError(f"{name} must be ({n_seq}, heads, at least {least}) float32 on the GPU, contiguous along its last axis")
-        return Weights(w.data_ptr(), w.stride(0), w.stride(1))
+        a = self._args[name]
+        a.p, a.seq_stride, a.head_stride = w.data_ptr(), w.stride(0), w.stride(1)
+        return self._refs[name]
 
     def _lse(self, lse, tokens):
         if lse is None:
-            return self._torch.empty((tokens, self._q), dtype=self._torch.float32, device=f"cuda:{self.params.device}")
+            return self._torch.empty((tokens, self._q), dtype=self._torch.float32, device=self._device)
         if lse.dtype != self._torch.float32 or tuple(lse.shape) != (tokens, self._q) or not lse.is_contiguous() or not lse.is_cuda:
             raise ValueError(f"lse must be a contiguous ({tokens}, {self._q}) float32 tensor on the GPU")
         return lse
@@ -542,10 +552,8 @@ class Cache:
     def append(self, seqs: Sequences, k, v, k_pages, v_pages):
         """grand_cache_append: the new tokens' keys and values go into their pages."""
         n = self._tokens(seqs, k)
-        rk, rv = self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n)
-        pg = self._pages(k_pages, v_pages)
-        self._check(self.lib.grand_cache_append(self.h, ctypes.byref(seqs.c), ctypes.byref(rk), ctypes.byref(rv),
-                                                ctypes.byref(pg)))
+        self._check(self.lib.grand_cache_append(self.h, seqs.ref, self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n),
+                                                self._pages(k_pages, v_pages)))
 
     def attend(self, seqs: Sequences, q, k_pages, v_pages, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                weights=None, weights_out=None, out=None, lse=None):
@@ -554,10 +562,9 @@ class Cache:
         n = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:
-            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=q.device)
+            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
-        pg = self._pages(k_pages, v_pages)
         wi = wo = None
         if weights is not None:
             weights_out = weights if weights_out is None else weights_out
@@ -566,8 +573,8 @@ class Cache:
         elif weights_out is not None:
             raise ValueError("weights_out needs weights")
         self._check(self.lib.grand_cache_attend(
-            self.h, ctypes.byref(seqs.c), ctypes.byref(rq), ctypes.byref(pg), self._dim ** -0.5 if scale is None else scale,
-            1 if causal else 0, window, ctypes.byref(ro), lse.data_ptr(), wi and ctypes.byref(wi), wo and ctypes.byref(wo)))
+            self.h, seqs.ref, rq, self._pages(k_pages, v_pages), self._dim ** -0.5 if scale is None else scale,
+            1 if causal else 0, window, ro, lse.data_ptr(), wi, wo))
         return (out, lse) if weights is None else (out, lse, weights_out)
 
     def attend_ids(self, q, k_pages, v_pages, ids, scale: Optional[float] = None, prior=None, out=None, lse=None):
@@ -578,19 +585,19 @@ class Cache:
         rq = self._rows("q", q, self._q, n)
         if ids.dim() != 3:
             raise ValueError("ids must be (sequences, q_heads, k)")
-        self._ints("ids", ids, (n, self._q, ids.shape[2]))
+        k, stride = int(ids.shape[2]), ids.stride()
+        self._ints("ids", ids, (n, self._q, k))
         if out is None:
-            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=q.device)
+            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
-        pg = self._pages(k_pages, v_pages)
         rp = zp = None
         if prior is not None:
             rp = self._rows("prior", prior[0], self._q, n)
             zp = self._lse(prior[1], n).data_ptr()
         self._check(self.lib.grand_cache_attend_ids(
-            self.h, n, ctypes.byref(rq), ctypes.byref(pg), ids.data_ptr(), ids.shape[2], ids.stride(0), ids.stride(1),
-            self._dim ** -0.5 if scale is None else scale, rp and ctypes.byref(rp), zp, ctypes.byref(ro), lse.data_ptr()))
+            self.h, n, rq, self._pages(k_pages, v_pages), ids.data_ptr(), k, stride[0], stride[1],
+            self._dim ** -0.5 if scale is None else scale, rp, zp, ro, lse.data_ptr()))
         return out, lse
 
     def evict(self, seqs: Sequences, weights, budget, sinks: int = 0, recent: int = 0):
@@ -600,12 +607,11 @@ class Cache:
         wi = self._weights("weights", weights, n, seqs.max_k)
         self._ints("budget", budget, (n,))
         heads, cap = weights.shape[1], weights.shape[2]
-        empty, i32, dev = self._torch.empty, self._torch.int32, weights.device
+        empty, i32, dev = self._torch.empty, self._torch.int32, self._device
         table, freed = empty((n, pages), dtype=i32, device=dev), empty((n, pages), dtype=i32, device=dev)
         lens, n_freed = empty(n, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
         new = empty((n, heads, cap), dtype=self._torch.float32, device=dev)
-        wo = Weights(new.data_ptr(), new.stride(0), new.stride(1))
-        self._check(self.lib.grand_cache_evict(
-            self.h, ctypes.byref(seqs.c), heads, cap, ctypes.byref(wi), budget.data_ptr(), sinks, recent, table.data_ptr(),
-            ctypes.byref(wo), lens.data_ptr(), freed.data_ptr(), n_freed.data_ptr()))
+        wo = self._weights("weights_out", new, n, cap)
+        self._check(self.lib.grand_cache_evict(self.h, seqs.ref, heads, cap, wi, budget.data_ptr(), sinks, recent, table.data_ptr(),
+                                               wo, lens.data_ptr(), freed.data_ptr(), n_freed.data_ptr()))
         return table, new, lens, freed, n_freed
