@@ -111,7 +111,7 @@ constexpr uint32_t kEvictSmall = 16384, kEvictTile = 2048;  // pages
 
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.
-constexpr uint32_t kFewRows = 32, kRowsTileRows = 128;
+constexpr uint32_t kFewRows = 32, kManyRows = 128;
 constexpr uint32_t kKeysStep = 128;  // keys that a workgroup of few rows takes at once (four waves of 32)
 
 hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);

@@ -365,7 +365,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   const uint64_t rows = (uint64_t)a.s.max_q * a.group;
   if (rows >= 1u << 30) return fail(h, GRAND_E_CAPACITY, "max_q is too large");
   const bool few = rows <= kFewRows;
-  const uint32_t tile_rows = rows <= 16 ? 16 : few ? 32 : kRowsTileRows;
+  const uint32_t tile_rows = rows <= 16 ? 16 : few ? 32 : kManyRows;
   a.row_tiles = (uint32_t)((rows + tile_rows - 1) / tile_rows);
   // Keys a row tile sees at most, and the splits of them.  A split costs a
   // workgroup's start and end (about 6 us, behind the others' loads) and a

@@ -21,6 +21,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again
 
 struct Bf16 {
   static constexpr uint32_t kExp = 0x7F807F80u, kExpLow = 0x00800080u, kInf = 0x7F80u;  // exponent bits of two elements, their lowest bits, of one
@@ -69,64 +70,84 @@ template <int DP> constexpr int k_row() { return DP * 2 + 16; }
 template <int DP> constexpr int v_row() { return DP * 2 + ((DP * 2) % 128 == 0 ? 64 : 0); }
 template <int DP, int KT> constexpr int tile_bytes() { return KT * (k_row<DP>() + v_row<DP>()); }
 
-// Global loads of one tile of KT keys by NT threads into registers, and
-// their way into LDS.  Keys at or past `end` repeat key end - 1.
-template <int DP, int KT, int NT>
+// Global loads of one tile of KT keys by 256 threads into registers, and
+// their way into LDS.  LPR lanes load a row, 16 bytes each (some idle where
+// rows are not a power of two long); a lane loads a piece of N consecutive
+// keys, which mostly lie in one page.  A key at or past `end` reads some slot
+// of the pool and is hidden.
+template <int DP, int KT>
 struct TileLoad {
-  static constexpr int NCH = DP / 8;
-  static constexpr int N = KT * NCH / NT;
+  static constexpr int LPR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, N = KT * LPR / 256;
   v4u k[N], v[N];
   uint32_t page[N];
+  int piece, krow;
+  bool in, one_page;
 
-  static __device__ __forceinline__ int row(int i, int t) { return (i * NT + t) / NCH; }
-  static __device__ __forceinline__ int col(int i, int t) { return (i * NT + t) % NCH; }
-
-  __device__ __forceinline__ void pages(const AttendArgs &a, const uint32_t *table, uint32_t key0, uint32_t end, int t) {
+  __device__ __forceinline__ TileLoad(const AttendArgs &a, int t) {
+    piece = t % LPR;
+    krow = t / LPR * N;
+    in = piece * 8 < (int)a.dim;
+    one_page = (1u << a.pg.shift) >= N;
+  }
+  __device__ __forceinline__ void pages(const AttendArgs &a, const uint32_t *table, uint32_t key0) {
+    if (one_page) {
+      page[0] = table[min((key0 + krow) >> a.pg.shift, a.s.max_pages - 1)];
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; i++) page[i] = table[min(key0 + row(i, t), end - 1) >> a.pg.shift];
+      for (int i = 0; i < N; i++) page[i] = table[min((key0 + krow + i) >> a.pg.shift, a.s.max_pages - 1)];
+    }
   }
   // seq: where a page outside the pool is reported
-  __device__ __forceinline__ void rows(const AttendArgs &a, uint32_t key0, uint32_t end, uint32_t kvh, int t, uint32_t seq) {
-    const uint32_t mask = (1u << a.pg.shift) - 1;
+  __device__ __forceinline__ void rows(const AttendArgs &a, uint32_t key0, uint32_t end, uint32_t kvh, uint32_t seq) {
+    const uint32_t mask = (1u << a.pg.shift) - 1, in_head = kvh * a.pg.head + (in ? piece * 16 : 0);
     bool bad = false;
+    if (one_page) {
+      bad = page[0] >= a.pg.n_pages && key0 + krow < end;
+      const uint64_t off = (uint64_t)min(page[0], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow) & mask) * a.pg.slot + in_head);
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      const uint32_t slot = min(key0 + row(i, t), end - 1) & mask;
-      bad |= page[i] >= a.pg.n_pages;
-      const uint32_t p = min(page[i], a.pg.n_pages - 1);
-      const bool in = col(i, t) * 8 < (int)a.dim;
-      const uint64_t off = (uint64_t)p * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head + (in ? col(i, t) * 16 : 0));
-      k[i] = *(const v4u *)(a.pg.k + off);
-      v[i] = *(const v4u *)(a.pg.v + off);
+      for (int i = 0; i < N; i++) {
+        k[i] = *(const v4u *)(a.pg.k + off + i * a.pg.slot);
+        v[i] = *(const v4u *)(a.pg.v + off + i * a.pg.slot);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end;
+        const uint64_t off = (uint64_t)min(page[i], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow + i) & mask) * a.pg.slot + in_head);
+        k[i] = *(const v4u *)(a.pg.k + off);
+        v[i] = *(const v4u *)(a.pg.v + off);
+      }
     }
     if (bad) cache_err(a.err, kCachePage, seq);
   }
-  // Infinite and NaN values become 0; returns whether there were any.
+  // Infinite and NaN values become 0; returns whether there were any among
+  // the keys before end.
   template <class E>
-  __device__ __forceinline__ bool clear_non_finite() {
+  __device__ __forceinline__ bool clear_non_finite(uint32_t key0, uint32_t end) {
     uint32_t any = 0;
 #pragma unroll
     for (int i = 0; i < N; i++)
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         const uint32_t odd = ((v[i][j] & E::kExp) + E::kExpLow) & 0x80008000u;  // the sign bits of such elements
-        any |= odd;
+        if (key0 + krow + i < end) any |= odd;
         v[i][j] &= ~((odd >> 15) * 0xFFFFu);
       }
     return any != 0;
   }
   // Elements past dim: the keys' are zeros, as the queries' are, the values'
   // are whatever was loaded, as their sums are not written.
-  __device__ __forceinline__ void store(const AttendArgs &a, uint8_t *lk, uint8_t *lv, int t) {
-    if (a.dim != DP) {
+  __device__ __forceinline__ void store(const AttendArgs &a, uint8_t *lk, uint8_t *lv) {
+    if (a.dim != DP && !in) {
 #pragma unroll
-      for (int i = 0; i < N; i++)
-        if (col(i, t) * 8 >= (int)a.dim) k[i] = v4u{0, 0, 0, 0};
+      for (int i = 0; i < N; i++) k[i] = v4u{0, 0, 0, 0};
     }
+    if (LPR * 8 == DP || piece * 8 < DP) {
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      *(v4u *)(lk + row(i, t) * k_row<DP>() + col(i, t) * 16) = k[i];
-      *(v4u *)(lv + row(i, t) * v_row<DP>() + col(i, t) * 16) = v[i];
+      for (int i = 0; i < N; i++) {
+        *(v4u *)(lk + (krow + i) * k_row<DP>() + piece * 16) = k[i];
+        *(v4u *)(lv + (krow + i) * v_row<DP>() + piece * 16) = v[i];
+      }
     }
   }
 };
@@ -163,39 +184,37 @@ __device__ __forceinline__ v8s v_operand(const uint8_t *lv, int t, int d, int la
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Adds the infinite and NaN values of the keys [begin, end) (blocks of 32,
-// `step` apart) to the rows that see them.  Tiles with a key that is hidden
+// Adds the infinite and NaN values of the keys [begin, end) to the rows that see them.  Tiles with a key that is hidden
 // from some row hold zeros in their place, as a hidden key's weight of zero
 // would make NaN of them; in other tiles the product took them already, and
 // adding them again changes nothing.
 template <class E, int DP>
 __device__ __forceinline__ void add_non_finite(const AttendArgs &a, const uint32_t *table, uint32_t kvh, uint32_t begin, uint32_t end,
-                                               uint32_t step, int first, int last, int half, v16f *o) {
-  for (uint32_t k0 = begin; k0 < end; k0 += step)
-    for (uint32_t key = k0; key < min(k0 + 32, end); key++) {
-      const uint32_t page = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & ((1u << a.pg.shift) - 1);
-      const uint8_t *p = a.pg.v + (uint64_t)page * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head);
-      const bool see = (int)key >= first && (int)key <= last;
+                                               int first, int last, int half, v16f *o) {
+  for (uint32_t key = begin; key < end; key++) {
+    const uint32_t page = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & ((1u << a.pg.shift) - 1);
+    const uint8_t *p = a.pg.v + (uint64_t)page * a.pg.page + (slot * a.pg.slot + kvh * a.pg.head);
+    const bool see = (int)key >= first && (int)key <= last;
 #pragma unroll
-      for (int d = 0; d < DP / 32; d++)
+    for (int d = 0; d < DP / 32; d++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-          const int at = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
-          if (at < (int)a.dim) {
-            const uint16_t u = *(const uint16_t *)(p + at * 2);
-            if (see && (u & E::kInf) == E::kInf) o[d][i] += (float)__builtin_bit_cast(typename E::T, u);
-          }
+      for (int i = 0; i < 16; i++) {
+        const int at = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        if (at < (int)a.dim) {
+          const uint16_t u = *(const uint16_t *)(p + at * 2);
+          if (see && (u & E::kInf) == E::kInf) o[d][i] += (float)__builtin_bit_cast(typename E::T, u);
         }
-    }
+      }
+  }
 }
 
 // One tile of KT keys: scores, running softmax, weighted values.
 // pos: the row's position; keys past it (causal) or `window` before it are
 // hidden, as are keys at or past end.  masked: some key of the tile is
-// hidden from some row of the wave.  emit(kb, s): sees the scores of block kb.
-template <class E, int DP, int KT, class F>
+// hidden from some row of the wave.
+template <class E, int DP, int KT>
 __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk, const uint8_t *lv, float c, uint32_t key0,
-                                          bool masked, int first, int last, int lane, F emit) {
+                                          bool masked, int first, int last, int lane) {
   const int col = lane & 31, half = lane >> 5;
   v16f s[KT / 32];
 #pragma unroll
@@ -220,7 +239,6 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
         if (key < first || key > last) s[kb][i] = neg_inf();
       }
   }
-  emit(s);
   float mx = s[0][0];
 #pragma unroll
   for (int kb = 0; kb < KT / 32; kb++)
@@ -320,9 +338,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
   const uint32_t kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const uint32_t rt = rest % a.row_tiles, split = rest / a.row_tiles, b = blockIdx.y;
   const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t rows = ch.ql * a.group, r0 = rt * kRowsTileRows;
+  const uint32_t rows = ch.ql * a.group, r0 = rt * kManyRows;
   if (r0 >= rows) return;
-  const uint32_t r1 = min(rows, r0 + kRowsTileRows) - 1;
+  const uint32_t r1 = min(rows, r0 + kManyRows) - 1;
   uint32_t lo, hi;
   key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
   const bool direct = a.n_splits == 1;
@@ -345,26 +363,26 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
     const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
     // the whole workgroup's rows see every key from all0 to all1
     const int all0 = a.window ? ch.p0 + (int)(r1 / a.group) - (int)a.window + 1 : 0;
-    const int all1 = a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
+    const int all1 = min(a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1, (int)end - 1);
     bool odd = false;
-    TileLoad<DP, KT, 256> ld;
-    ld.pages(a, table, begin, end, t);
-    ld.rows(a, begin, end, kvh, t, b);
-    ld.pages(a, table, min(begin + KT, end - 1), end, t);
+    TileLoad<DP, KT> ld(a, t);
+    ld.pages(a, table, begin);
+    ld.rows(a, begin, end, kvh, b);
+    ld.pages(a, table, begin + KT);
     int buf = 0;
     for (uint32_t key0 = begin; key0 < end; key0 += KT, buf ^= 1) {
       uint8_t *lk = smem + buf * tile_bytes<DP, KT>(), *lv = lk + KT * k_row<DP>();
-      if ((int)key0 < all0 || (int)key0 + KT - 1 > all1) odd |= ld.template clear_non_finite<E>();
-      ld.store(a, lk, lv, t);
+      if ((int)key0 < all0 || (int)key0 + KT - 1 > all1) odd |= ld.template clear_non_finite<E>(key0, end);
+      ld.store(a, lk, lv);
       if (key0 + KT < end) {
-        ld.rows(a, key0 + KT, end, kvh, t, b);
-        ld.pages(a, table, min(key0 + 2 * KT, end - 1), end, t);
+        ld.rows(a, key0 + KT, end, kvh, b);
+        ld.pages(a, table, key0 + 2 * KT);
       }
       lds_barrier();
-      const bool masked = (int)key0 < wfirst || (int)key0 + KT - 1 > wlast || key0 + KT > end;
-      tile_step<E, DP, KT>(st, lk, lv, a.c, key0, masked, first, min(last, (int)end - 1), lane, [](v16f *) {});
+      const bool masked = (int)key0 < wfirst || (int)key0 + KT - 1 > min(wlast, (int)end - 1);
+      tile_step<E, DP, KT>(st, lk, lv, a.c, key0, masked, first, min(last, (int)end - 1), lane);
     }
-    if (__syncthreads_or(odd)) add_non_finite<E, DP>(a, table, kvh, begin, end, 32, first, last, half, st.o);
+    if (__syncthreads_or(odd)) add_non_finite<E, DP>(a, table, kvh, begin, end, first, last, half, st.o);
   }
   st.l = halves(st.l, fadd2);
   if (valid) write_row<E, DP>(a, st.o, st.m, st.l, ch.r0 + tok, head, split, direct, half);
@@ -808,54 +826,83 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
     if (key0 + j * 256 < ch.kl) wout[key0 + j * 256] = sum[j];
 }
 
-// Weights from scores computed again: a wave keeps 32 keys, the rows of the
-// chunk pass by in tiles of 32.
+// Weights from scores computed again: a wave keeps 64 keys in registers, the
+// rows of the chunk pass by in tiles of 32.  Every score costs an
+// exponential, a product and a sum, 24 cycles of a SIMD for 64 scores, against
+// 16 for its matrix product: the vector unit bounds it.
 template <class E, int DP>
-__global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendArgs a) {
   constexpr int kStride = DP * 2 + 16;
   __shared__ __align__(16) uint8_t lq[2][32 * kStride];
   __shared__ float lz[2][32];
-  __shared__ float total[128];
+  __shared__ float total[kAgainKeys];
   const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, kt = blockIdx.x / a.kv_heads;
   const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t key0 = kt * 128;
+  const uint32_t key0 = kt * kAgainKeys;
   if (key0 >= ch.kl) return;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, half = lane >> 5, col = lane & 31;
-  typename E::V k[DP / 16];
-  {
-    const uint32_t key = min(key0 + wave * 32 + col, ch.kl - 1);
-    uint32_t p = a.s.table[(int64_t)b * a.s.table_stride + (key >> a.pg.shift)];
-    p = min(p, a.pg.n_pages - 1);
-    const uint8_t *at = a.pg.k + (uint64_t)p * a.pg.page + ((key & ((1u << a.pg.shift) - 1)) * a.pg.slot + kvh * a.pg.head);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, col = lane & 31;
+  const int wkey = (int)key0 + wave * 64;  // the wave's first key
+  typename E::V k[2][DP / 16];
+#pragma unroll
+  for (int kb = 0; kb < 2; kb++) {
+    const uint32_t key = min((uint32_t)wkey + kb * 32 + col, ch.kl - 1);
+    const uint32_t page = min(a.s.table[(int64_t)b * a.s.table_stride + (key >> a.pg.shift)], a.pg.n_pages - 1);
+    const uint8_t *at = a.pg.k + (uint64_t)page * a.pg.page + ((key & ((1u << a.pg.shift) - 1)) * a.pg.slot + kvh * a.pg.head);
 #pragma unroll
     for (int s = 0; s < DP / 16; s++) {
       v4u x{0, 0, 0, 0};
       if ((2 * s + half) * 8 < (int)a.dim) x = *(const v4u *)(at + (2 * s + half) * 16);
-      k[s] = __builtin_bit_cast(typename E::V, x);
+      k[kb][s] = __builtin_bit_cast(typename E::V, x);
     }
   }
   // rows that see a key of this tile
-  const int klast = (int)min(key0 + 128, ch.kl) - 1;
+  const int klast = (int)min(key0 + kAgainKeys, ch.kl) - 1;
   const int t_lo = a.causal ? max(0, (int)key0 - ch.p0) : 0;
   const int t_hi = a.window ? min((int)ch.ql, klast + (int)a.window - ch.p0) : (int)ch.ql;
   const uint32_t r_lo = (uint32_t)min(t_lo, (int)ch.ql) * a.group, r_hi = (uint32_t)max(t_hi, 0) * a.group;
-  v16f acc{};
+  v16f acc[2] = {v16f{}, v16f{}};
   constexpr int NCH = DP / 8, N = (32 * NCH + 255) / 256;
+  // places of the rows that this thread loads: 32 rows on is some tokens and
+  // some heads on, a pointer's step and another where the heads wrap around
+  const uint32_t step_t = 32 / a.group, step_g = 32 % a.group;
+  const int64_t q_step = step_t * a.q.token + step_g * a.q.head, q_wrap = a.q.token - (int64_t)a.group * a.q.head;
+  const int64_t z_step = (int64_t)step_t * a.q_heads + step_g, z_wrap = (int64_t)a.q_heads - a.group;
+  const uint8_t *qp[N];
+  const float *zp;
+  uint32_t gr[N + 1];
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    const uint32_t r = r_lo + (i * 256 + t) / NCH;
+    gr[i] = r % a.group;
+    qp[i] = a.q.p + (int64_t)(ch.r0 + r / a.group) * a.q.token + (int64_t)(kvh * a.group + gr[i]) * a.q.head + (i * 256 + t) % NCH * 16;
+  }
+  gr[N] = (r_lo + (t & 31)) % a.group;
+  zp = a.lse2 + (size_t)(ch.r0 + (r_lo + (t & 31)) / a.group) * a.q_heads + kvh * a.group + gr[N];
+  uint32_t first_tok = r_lo / a.group, first_g = 0;
   v4u next[N];
   float nextz = 0.f;
   auto load = [&](uint32_t r0) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const int x = i * 256 + t;
-      const uint32_t r = r0 + x / NCH;
       next[i] = v4u{0, 0, 0, 0};
-      if (x < 32 * NCH && r < r_hi && (x % NCH) * 8 < (int)a.dim)
-        next[i] = *(const v4u *)(a.q.p + (int64_t)(ch.r0 + r / a.group) * a.q.token + (int64_t)(kvh * a.group + r % a.group) * a.q.head + (x % NCH) * 16);
+      if (x < 32 * NCH && r0 + x / NCH < r_hi && (x % NCH) * 8 < (int)a.dim) next[i] = *(const v4u *)qp[i];
+      qp[i] += q_step;
+      gr[i] += step_g;
+      if (gr[i] >= a.group) {
+        gr[i] -= a.group;
+        qp[i] += q_wrap;
+      }
     }
     if (t < 32) {
-      const uint32_t r = r0 + t;
-      const float z = r < r_hi ? a.lse2[(size_t)(ch.r0 + r / a.group) * a.q_heads + kvh * a.group + r % a.group] : neg_inf();
-      nextz = z == neg_inf() ? __builtin_inff() : z;
+      const float z = r0 + t < r_hi ? *zp : neg_inf();
+      nextz = z == neg_inf() ? __builtin_inff() : z;  // a row that sees nothing gives nothing
+      zp += z_step;
+      gr[N] += step_g;
+      if (gr[N] >= a.group) {
+        gr[N] -= a.group;
+        zp += z_wrap;
+      }
     }
   };
   if (r_lo < r_hi) load(r_lo);
@@ -869,37 +916,51 @@ __global__ __launch_bounds__(256, 2) void k_weights_again(AttendArgs a) {
     if (t < 32) lz[buf][t] = nextz;
     if (r0 + 32 < r_hi) load(r0 + 32);
     lds_barrier();
-    v16f s{};
+    v16f s[2] = {v16f{}, v16f{}};
 #pragma unroll
     for (int x = 0; x < DP / 16; x++) {
       const v4u q = *(const v4u *)(lq[buf] + col * kStride + (2 * x + half) * 16);
-      s = E::mul(k[x], __builtin_bit_cast(typename E::V, q), s);
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) s[kb] = E::mul(k[kb][x], __builtin_bit_cast(typename E::V, q), s[kb]);
     }
     const float z = lz[buf][col];
-    const int p_lo = ch.p0 + (int)(r0 / a.group), p_hi = ch.p0 + (int)(min(r0 + 31, r_hi - 1) / a.group);
-    const bool masked = (a.causal && (int)(key0 + wave * 32 + 31) > p_lo) ||
-                        (a.window && (int)(key0 + wave * 32) <= p_hi - (int)a.window);
-    if (masked) {
+    // (the last row's token is at most 31 / group + 1 on)
+    const int p_lo = ch.p0 + (int)first_tok, p_hi = p_lo + (int)(31 / a.group) + 1;
+    if ((a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window)) {
+      int k0 = wkey;
+      asm volatile("" : "+s"(k0));
       const int pos = ch.p0 + (int)(min(r0 + col, r_hi - 1) / a.group);
 #pragma unroll
-      for (int i = 0; i < 16; i++) {
-        const int key = (int)key0 + wave * 32 + (i / 4) * 8 + half * 4 + i % 4;
-        if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[i] = neg_inf();
-      }
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+          const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
+          if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[kb][i] = neg_inf();
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 16; i++) acc[i] += ex2(__builtin_fmaf(s[i], a.c, -z));
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) acc[kb][i] += ex2(__builtin_fmaf(s[kb][i], a.c, -z));
+    first_tok += step_t;
+    first_g += step_g;
+    if (first_g >= a.group) {
+      first_g -= a.group;
+      first_tok++;
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
-    float x = acc[i];
+  for (int kb = 0; kb < 2; kb++)
 #pragma unroll
-    for (int j = 16; j; j >>= 1) x += __shfl_xor(x, j, 64);
-    if (col == 0) total[wave * 32 + (i / 4) * 8 + half * 4 + i % 4] = x;
-  }
+    for (int i = 0; i < 16; i++) {
+      float x = acc[kb][i];
+#pragma unroll
+      for (int j = 16; j; j >>= 1) x += __shfl_xor(x, j, 64);
+      if (col == 0) total[wave * 64 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4] = x;
+    }
   __syncthreads();
   const uint32_t key = key0 + t;
-  if (t < 128 && key < ch.kl)
+  if (key < ch.kl)
     a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] =
         a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key] + total[t];
 }
@@ -922,7 +983,7 @@ hipError_t few_dim(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
 
 template <class E>
 hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) {
-  if (tile_rows == kRowsTileRows) {
+  if (tile_rows == kManyRows) {
     if (a.dim <= 64) return rows_dim<E, 64>(a, st);
     if (a.dim <= 128) return rows_dim<E, 128>(a, st);
     return rows_dim<E, 256>(a, st);
@@ -936,7 +997,7 @@ hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) 
 
 template <class E>
 hipError_t weights_type(const AttendArgs &a, hipStream_t st) {
-  const dim3 grid((a.s.max_k + 127) / 128 * a.kv_heads, a.s.n_seq);
+  const dim3 grid((a.s.max_k + kAgainKeys - 1) / kAgainKeys * a.kv_heads, a.s.n_seq);
   if (a.dim <= 64) k_weights_again<E, 64><<<grid, 256, 0, st>>>(a);
   else if (a.dim <= 128) k_weights_again<E, 128><<<grid, 256, 0, st>>>(a);
   else k_weights_again<E, 256><<<grid, 256, 0, st>>>(a);
