@@ -827,14 +827,14 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
 }
 
 // Weights from scores computed again: a wave keeps 64 keys in registers, the
-// rows of the chunk pass by in tiles of 32.  Every score costs an
+// rows of the chunk pass by in tiles of 64 (32 where rows are long).  Every score costs an
 // exponential, a product and a sum, 24 cycles of a SIMD for 64 scores, against
 // 16 for its matrix product: the vector unit bounds it.
 template <class E, int DP>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendArgs a) {
-  constexpr int kStride = DP * 2 + 16;
-  __shared__ __align__(16) uint8_t lq[2][32 * kStride];
-  __shared__ float lz[2][32];
+  constexpr int kStride = DP * 2 + 16, RT = DP > 128 ? 32 : 64;  // rows of a tile
+  __shared__ __align__(16) uint8_t lq[2][RT * kStride];
+  __shared__ float lz[2][RT];
   __shared__ float total[kAgainKeys];
   const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, kt = blockIdx.x / a.kv_heads;
   const Chunk ch = chunk_of(a.s, b, a.err);
@@ -861,10 +861,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
   const int t_hi = a.window ? min((int)ch.ql, klast + (int)a.window - ch.p0) : (int)ch.ql;
   const uint32_t r_lo = (uint32_t)min(t_lo, (int)ch.ql) * a.group, r_hi = (uint32_t)max(t_hi, 0) * a.group;
   v16f acc[2] = {v16f{}, v16f{}};
-  constexpr int NCH = DP / 8, N = (32 * NCH + 255) / 256;
-  // places of the rows that this thread loads: 32 rows on is some tokens and
+  constexpr int NCH = DP / 8, N = (RT * NCH + 255) / 256;
+  // places of the rows that this thread loads: RT rows on is some tokens and
   // some heads on, a pointer's step and another where the heads wrap around
-  const uint32_t step_t = 32 / a.group, step_g = 32 % a.group;
+  const uint32_t step_t = RT / a.group, step_g = RT % a.group;
   const int64_t q_step = step_t * a.q.token + step_g * a.q.head, q_wrap = a.q.token - (int64_t)a.group * a.q.head;
   const int64_t z_step = (int64_t)step_t * a.q_heads + step_g, z_wrap = (int64_t)a.q_heads - a.group;
   const uint8_t *qp[N];
@@ -876,8 +876,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
     gr[i] = r % a.group;
     qp[i] = a.q.p + (int64_t)(ch.r0 + r / a.group) * a.q.token + (int64_t)(kvh * a.group + gr[i]) * a.q.head + (i * 256 + t) % NCH * 16;
   }
-  gr[N] = (r_lo + (t & 31)) % a.group;
-  zp = a.lse2 + (size_t)(ch.r0 + (r_lo + (t & 31)) / a.group) * a.q_heads + kvh * a.group + gr[N];
+  gr[N] = (r_lo + t % RT) % a.group;
+  zp = a.lse2 + (size_t)(ch.r0 + (r_lo + t % RT) / a.group) * a.q_heads + kvh * a.group + gr[N];
   uint32_t first_tok = r_lo / a.group, first_g = 0;
   v4u next[N];
   float nextz = 0.f;
@@ -886,7 +886,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
     for (int i = 0; i < N; i++) {
       const int x = i * 256 + t;
       next[i] = v4u{0, 0, 0, 0};
-      if (x < 32 * NCH && r0 + x / NCH < r_hi && (x % NCH) * 8 < (int)a.dim) next[i] = *(const v4u *)qp[i];
+      if (x < RT * NCH && r0 + x / NCH < r_hi && (x % NCH) * 8 < (int)a.dim) next[i] = *(const v4u *)qp[i];
       qp[i] += q_step;
       gr[i] += step_g;
       if (gr[i] >= a.group) {
@@ -894,7 +894,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
         qp[i] += q_wrap;
       }
     }
-    if (t < 32) {
+    if (t < RT) {
       const float z = r0 + t < r_hi ? *zp : neg_inf();
       nextz = z == neg_inf() ? __builtin_inff() : z;  // a row that sees nothing gives nothing
       zp += z_step;
@@ -907,41 +907,45 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
   };
   if (r_lo < r_hi) load(r_lo);
   int buf = 0;
-  for (uint32_t r0 = r_lo; r0 < r_hi; r0 += 32, buf ^= 1) {
+  for (uint32_t r0 = r_lo; r0 < r_hi; r0 += RT, buf ^= 1) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const int x = i * 256 + t;
-      if (x < 32 * NCH) *(v4u *)(lq[buf] + (x / NCH) * kStride + (x % NCH) * 16) = next[i];
+      if (x < RT * NCH) *(v4u *)(lq[buf] + (x / NCH) * kStride + (x % NCH) * 16) = next[i];
     }
-    if (t < 32) lz[buf][t] = nextz;
-    if (r0 + 32 < r_hi) load(r0 + 32);
+    if (t < RT) lz[buf][t] = nextz;
+    if (r0 + RT < r_hi) load(r0 + RT);
     lds_barrier();
-    v16f s[2] = {v16f{}, v16f{}};
+    // (the last row's token is at most (RT - 1) / group + 1 on)
+    const int p_lo = ch.p0 + (int)first_tok, p_hi = p_lo + (int)((RT - 1) / a.group) + 1;
+    const bool masked = (a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window);
 #pragma unroll
-    for (int x = 0; x < DP / 16; x++) {
-      const v4u q = *(const v4u *)(lq[buf] + col * kStride + (2 * x + half) * 16);
+    for (int rb = 0; rb < RT / 32; rb++) {
+      v16f s[2] = {v16f{}, v16f{}};
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) s[kb] = E::mul(k[kb][x], __builtin_bit_cast(typename E::V, q), s[kb]);
-    }
-    const float z = lz[buf][col];
-    // (the last row's token is at most 31 / group + 1 on)
-    const int p_lo = ch.p0 + (int)first_tok, p_hi = p_lo + (int)(31 / a.group) + 1;
-    if ((a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window)) {
-      int k0 = wkey;
-      asm volatile("" : "+s"(k0));
-      const int pos = ch.p0 + (int)(min(r0 + col, r_hi - 1) / a.group);
+      for (int x = 0; x < DP / 16; x++) {
+        const v4u q = *(const v4u *)(lq[buf] + (rb * 32 + col) * kStride + (2 * x + half) * 16);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) s[kb] = E::mul(k[kb][x], __builtin_bit_cast(typename E::V, q), s[kb]);
+      }
+      const float z = lz[buf][rb * 32 + col];
+      if (masked) {
+        int k0 = wkey;
+        asm volatile("" : "+s"(k0));
+        const int pos = ch.p0 + (int)(min(r0 + rb * 32 + col, r_hi - 1) / a.group);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
+            if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[kb][i] = neg_inf();
+          }
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; kb++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-          const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
-          if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[kb][i] = neg_inf();
-        }
+        for (int i = 0; i < 16; i++) acc[kb][i] += ex2(__builtin_fmaf(s[kb][i], a.c, -z));
     }
-#pragma unroll
-    for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-      for (int i = 0; i < 16; i++) acc[kb][i] += ex2(__builtin_fmaf(s[kb][i], a.c, -z));
     first_tok += step_t;
     first_g += step_g;
     if (first_g >= a.group) {
