@@ -32,6 +32,9 @@ struct grand_cache {
 
 namespace {
 
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr uint64_t kMostGroups = 1u << 24;  // workgroups of 256 in a grid's x: fewer than 2^32 threads
+
 grand_status fail(grand_cache *h, grand_status code, const char *fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -339,7 +342,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   const grand_cache_params &p = h->p;
   AttendArgs a{};
   TRY(check_seqs(h, s, true, &a.s));
-  if (!(scale > 0.f) || !isfinite(scale)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
+  if (!(scale > 0.f) || !isfinite(scale * kLog2e)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
   if (!weights_in != !weights_out) return fail(h, GRAND_E_ARG, "weights_in and weights_out come together");
   TRY(check_pages(h, pages, &a.pg));
   if (s->n_tokens) {
@@ -357,7 +360,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   a.group = p.q_heads / p.kv_heads;
   a.dim = p.head_dim;
   a.scale = scale;
-  a.c = scale * 1.44269504088896341f;
+  a.c = scale * kLog2e;
   a.causal = causal != 0;
   a.window = window < s->max_k ? window : 0;  // a window as long as the cache hides nothing
   a.err = h->err;
@@ -381,7 +384,9 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   if (span <= split) a.n_splits = 1, split = span + 31;
   a.split = (uint32_t)split;
-  if (base / s->n_seq * a.n_splits >= 1ull << 31) return fail(h, GRAND_E_CAPACITY, "max_q is too large");
+  const uint64_t groups = few ? (base * a.n_splits + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;
+  if (groups >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "too many sequences, heads and new tokens for one call");
+  if (weights_out && ((uint64_t)s->max_k / 256 + 1) * p.kv_heads >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "max_k is too large");
 
   Parts w;
   const uint64_t all_rows = (uint64_t)s->n_tokens * p.q_heads;
@@ -422,9 +427,9 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
   HCHK(h, hipSetDevice(h->p.device));
   const grand_cache_params &p = h->p;
   IdsArgs a{};
-  if (!(scale > 0.f) || !isfinite(scale)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
+  if (!(scale > 0.f) || !isfinite(scale * kLog2e)) return fail(h, GRAND_E_ARG, "scale must be positive and finite");
   if (!prior != !prior_lse) return fail(h, GRAND_E_ARG, "prior and prior_lse come together");
-  if ((uint64_t)n_seq * p.q_heads >= 1u << 31) return fail(h, GRAND_E_CAPACITY, "too many rows");
+  if ((uint64_t)n_seq * p.q_heads >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "too many sequences and heads for one call");
   if (k >= 1u << 30) return fail(h, GRAND_E_CAPACITY, "lists are too long");
   TRY(check_pages(h, pages, &a.pg));
   TRY(check_rows(h, "q", q, n_seq, p.q_heads, false, &a.q));
@@ -447,7 +452,7 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
   a.q_heads = p.q_heads;
   a.group = p.q_heads / p.kv_heads;
   a.dim = p.head_dim;
-  a.c = scale * 1.44269504088896341f;
+  a.c = scale * kLog2e;
   a.err = h->err;
   HCHK(h, launch_attend_ids(p.dtype == GRAND_F16, a, h->stream));
   return GRAND_OK;

@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256, DP > 192 ? 1 : DP > 128 || NB > 1 ? 2 : 3) voi
       for (int i = 0; i < N; i++) page[i] = table[min((key0 + krow + i) >> a.pg.shift, a.s.max_pages - 1)];
     }
   };
-  pages(split * a.split + wave * 32);
+  if (a.s.max_pages) pages(split * a.split + wave * 32);
   const Chunk ch = chunk_of(a.s, b, a.err);
   const uint32_t rows = ch.ql * a.group, r0 = rt * ROWS;
   if (r0 >= rows) return;

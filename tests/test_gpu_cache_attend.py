@@ -417,6 +417,26 @@ def test_without_starts_every_sequence_has_one_new_token():
     assert (c["k_pages"][int(c["table"][1, 89 // 16]), 89 % 16] == 1).all()
 
 
+def test_tables_of_no_pages():
+    """Nothing cached at all: a table without columns."""
+    import torch
+
+    from paper_2608_21163_amd import Cache
+
+    cache = Cache("bf16", 4, 2, 64, 16, stream=torch.cuda.current_stream().cuda_stream)
+    pages = torch.zeros(1, 16, 2, 64, dtype=torch.bfloat16, device="cuda")
+    for n in (1, 20):
+        s = cache.sequences(torch.zeros(2, 0, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"),
+                            torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda"), max_q=n)
+        q = torch.ones(2 * n, 4, 64, dtype=torch.bfloat16, device="cuda")
+        out, lse = cache.attend(s, q, pages, pages)
+        cache.check()
+        assert not out.any() and torch.isneginf(lse).all()
+    table, w, lens, freed, n_freed = cache.evict(s, torch.ones(2, 2, 3, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert table.shape == (2, 0) and not w.any() and not lens.any() and not n_freed.any()
+    cache.check()
+
+
 def test_what_kernels_report():
     """Values in device memory that are out of range: nothing outside the
     buffers is touched, other sequences keep their results, check() says
