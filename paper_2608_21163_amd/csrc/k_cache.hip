@@ -214,6 +214,7 @@ __device__ __forceinline__ float page_score(const EvictArgs &a, uint32_t b, uint
   float s = 0.f;
   if (!a.quads) {
     for (uint32_t h = 0; h < a.heads; h++)
+#pragma unroll 4
       for (uint32_t i = 0; i < a.page; i++) s += w[(int64_t)h * a.win.head + i];
     return s;
   }
@@ -432,6 +433,7 @@ __global__ __launch_bounds__(512) void k_evict_small(EvictArgs a) {
 // counted by all workgroups together, one launch a digit, then each tile's
 // keys above and at the threshold, then the tiles move.
 constexpr uint32_t kBins = 2048;
+constexpr int kPerThread = kEvictTile / 512;  // pages of a tile a thread takes
 __device__ __forceinline__ uint32_t *evict_hist(const EvictArgs &a, uint32_t b, int pass) { return a.hist + ((size_t)b * 3 + pass) * kBins; }
 
 __global__ __launch_bounds__(512) void k_evict_clear(EvictArgs a) {
@@ -458,17 +460,27 @@ __global__ __launch_bounds__(512) void k_evict_digit(EvictArgs a) {
   if (p0 >= e.n) return;
   const uint32_t p1 = min(e.n, p0 + kEvictTile);
   uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
+  // all of a thread's pages are loaded before the first is counted
+  uint32_t k[kPerThread];
+#pragma unroll
+  for (int i = 0; i < kPerThread; i++) {
+    const uint32_t p = p0 + i * 512 + t;
+    k[i] = p >= p1 ? 0 : PASS == 0 ? page_key(a, e, b, p) : keys[p];
+  }
   uint32_t thr = 0, left = 0;
   if (e.keep > 0 && e.keep < e.n) evict_prefix(a, e, b, PASS, tmp, thr, left);
   for (int i = t; i < (int)kBins; i += 512) hist[i] = 0;
   __syncthreads();
-  for (uint32_t p = p0 + t; p < p1; p += 512) {
-    uint32_t k;
-    if (PASS == 0) keys[p] = k = page_key(a, e, b, p);
-    else k = keys[p];
-    if (PASS == 0) atomicAdd(&hist[k >> 21], 1u);
-    if (PASS == 1 && (k >> 21) == (thr >> 21)) atomicAdd(&hist[(k >> 10) & 2047], 1u);
-    if (PASS == 2 && (k >> 10) == (thr >> 10)) atomicAdd(&hist[k & 1023], 1u);
+#pragma unroll
+  for (int i = 0; i < kPerThread; i++) {
+    const uint32_t p = p0 + i * 512 + t;
+    if (p >= p1) break;
+    if (PASS == 0) {
+      keys[p] = k[i];
+      atomicAdd(&hist[k[i] >> 21], 1u);
+    }
+    if (PASS == 1 && (k[i] >> 21) == (thr >> 21)) atomicAdd(&hist[(k[i] >> 10) & 2047], 1u);
+    if (PASS == 2 && (k[i] >> 10) == (thr >> 10)) atomicAdd(&hist[k[i] & 1023], 1u);
   }
   __syncthreads();
   uint32_t *sum = evict_hist(a, b, PASS);
@@ -495,12 +507,16 @@ __global__ __launch_bounds__(512) void k_evict_count(EvictArgs a) {
   const EvictSeq e = evict_seq(a, b);
   if (p0 >= e.n) return;
   uint32_t thr, left, above = 0, equal = 0;
+  const uint32_t *keys = a.keys + (size_t)b * a.s.max_pages, p1 = min(e.n, p0 + kEvictTile);
+  uint32_t k[kPerThread];
+#pragma unroll
+  for (int i = 0; i < kPerThread; i++) k[i] = p0 + i * 512 + t < p1 ? keys[p0 + i * 512 + t] : 0;
   evict_threshold(a, e, b, tmp, thr, left);
-  const uint32_t *keys = a.keys + (size_t)b * a.s.max_pages;
-  for (uint32_t p = p0 + t; p < min(e.n, p0 + kEvictTile); p += 512) {
-    const uint32_t k = keys[p];
-    above += e.keep >= e.n || k > thr;
-    equal += e.keep < e.n && k == thr;
+#pragma unroll
+  for (int i = 0; i < kPerThread; i++) {
+    const bool live = p0 + i * 512 + t < p1;
+    above += live && (e.keep >= e.n || k[i] > thr);
+    equal += live && e.keep < e.n && k[i] == thr;
   }
 #pragma unroll
   for (int j = 32; j; j >>= 1) {
