@@ -63,6 +63,8 @@ struct AttendArgs {
   float *lse2;               // log2-unit lse of every row, for the weights
   float *scores;             // log2-unit scores by (sequence, key/value head, row, key); null: recomputed
   uint32_t score_rows, score_keys;
+  uint32_t row_splits;       // where they are recomputed: splits of the rows, whose sums are
+  float *row_sums;           // by (split, sequence, key/value head, key) if there is more than one
   CacheErr *err;
 };
 
@@ -107,11 +109,15 @@ struct EvictArgs {
   CacheErr *err;
 };
 
-constexpr uint32_t kEvictSmall = 16384, kEvictTile = 2048;  // pages
+// Pages: tables up to kEvictSmall are handled by one launch whose workgroups
+// all find the threshold (8 x 8,000 pages of 16: 36 us, by tiles 44; 8 x 16,000:
+// 62 and 51).
+constexpr uint32_t kEvictSmall = 8192, kEvictTile = 2048;
 
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.
 constexpr uint32_t kFewRows = 32, kManyRows = 128;
+constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again
 constexpr uint32_t kKeysStep = 128;  // keys that a workgroup of few rows takes at once (four waves of 32)
 
 hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);

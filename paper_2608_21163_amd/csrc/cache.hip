@@ -388,29 +388,41 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   a.split = (uint32_t)split;
   const uint64_t groups = few ? (base * a.n_splits + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;
   if (groups >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "too many sequences, heads and new tokens for one call");
-  if (weights_out && ((uint64_t)s->max_k / 256 + 1) * p.kv_heads >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "max_k is too large");
+  if (weights_out && ((uint64_t)s->max_k / kAgainKeys + 1) * p.kv_heads * 32 >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "max_k is too large");
 
   Parts w;
   const uint64_t all_rows = (uint64_t)s->n_tokens * p.q_heads;
   const int w_part = a.n_splits > 1 ? w.add(all_rows * a.n_splits * p.head_dim * 4) : -1;
   const int w_ml = a.n_splits > 1 ? w.add(all_rows * a.n_splits * 8) : -1;
-  int w_lse = -1, w_scores = -1;
+  int w_lse = -1, w_scores = -1, w_sums = -1;
+  a.row_splits = 1;
   if (weights_out) {
     w_lse = w.add(all_rows * 4);
     // scores of a few rows are kept (4 bytes a row and key, against half of
     // the cache to compute them again)
     const uint64_t keys = ((uint64_t)s->max_k + 31) / 32 * 32;
     const uint64_t bytes = (uint64_t)s->n_seq * p.kv_heads * rows * keys * 4;
-    if (few && bytes <= 256ull << 20) {
+    if (few && bytes <= 1ull << 30) {
       w_scores = w.add(bytes);
       a.score_rows = (uint32_t)rows;
-      a.score_keys = (uint32_t)keys;
+    } else {
+      // workgroups of 256 keys that have rows, and splits of the rows (256 at
+      // least) where they are too few: six chunks of up to 614 tokens, 8 query
+      // heads of 256 elements to one key/value head, over up to 1,904 cached
+      // ones take 386 us with 48 workgroups, 172 with splits
+      const uint64_t seen = a.window ? std::min<uint64_t>(s->max_k, (uint64_t)a.window + a.s.max_q) : s->max_k;
+      const uint64_t tiles = (seen / kAgainKeys + 1) * p.kv_heads * s->n_seq;
+      const uint64_t most = std::min<uint64_t>((rows + 255) / 256, std::max<uint64_t>(1, (256ull << 20) / ((uint64_t)s->n_seq * p.kv_heads * keys * 4 + 1)));
+      a.row_splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((1024 + tiles - 1) / tiles, std::min<uint64_t>(most, 32)));
+      if (a.row_splits > 1) w_sums = w.add((uint64_t)a.row_splits * s->n_seq * p.kv_heads * keys * 4);
     }
+    a.score_keys = (uint32_t)keys;
   }
   TRY(ensure_ws(h, w.total));
   if (w_part >= 0) a.part = (float *)(h->ws + w.at[w_part]);
   if (w_ml >= 0) a.part_ml = (float2 *)(h->ws + w.at[w_ml]);
   if (w_lse >= 0) a.lse2 = (float *)(h->ws + w.at[w_lse]);
+  if (w_sums >= 0) a.row_sums = (float *)(h->ws + w.at[w_sums]);
   if (w_scores >= 0) a.scores = (float *)(h->ws + w.at[w_scores]);
   const bool f16 = p.dtype == GRAND_F16;
   if (s->n_tokens && s->max_q) {

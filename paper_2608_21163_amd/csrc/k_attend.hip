@@ -21,7 +21,6 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again
 
 struct Bf16 {
   static constexpr uint32_t kExp = 0x7F807F80u, kExpLow = 0x00800080u, kInf = 0x7F80u;  // exponent bits of two elements, their lowest bits, of one
@@ -331,7 +330,15 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, const v16f *o, fl
   }
 }
 
-// Four waves of 32 rows each over shared tiles of KT keys.
+// Four waves of 32 rows each over shared tiles of KT keys: chunks.  A wave
+// reads each tile's keys and values once from LDS for 32 rows, 32 cycles of
+// the matrix unit a 1 KB operand.  2,048 tokens of 32 heads over 32,768 cached
+// ones take 1.17 to 1.25 ms, 0.85 to 0.91 PFLOP/s, where a large library product
+// reaches 1.23; the matrix unit is busy 45% of the time, the vector unit
+// (exponentials, sums, maxima, rounding) 55%, LDS 36%.  Tiles of 32 keys are 5%
+// slower, 256 rows a workgroup 5%, the next block's scores beside this one's
+// softmax 3%, operands read ahead of the products 0 to 3%; splits read the
+// keys again through L2.
 template <class E, int DP, int KT>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArgs a) {
   extern __shared__ uint8_t smem[];
@@ -394,8 +401,11 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
 // many loads are in flight and that each takes whole cache lines, past which
 // the caches are told not to keep them (an instruction reads whole rows of 2
 // to 8 keys).  A tile's keys, then its values pass through the same LDS.
+// 64 tokens over 1 to 8,192 cached ones, 1.15 GB: 200 us, 5.8 TB/s, where a
+// plain read of as much takes 174 (past the caches) to 195.  With loads that
+// the caches keep 227 us, with 64 bytes of 16 rows an instruction 258.
 template <class E, int DP, int NB>
-__global__ __launch_bounds__(256, DP > 192 ? 1 : DP > 128 || NB > 1 ? 2 : 3) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 128 || NB > 1 ? 2 : 3) void k_attend_few(AttendArgs a) {
   typedef typename E::V V;
   constexpr int NS = DP / 32, KROW = k_row<DP>(), VROW = v_row<DP>(), ROWS = 16 * NB;
   constexpr int LPR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;  // lanes that load a row, 16 bytes each (96, 192: some idle)
@@ -577,7 +587,9 @@ __global__ __launch_bounds__(256, DP > 192 ? 1 : DP > 128 || NB > 1 ? 2 : 3) voi
         float mx = fmaxf(fmaxf(fmaxf(sc[nb][0][0], sc[nb][0][1]), fmaxf(sc[nb][0][2], sc[nb][0][3])),
                          fmaxf(fmaxf(sc[nb][1][0], sc[nb][1][1]), fmaxf(sc[nb][1][2], sc[nb][1][3])));
         mx = halves(rows16(mx, fmax2), fmax2) * a.c;
-        if (__ballot(mx > m[nb] + 8.f)) {  // as in tile_step
+        // the true maximum (unlike tile_step's): the largest probability is
+        // then 1, which 16 bits hold, and the loads hide the rescaling
+        if (__ballot(mx > m[nb])) {
           const float mn = fmaxf(m[nb], mx), scale = m[nb] == neg_inf() ? 0.f : ex2(m[nb] - mn);
 #pragma unroll
           for (int d = 0; d < DP / 16; d++) o[nb][d] *= scale;
@@ -675,6 +687,10 @@ __global__ __launch_bounds__(256, DP > 192 ? 1 : DP > 128 || NB > 1 ? 2 : 3) voi
 }
 
 // Joins the splits of one row: LQ lanes read one split's sums, 16 bytes each.
+// A launch of its own (4 to 8 us): with the last workgroup of a row's splits
+// joining them, the fences that carry sums between XCDs made a token over
+// 1,000 cached ones 14 us instead of 7 + 4, a step of 64 sequences 820 instead
+// of 210.
 template <class E, int LQ>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile_rows) {
   constexpr int G = 256 / LQ, CHUNK = 1024;
@@ -747,7 +763,8 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile
   }
 }
 
-// The same for few splits and many rows: LQ lanes a row.
+// The same for few splits and many rows: LQ lanes a row.  Seven chunks of up
+// to 300 tokens in three splits: 4.4 us, a workgroup a row 26.
 constexpr uint32_t kShortSplits = 8;
 template <class E, int LQ>
 __global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_t tile_rows) {
@@ -793,6 +810,8 @@ __global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_
 }
 
 // Weights from stored scores: a thread sums four keys' weights over the rows.
+// 50 MB of scores and weights in 11 us; computing the scores again would read
+// half of the cache.
 __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
   __shared__ float z[kFewRows];
   const uint32_t b = blockIdx.z, kvh = blockIdx.y, key0 = blockIdx.x * 1024 + threadIdx.x;
@@ -828,18 +847,47 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
 
 // Weights from scores computed again: a wave keeps 64 keys in registers, the
 // rows of the chunk pass by in tiles of 64 (32 where rows are long).  Every score costs an
-// exponential, a product and a sum, 24 cycles of a SIMD for 64 scores, against
-// 16 for its matrix product: the vector unit bounds it.
+// exponential, a product and a sum, about 23 cycles of a SIMD for 64 scores,
+// against 16 for its matrix product: the vector unit bounds it.  2,048 tokens
+// of 32 heads over 32,768: 0.65 to 0.70 ms (32 keys a wave 0.80, tiles of 32
+// rows 0.70 to 0.75).
+// Where that gives too few workgroups the rows are split, and their sums are
+// added by another launch.
+struct AgainRows {
+  uint32_t lo, hi, per, n;  // rows that see a key of the tile, rows of a split, splits that have any
+};
+__device__ __forceinline__ AgainRows again_rows(const AttendArgs &a, const Chunk &ch, uint32_t key0) {
+  AgainRows r;
+  const int klast = (int)min(key0 + kAgainKeys, ch.kl) - 1;
+  const int t_lo = a.causal ? max(0, (int)key0 - ch.p0) : 0;
+  const int t_hi = a.window ? min((int)ch.ql, klast + (int)a.window - ch.p0) : (int)ch.ql;
+  r.lo = (uint32_t)min(t_lo, (int)ch.ql) * a.group;
+  r.hi = max((uint32_t)max(t_hi, 0) * a.group, r.lo);
+  const uint32_t tiles = (r.hi - r.lo + 63) / 64;
+  r.per = max((tiles + a.row_splits - 1) / a.row_splits, 1u) * 64;
+  r.n = (r.hi - r.lo + r.per - 1) / r.per;
+  return r;
+}
+
 template <class E, int DP>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendArgs a) {
   constexpr int kStride = DP * 2 + 16, RT = DP > 128 ? 32 : 64;  // rows of a tile
   __shared__ __align__(16) uint8_t lq[2][RT * kStride];
   __shared__ float lz[2][RT];
   __shared__ float total[kAgainKeys];
-  const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, kt = blockIdx.x / a.kv_heads;
+  const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
+  const uint32_t part = rest % a.row_splits, kt = rest / a.row_splits;
   const Chunk ch = chunk_of(a.s, b, a.err);
   const uint32_t key0 = kt * kAgainKeys;
   if (key0 >= ch.kl) return;
+  const AgainRows range = again_rows(a, ch, key0);
+  const float *win = a.win.p + (int64_t)b * a.win.seq + (int64_t)kvh * a.win.head;
+  float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head;
+  if (part >= range.n) {
+    if (a.row_splits == 1 && key0 + threadIdx.x < ch.kl) wout[key0 + threadIdx.x] = win[key0 + threadIdx.x];
+    return;
+  }
+  const uint32_t r_lo = range.lo + part * range.per, r_hi = min(range.hi, r_lo + range.per);
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, col = lane & 31;
   const int wkey = (int)key0 + wave * 64;  // the wave's first key
   typename E::V k[2][DP / 16];
@@ -855,11 +903,6 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
       k[kb][s] = __builtin_bit_cast(typename E::V, x);
     }
   }
-  // rows that see a key of this tile
-  const int klast = (int)min(key0 + kAgainKeys, ch.kl) - 1;
-  const int t_lo = a.causal ? max(0, (int)key0 - ch.p0) : 0;
-  const int t_hi = a.window ? min((int)ch.ql, klast + (int)a.window - ch.p0) : (int)ch.ql;
-  const uint32_t r_lo = (uint32_t)min(t_lo, (int)ch.ql) * a.group, r_hi = (uint32_t)max(t_hi, 0) * a.group;
   v16f acc[2] = {v16f{}, v16f{}};
   constexpr int NCH = DP / 8, N = (RT * NCH + 255) / 256;
   // places of the rows that this thread loads: RT rows on is some tokens and
@@ -878,7 +921,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
   }
   gr[N] = (r_lo + t % RT) % a.group;
   zp = a.lse2 + (size_t)(ch.r0 + (r_lo + t % RT) / a.group) * a.q_heads + kvh * a.group + gr[N];
-  uint32_t first_tok = r_lo / a.group, first_g = 0;
+  uint32_t first_tok = r_lo / a.group, first_g = r_lo % a.group;
   v4u next[N];
   float nextz = 0.f;
   auto load = [&](uint32_t r0) {
@@ -905,7 +948,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
       }
     }
   };
-  if (r_lo < r_hi) load(r_lo);
+  load(r_lo);
   int buf = 0;
   for (uint32_t r0 = r_lo; r0 < r_hi; r0 += RT, buf ^= 1) {
 #pragma unroll
@@ -964,9 +1007,21 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
     }
   __syncthreads();
   const uint32_t key = key0 + t;
-  if (key < ch.kl)
-    a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] =
-        a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key] + total[t];
+  if (key < ch.kl) {
+    if (a.row_splits == 1) wout[key] = win[key] + total[t];
+    else a.row_sums[(((size_t)part * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key] = total[t];
+  }
+}
+
+__global__ __launch_bounds__(256) void k_weights_add(AttendArgs a) {
+  const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, key0 = blockIdx.x / a.kv_heads * kAgainKeys, key = key0 + threadIdx.x;
+  const Chunk ch = chunk_of(a.s, b, a.err);
+  if (key >= ch.kl) return;
+  const AgainRows range = again_rows(a, ch, key0);
+  float sum = a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key];
+#pragma unroll 4
+  for (uint32_t i = 0; i < range.n; i++) sum += a.row_sums[(((size_t)i * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key];
+  a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] = sum;
 }
 
 template <class E, int DP>
@@ -989,7 +1044,9 @@ template <class E>
 hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) {
   if (tile_rows == kManyRows) {
     if (a.dim <= 64) return rows_dim<E, 64>(a, st);
+    if (a.dim <= 96) return rows_dim<E, 96>(a, st);
     if (a.dim <= 128) return rows_dim<E, 128>(a, st);
+    if (a.dim <= 192) return rows_dim<E, 192>(a, st);
     return rows_dim<E, 256>(a, st);
   }
   if (a.dim <= 64) return few_dim<E, 64>(a, tile_rows, st);
@@ -1001,10 +1058,14 @@ hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) 
 
 template <class E>
 hipError_t weights_type(const AttendArgs &a, hipStream_t st) {
-  const dim3 grid((a.s.max_k + kAgainKeys - 1) / kAgainKeys * a.kv_heads, a.s.n_seq);
+  const uint32_t tiles = (a.s.max_k + kAgainKeys - 1) / kAgainKeys;
+  const dim3 grid(tiles * a.row_splits * a.kv_heads, a.s.n_seq);
   if (a.dim <= 64) k_weights_again<E, 64><<<grid, 256, 0, st>>>(a);
+  else if (a.dim <= 96) k_weights_again<E, 96><<<grid, 256, 0, st>>>(a);
   else if (a.dim <= 128) k_weights_again<E, 128><<<grid, 256, 0, st>>>(a);
+  else if (a.dim <= 192) k_weights_again<E, 192><<<grid, 256, 0, st>>>(a);
   else k_weights_again<E, 256><<<grid, 256, 0, st>>>(a);
+  if (a.row_splits > 1) k_weights_add<<<dim3(tiles * a.kv_heads, a.s.n_seq), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -127,6 +127,19 @@ def test_lengths(name, dtype, hq, hk, dim):
     compare(c, *run(c))
 
 
+@pytest.mark.parametrize("dim", [72, 96, 136, 192])
+def test_chunks_of_rows_that_are_no_power_of_two(dim):
+    import torch
+
+    say(f"[cache chunks] {dim}")
+    c = make("bf16", 6, 2, dim, 4, qs=(50, 7, 1), ks=(333, 130, 64), seed=dim)
+    before = torch.rand(3, 2, 340, device="cuda")
+    after = before.clone()
+    out, lse, w = run(c, weights=after)
+    compare(c, out, lse, weights=after, before=before)
+    compare(c, *run(c, window=40), window=40)
+
+
 def test_bounds_may_be_loose():
     """max_q and max_k are upper bounds: far larger ones change nothing but
     the order of sums."""
