@@ -332,7 +332,8 @@ const char *grand_last_error(const grand_index *h);
  *  - Every pointer to data is device memory of the cache's GPU, and the
  *    calls only enqueue work on the cache's stream: they return before it
  *    is done, and the memory must live until then.  A handle keeps
- *    workspaces, no results; calls on one handle are ordered by its stream.
+ *    workspaces, no results; calls on one handle are ordered by its stream,
+ *    and one host thread at a time makes them.
  *  - A workspace grows when a call needs more than any call before it (the
  *    growth waits for the device).  A stream capture does not allow that:
  *    run the call once before the capture, else it fails with
@@ -419,7 +420,7 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
  * out = 0 and lse = -inf.  Hidden tokens have no influence, whatever their
  * keys and values hold.  Query head h uses key/value head
  * h / (q_heads / kv_heads).  scale > 0.
- * lse: n_tokens x q_heads, or null.
+ * lse: n_tokens x q_heads, or null.  Rows of no sequence are not written.
  * weights_in, weights_out: null, or rows of at least max_k entries: entry j
  * of weights_out becomes entry j of weights_in plus the softmax weight that
  * the new tokens give to cached token j, summed over them and the query

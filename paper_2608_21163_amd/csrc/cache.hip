@@ -375,13 +375,15 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   // row of sums to join; too few leave the last workgroups alone.  64 single
   // tokens over 1 to 8,192 cached ones, 8 heads: 1,024 workgroups 222 us,
   // 4,096 212 us, 8,192 216 us; two over 131,072: 211, 215, 222 us.  Chunks
-  // of 512 over up to 8,192: 512 workgroups 187 us, 1,024 162 us.  A split of
-  // few rows has 512 keys at least: one launch for a token over 300 instead
-  // of two, 10.9 us against 13.4, and the same for 1,000 to 4,000.
+  // of 512 over up to 8,192: 512 workgroups 187 us, 1,024 162 us.  Few rows:
+  // up to 512 keys are one launch (a token over 300: 10.9 us, in two splits
+  // 13.4); splits have 256 keys while that leaves CUs idle (a token over
+  // 1,000 waited for: 28.5 us, with 512 30.4), else 512 (16,000: 35.9, 35.0).
   const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) + 31 : s->max_k);
   const uint64_t base = std::max<uint64_t>(1, (uint64_t)p.kv_heads * a.row_tiles * s->n_seq);
   const uint64_t want = ((few ? 4096 : 1024) + base - 1) / base;
-  uint64_t split = std::max<uint64_t>(few ? 512 : 256, (span + want - 1) / want);
+  const uint64_t least = !few || (span > 512 && base * ((span + 255) / 256) <= 256) ? 256 : 512;
+  uint64_t split = std::max<uint64_t>(least, (span + want - 1) / want);
   split = (split + kKeysStep - 1) / kKeysStep * kKeysStep;
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   if (span <= split) a.n_splits = 1, split = span + 31;
