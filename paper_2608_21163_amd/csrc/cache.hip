@@ -379,7 +379,9 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   // up to 512 keys are one launch (a token over 300: 10.9 us, in two splits
   // 13.4); splits have 256 keys while that leaves CUs idle (a token over
   // 1,000 waited for: 28.5 us, with 512 30.4), else 512 (16,000: 35.9, 35.0).
-  const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) + 31 : s->max_k);
+  // (a tile's rows see up to its last token, or up to the chunk's if not causal)
+  const uint64_t tokens = causal ? std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) : a.s.max_q;
+  const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + tokens + 31 : s->max_k);
   const uint64_t base = std::max<uint64_t>(1, (uint64_t)p.kv_heads * a.row_tiles * s->n_seq);
   const uint64_t want = ((few ? 4096 : 1024) + base - 1) / base;
   const uint64_t least = !few || (span > 512 && base * ((span + 255) / 256) <= 256) ? 256 : 512;

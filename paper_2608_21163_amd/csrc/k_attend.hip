@@ -838,7 +838,10 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         const uint32_t key = key0 + j * 256;
-        if (key >= lo && key < hi) sum[j] += ex2(sc[(size_t)r * a.score_keys + key] - z[r]);
+        if (key >= lo && key < hi) {
+          const float x = sc[(size_t)r * a.score_keys + key];
+          sum[j] += x == neg_inf() ? 0.f : ex2(x - z[r]);  // hidden: nothing, though the row's sum be NaN
+        }
       }
   }
   float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head;
@@ -983,13 +986,15 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
-            if ((a.causal && key > pos) || (a.window && key <= pos - (int)a.window)) s[kb][i] = neg_inf();
+            const bool hidden = (a.causal && key > pos) || (a.window && key <= pos - (int)a.window);
+            acc[kb][i] += hidden ? 0.f : ex2(__builtin_fmaf(s[kb][i], a.c, -z));
           }
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) acc[kb][i] += ex2(__builtin_fmaf(s[kb][i], a.c, -z));
       }
-#pragma unroll
-      for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) acc[kb][i] += ex2(__builtin_fmaf(s[kb][i], a.c, -z));
     }
     first_tok += step_t;
     first_g += step_g;

@@ -447,6 +447,7 @@ class Cache:
         self.h = h
         self._torch, self._device = torch, torch.device("cuda", device)
         self._q, self._kv, self._dim, self._page = q_heads, kv_heads, head_dim, page_size
+        self._page_shape = (page_size, kv_heads, head_dim)
         self._int = (torch.int32, torch.uint32)
         # argument structs, filled anew by every call
         self._args = {n: Rows() for n in ("q", "out", "k", "v", "prior")}
@@ -482,14 +483,14 @@ class Cache:
 
     # ------------------------------------------------------------ arguments
     def _ints(self, name, x, shape):
-        if x.dtype not in self._int or not x.is_cuda or tuple(x.shape) != shape:
+        if x.dtype not in self._int or not x.is_cuda or x.shape != shape:
             raise ValueError(f"{name} must be a 32-bit integer tensor {shape} on the GPU")
         if x.shape and x.shape[-1] > 1 and x.stride(-1) != 1:
             raise ValueError(f"{name} must be contiguous along its last axis")
 
     def _rows(self, name, x, heads, tokens):
         stride = x.stride()
-        if x.dtype != self.torch_dtype or tuple(x.shape) != (tokens, heads, self._dim) or not x.is_cuda or stride[2] != 1:
+        if x.dtype != self.torch_dtype or x.shape != (tokens, heads, self._dim) or not x.is_cuda or stride[2] != 1:
             raise ValueError(f"{name} must be ({tokens}, {heads}, {self._dim}) {self.torch_dtype} on the GPU, contiguous "
                              "along its last axis")
         r = self._args[name]
@@ -498,8 +499,8 @@ class Cache:
 
     def _pages(self, k, v):
         shape, stride = k.shape, k.stride()
-        if (k.dtype != self.torch_dtype or v.dtype != self.torch_dtype or tuple(shape[1:]) != (self._page, self._kv, self._dim)
-                or v.shape != shape or not k.is_cuda or not v.is_cuda or stride[3] != 1):
+        if (k.dtype != self.torch_dtype or v.dtype != self.torch_dtype or shape[1:] != self._page_shape or v.shape != shape
+                or not k.is_cuda or not v.is_cuda or stride[3] != 1):
             raise ValueError(f"k_pages and v_pages must be (pages, {self._page}, {self._kv}, {self._dim}) {self.torch_dtype} on the "
                              "GPU, contiguous along their last axis")
         if v.stride() != stride:
@@ -517,10 +518,15 @@ class Cache:
         a.p, a.seq_stride, a.head_stride = w.data_ptr(), w.stride(0), w.stride(1)
         return self._refs[name]
 
+    def _out(self, q, tokens):
+        if q.is_contiguous():
+            return self._torch.empty_like(q)
+        return self._torch.empty((tokens, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
+
     def _lse(self, lse, tokens):
         if lse is None:
             return self._torch.empty((tokens, self._q), dtype=self._torch.float32, device=self._device)
-        if lse.dtype != self._torch.float32 or tuple(lse.shape) != (tokens, self._q) or not lse.is_contiguous() or not lse.is_cuda:
+        if lse.dtype != self._torch.float32 or lse.shape != (tokens, self._q) or not lse.is_contiguous() or not lse.is_cuda:
             raise ValueError(f"lse must be a contiguous ({tokens}, {self._q}) float32 tensor on the GPU")
         return lse
 
@@ -562,7 +568,7 @@ class Cache:
         n = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:
-            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
+            out = self._out(q, n)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
         wi = wo = None
@@ -588,7 +594,7 @@ class Cache:
         k, stride = int(ids.shape[2]), ids.stride()
         self._ints("ids", ids, (n, self._q, k))
         if out is None:
-            out = self._torch.empty((n, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
+            out = self._out(q, n)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
         rp = zp = None

@@ -252,6 +252,43 @@ def test_weights(qs, ks, window, dtype, hq, hk, dim):
     assert w2 is other and torch.equal(other, after) and torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("qs,ks", [((5, 0, 2), (40, 0, 700)), ((60, 3), (300, 0)), ((300,), (900,))])
+def test_weights_without_causality(window, qs, ks):
+    import torch
+
+    say(f"[cache weights] not causal, window {window} {qs} {ks}")
+    c = make("f16", 8, 1, 64, qs=qs, ks=ks, seed=window)
+    before = torch.rand(len(ks), 1, max(ks), device="cuda")
+    after = before.clone()
+    out, lse, w = run(c, window=window, causal=False, weights=after)
+    compare(c, out, lse, causal=False, window=window, weights=after, before=before)
+
+
+@pytest.mark.parametrize("qs,ks,window", [((4,), (90,), 0), ((70,), (300,), 0), ((3,), (90,), 8), ((60,), (200,), 16)])
+def test_weights_of_hidden_tokens_that_hold_anything(qs, ks, window):
+    """Keys of tokens that some rows do not see are infinite or NaN: the
+    weights that those rows give are as without them."""
+    import torch
+
+    say(f"[cache weights] hidden {qs} {ks} window {window}")
+    c = make("bf16", 4, 2, 64, qs=qs, ks=ks, seed=8)
+    zero = torch.zeros(1, 2, ks[0], device="cuda")
+    only = dict(c, lens=c["lens"] - 1, ks=(ks[0] - 1,), qs=(qs[0] - 1,), q=c["q"][:qs[0] - 1],
+                q_start=torch.tensor([0, qs[0] - 1], dtype=torch.int32, device="cuda"))
+    want = run(only, window=window, weights=zero.clone())[2]       # the chunk without its last token
+    keys = c["k_pages"].clone()
+    for pos, x in [(ks[0] - 1, math.nan)] + ([(ks[0] - qs[0] - window, math.inf)] if window else []):
+        keys[int(c["table"][0, pos // 16]), pos % 16] = x
+    got = run(dict(only, k_pages=keys), window=window, weights=zero.clone())[2]
+    assert torch.equal(got, want)
+    # the last token's own row is the only one that sees its key
+    whole = run(dict(c, k_pages=keys), window=window, weights=zero.clone())[2]
+    first = max(0, ks[0] - window) if window else 0
+    assert torch.isnan(whole[0, :, first:]).all()
+    assert torch.allclose(whole[0, :, :first], want[0, :, :first], rtol=1e-6, atol=0)
+
+
 def test_weights_sum_to_rows():
     """Every row that sees anything hands out a weight of one."""
     import torch
