@@ -825,9 +825,10 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
     z[threadIdx.x] = x == neg_inf() ? __builtin_inff() : x;  // a row that sees nothing gives nothing
   }
   const float *win = a.win.p + (int64_t)b * a.win.seq + (int64_t)kvh * a.win.head;
-  float sum[4];
+  // the rows' weights first: the running sum takes one rounding a call
+  float sum[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
 #pragma unroll
-  for (int j = 0; j < 4; j++) sum[j] = key0 + j * 256 < ch.kl ? win[key0 + j * 256] : 0.f;
+  for (int j = 0; j < 4; j++) old[j] = key0 + j * 256 < ch.kl ? win[key0 + j * 256] : 0.f;
   __syncthreads();
   if (rows) {
     uint32_t lo, hi;
@@ -847,7 +848,7 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
   float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head;
 #pragma unroll
   for (int j = 0; j < 4; j++)
-    if (key0 + j * 256 < ch.kl) wout[key0 + j * 256] = sum[j];
+    if (key0 + j * 256 < ch.kl) wout[key0 + j * 256] = old[j] + sum[j];
 }
 
 // Weights from scores computed again: a wave keeps 64 keys in registers, the
@@ -1025,10 +1026,11 @@ __global__ __launch_bounds__(256) void k_weights_add(AttendArgs a) {
   const Chunk ch = chunk_of(a.s, b, a.err);
   if (key >= ch.kl) return;
   const AgainRows range = again_rows(a, ch, key0);
-  float sum = a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key];
+  const float old = a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key];
+  float sum = 0.f;
 #pragma unroll 4
   for (uint32_t i = 0; i < range.n; i++) sum += a.row_sums[(((size_t)i * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key];
-  a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] = sum;
+  a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] = old + sum;
 }
 
 template <class E, int DP>
