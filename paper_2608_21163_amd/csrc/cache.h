@@ -50,7 +50,6 @@ struct AttendArgs {
   float *lse;                // n_tokens x q_heads, may be null
   WeightsView win, wout;     // wout.p null: no weights
   uint32_t q_heads, kv_heads, group, dim;
-  float scale;               // of the scores
   float c;                   // scale * log2(e)
   uint32_t window;           // keys a row sees, its own included; 0: all; below 2^31
   int causal;

@@ -359,7 +359,6 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   a.kv_heads = p.kv_heads;
   a.group = p.q_heads / p.kv_heads;
   a.dim = p.head_dim;
-  a.scale = scale;
   a.c = scale * kLog2e;
   a.causal = causal != 0;
   a.window = window < s->max_k ? window : 0;  // a window as long as the cache hides nothing
@@ -375,7 +374,10 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   // row of sums to join; too few leave the last workgroups alone.  64 single
   // tokens over 1 to 8,192 cached ones, 8 heads: 1,024 workgroups 222 us,
   // 4,096 212 us, 8,192 216 us; two over 131,072: 211, 215, 222 us.  Chunks
-  // of 512 over up to 8,192: 512 workgroups 187 us, 1,024 162 us.  Few rows:
+  // of one or two sequences, whose tiles are alike, fill the chip once (512
+  // over 8,192: 512 workgroups 93 us, 1,024 123; two of up to 1,024 over up to
+  // 20,000: 498, 566), of more, whose lengths differ, twice (four of up to 512
+  // over up to 8,192: 188, 163).  Few rows:
   // up to 512 keys are one launch (a token over 300: 10.9 us, in two splits
   // 13.4); splits have 256 keys while that leaves CUs idle (a token over
   // 1,000 waited for: 28.5 us, with 512 30.4), else 512 (16,000: 35.9, 35.0).
@@ -383,7 +385,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   const uint64_t tokens = causal ? std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) : a.s.max_q;
   const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + tokens + 31 : s->max_k);
   const uint64_t base = std::max<uint64_t>(1, (uint64_t)p.kv_heads * a.row_tiles * s->n_seq);
-  const uint64_t want = ((few ? 4096 : 1024) + base - 1) / base;
+  const uint64_t want = ((few ? 4096 : s->n_seq <= 2 ? 512 : 1024) + base - 1) / base;
   const uint64_t least = !few || (span > 512 && base * ((span + 255) / 256) <= 256) ? 256 : 512;
   uint64_t split = std::max<uint64_t>(least, (span + want - 1) / want);
   split = (split + kKeysStep - 1) / kKeysStep * kKeysStep;

@@ -404,8 +404,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
 // the caches are told not to keep them (an instruction reads whole rows of 2
 // to 8 keys).  A tile's keys, then its values pass through the same LDS.
 // 64 tokens over 1 to 8,192 cached ones, 1.15 GB: 200 us, 5.8 TB/s, where a
-// plain read of as much takes 174 (past the caches) to 195.  With loads that
-// the caches keep 227 us, with 64 bytes of 16 rows an instruction 258.
+// plain read of as much takes 174 (past the caches) to 195.  The whole call, 213
+// us, takes 239 with loads that the caches keep, 258 with 64 bytes of 16 rows an
+// instruction.
 template <class E, int DP, int NB>
 __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 128 || NB > 1 ? 2 : 3) void k_attend_few(AttendArgs a) {
   typedef typename E::V V;
