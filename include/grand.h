@@ -438,7 +438,8 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
  * counts each time.
  * prior, prior_lse: null, or another attention's result of the same rows
  * over other tokens (out and lse of grand_cache_attend): the call returns
- * what attention over both would.  lse: n_seq x q_heads, or null. */
+ * what attention over both would.  lse: n_seq x q_heads, or null.
+ * out and lse may be prior (with its strides) and prior_lse themselves. */
 grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_rows *q, const grand_pages *pages,
                                     const uint32_t *ids, uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride,
                                     float scale, const grand_rows *prior, const float *prior_lse,

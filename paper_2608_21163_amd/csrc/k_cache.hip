@@ -129,12 +129,13 @@ __global__ __launch_bounds__(256) void k_attend_ids(IdsArgs a) {
     for (int i = 0; i < 8; i++) sacc[wave][c * 8 + i] = acc[i];
   }
   if (lane == 0) sml[wave] = make_float2(top, l);
+  const size_t row = (size_t)b * a.q_heads + head;
+  // read before the barrier: lse may be the same memory, and one thread writes it
+  const float z0 = a.prior.p ? a.prior_lse[row] * (1.f / kLn2) : neg_inf();
   __syncthreads();
   if (t >= DP) return;
-  float z0 = neg_inf(), o0 = 0.f;
-  const size_t row = (size_t)b * a.q_heads + head;
+  float o0 = 0.f;
   if (a.prior.p) {
-    z0 = a.prior_lse[row] * (1.f / kLn2);
     if (t < (int)a.dim)
       o0 = (float)*(const typename E::T *)(a.prior.p + (int64_t)b * a.prior.token + (int64_t)head * a.prior.head + t * 2);
   }

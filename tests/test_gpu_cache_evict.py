@@ -243,6 +243,26 @@ def test_joined_with_the_window():
     assert ((out.float() - whole.float()).abs() <= 2.0 ** -7 * (1 + whole.float().abs())).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_results_in_place_of_the_earlier_ones(dim):
+    import torch
+
+    from paper_2608_21163_amd import Cache
+
+    g = torch.Generator().manual_seed(dim)
+    b, hq, hk, n, k = 64, 8, 2, 300, 40
+    kp, vp = (torch.randn(n, 1, hk, dim, generator=g).bfloat16().cuda() for _ in range(2))
+    q, o = (torch.randn(b, hq, dim, generator=g).bfloat16().cuda() for _ in range(2))
+    z = torch.randn(b, hq, generator=g).cuda()
+    ids = torch.randint(0, n, (b, hq, k), generator=g).to(torch.int32).cuda()
+    cache = Cache("bf16", hq, hk, dim, 1, stream=torch.cuda.current_stream().cuda_stream)
+    want, zw = cache.attend_ids(q, kp, vp, ids, prior=(o, z))
+    out, lse = o.clone(), z.clone()
+    cache.attend_ids(q, kp, vp, ids, prior=(out, lse), out=out, lse=lse)
+    cache.check()
+    assert torch.equal(out, want) and torch.equal(lse, zw)
+
+
 def test_ids_refusals_and_reports():
     import torch
 
