@@ -418,7 +418,7 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
  * s_j = scale <q, k_j>, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and
  * lse = ln sum_j exp(s_j), by (token, q_head); a row that sees nothing has
  * out = 0 and lse = -inf.  Hidden tokens have no influence, whatever their
- * keys and values hold.  Query head h uses key/value head
+ * keys and values hold, and pages that no row sees may have any id.  Query head h uses key/value head
  * h / (q_heads / kv_heads).  scale > 0.
  * lse: n_tokens x q_heads, or null.  Rows of no sequence are not written.
  * weights_in, weights_out: null, or rows of at least max_k entries: entry j

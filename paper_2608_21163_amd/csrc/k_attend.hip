@@ -96,12 +96,13 @@ struct TileLoad {
       for (int i = 0; i < N; i++) page[i] = table[min((key0 + krow + i) >> a.pg.shift, a.s.max_pages - 1)];
     }
   }
-  // seq: where a page outside the pool is reported
-  __device__ __forceinline__ void rows(const AttendArgs &a, uint32_t key0, uint32_t end, uint32_t kvh, uint32_t seq) {
+  // Of the keys from seen to end, a page outside the pool is reported of seq;
+  // what lies before them is hidden, and a window's user may have freed it.
+  __device__ __forceinline__ void rows(const AttendArgs &a, uint32_t key0, uint32_t seen, uint32_t end, uint32_t kvh, uint32_t seq) {
     const uint32_t mask = (1u << a.pg.shift) - 1, in_head = kvh * a.pg.head + (in ? piece * 16 : 0);
     bool bad = false;
     if (one_page) {
-      bad = page[0] >= a.pg.n_pages && key0 + krow < end;
+      bad = page[0] >= a.pg.n_pages && key0 + krow < end && key0 + krow + N > seen;
       const uint64_t off = (uint64_t)min(page[0], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow) & mask) * a.pg.slot + in_head);
 #pragma unroll
       for (int i = 0; i < N; i++) {
@@ -111,7 +112,7 @@ struct TileLoad {
     } else {
 #pragma unroll
       for (int i = 0; i < N; i++) {
-        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end;
+        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end && key0 + krow + i >= seen;
         const uint64_t off = (uint64_t)min(page[i], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow + i) & mask) * a.pg.slot + in_head);
         k[i] = *(const v4u *)(a.pg.k + off);
         v[i] = *(const v4u *)(a.pg.v + off);
@@ -285,14 +286,16 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
   }
 }
 
-// The keys that rows [first token, last token] of a chunk see.
-__device__ __forceinline__ void key_range(const AttendArgs &a, const Chunk &c, uint32_t t0, uint32_t t1, uint32_t align,
-                                          uint32_t &lo, uint32_t &hi) {
+// The keys that rows [first token, last token] of a chunk see: from the result
+// on, lo is that rounded down to `align`, to before hi.
+__device__ __forceinline__ uint32_t key_range(const AttendArgs &a, const Chunk &c, uint32_t t0, uint32_t t1, uint32_t align,
+                                              uint32_t &lo, uint32_t &hi) {
   int l = 0, h = (int)c.kl;
   if (a.causal) h = min(h, c.p0 + (int)t1 + 1);
   if (a.window) l = max(0, c.p0 + (int)t0 - (int)a.window + 1);
   lo = (uint32_t)l / align * align;
   hi = (uint32_t)max(h, (int)lo);
+  return (uint32_t)l;
 }
 
 template <class E, int DP>
@@ -351,7 +354,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
   if (r0 >= rows) return;
   const uint32_t r1 = min(rows, r0 + kManyRows) - 1;
   uint32_t lo, hi;
-  key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
+  const uint32_t seen = key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
   const bool direct = a.n_splits == 1;
   const uint32_t begin = lo + split * a.split, end = min(hi, begin + a.split);
   if (split && begin >= hi) return;
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
     bool odd = false;
     TileLoad<DP, KT> ld(a, t);
     ld.pages(a, table, begin);
-    ld.rows(a, begin, end, kvh, b);
+    ld.rows(a, begin, seen, end, kvh, b);
     ld.pages(a, table, begin + KT);
     int buf = 0;
     for (uint32_t key0 = begin; key0 < end; key0 += KT, buf ^= 1) {
@@ -384,7 +387,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
       if ((int)key0 < all0 || (int)key0 + KT - 1 > all1) odd |= ld.template clear_non_finite<E>(key0, end);
       ld.store(a, lk, lv);
       if (key0 + KT < end) {
-        ld.rows(a, key0 + KT, end, kvh, b);
+        ld.rows(a, key0 + KT, seen, end, kvh, b);
         ld.pages(a, table, key0 + 2 * KT);
       }
       lds_barrier();
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
   if (r0 >= rows) return;
   const uint32_t r1 = min(rows, r0 + ROWS) - 1;
   uint32_t lo, hi;
-  key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
+  const uint32_t seen = key_range(a, ch, r0 / a.group, r1 / a.group, 32, lo, hi);
   const uint32_t begin = lo + split * a.split, end = min(hi, begin + a.split);
   if (split && begin >= hi) return;
   if (lo) pages(begin + wave * 32);
@@ -490,14 +493,14 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
     bool bad = false;
     const uint32_t mask = (1u << a.pg.shift) - 1, in_head = kvh * a.pg.head + (in ? piece * 16 : 0);
     if (one_page) {
-      bad = page[0] >= a.pg.n_pages && key0 + krow < end;
+      bad = page[0] >= a.pg.n_pages && key0 + krow < end && key0 + krow + N > seen;
       off[0] = (uint64_t)min(page[0], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow) & mask) * a.pg.slot + in_head);
 #pragma unroll
       for (int i = 1; i < N; i++) off[i] = off[i - 1] + a.pg.slot;
     } else {
 #pragma unroll
       for (int i = 0; i < N; i++) {
-        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end;
+        bad |= page[i] >= a.pg.n_pages && key0 + krow + i < end && key0 + krow + i >= seen;
         off[i] = (uint64_t)min(page[i], a.pg.n_pages - 1) * a.pg.page + (((key0 + krow + i) & mask) * a.pg.slot + in_head);
       }
     }

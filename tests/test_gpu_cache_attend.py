@@ -157,6 +157,36 @@ def test_windows(window, causal, qs, ks):
     compare(c, *run(c, window=window, causal=causal), causal=causal, window=window)
 
 
+@pytest.mark.parametrize("page", [1, 8, 16])
+@pytest.mark.parametrize("qs,ks", [((1, 1), (301, 90)), ((3,), (777,)), ((50, 33), (300, 95))])
+def test_pages_behind_the_window_may_be_gone(page, qs, ks):
+    """Every page that the window has left is freed: no results change and
+    nothing is reported; one page further is."""
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ID
+
+    window = 37
+    c = make(qs=qs, ks=ks, page=page)
+    want = run(c, window=window)
+    w = torch.zeros(len(ks), c["hk"], max(ks), device="cuda")
+    cache = cache_for(c)
+    for b, (ql, kl) in enumerate(zip(qs, ks)):
+        c["table"][b, :max(0, kl - ql - window + 1) // page] = -1
+    s = seqs_for(cache, c)
+    q = c["q"].cuda()
+    got = cache.attend(s, q, c["k_pages"], c["v_pages"], window=window)
+    with_weights = cache.attend(s, q, c["k_pages"], c["v_pages"], window=window, weights=w)
+    cache.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(with_weights, want))
+    c["table"][0, max(0, ks[0] - qs[0] - window + 1) // page] = -1
+    cache.attend(s, q, c["k_pages"], c["v_pages"], window=window)
+    with pytest.raises(GrandError) as e:
+        cache.check()
+    assert e.value.code == E_ID
+
+
 def test_not_causal():
     c = make("f16", qs=(5, 60), ks=(5, 200))
     compare(c, *run(c, causal=False), causal=False)
