@@ -337,7 +337,9 @@ const char *grand_last_error(const grand_index *h);
  *  - A workspace grows when a call needs more than any call before it (the
  *    growth waits for the device).  A stream capture does not allow that:
  *    run the call once before the capture, else it fails with
- *    GRAND_E_CAPACITY and nothing is done.
+ *    GRAND_E_CAPACITY and nothing is done.  A workspace that a captured call
+ *    uses is kept until the handle is destroyed, so its graph may be replayed
+ *    after larger calls, ordered among the handle's calls as they are.
  *  - Sizes, strides, alignment and the extent of device buffers are checked
  *    before anything is enqueued.  What lies in device memory (page ids,
  *    lengths, chunk starts, slot ids) is checked by the kernels: nothing is

@@ -22,6 +22,8 @@ struct grand_cache {
   uint32_t shift = 0;       // log2 of the page size
   uint8_t *ws = nullptr;    // workspace
   size_t ws_bytes = 0;
+  bool ws_captured = false; // a graph may use it: kept until the handle goes
+  struct Kept { uint8_t *p; Kept *next; } *kept = nullptr;
   CacheErr *err = nullptr;  // device
   // allocations that buffers of the present call were found in: small
   // tensors share theirs, and asking for one takes 0.6 us
@@ -204,15 +206,27 @@ struct Parts {
   }
 };
 grand_status ensure_ws(grand_cache *h, size_t bytes) {
-  if (bytes <= h->ws_bytes) return GRAND_OK;
+  if (!bytes) return GRAND_OK;
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
   HCHK(h, hipStreamIsCapturing(h->stream, &cs));
-  if (cs != hipStreamCaptureStatusNone)
+  const bool capturing = cs != hipStreamCaptureStatusNone;
+  if (bytes <= h->ws_bytes) {
+    h->ws_captured |= capturing;
+    return GRAND_OK;
+  }
+  if (capturing)
     return fail(h, GRAND_E_CAPACITY, "the workspace must grow to %zu bytes: run the call once before the capture", bytes);
   HCHK(h, hipStreamSynchronize(h->stream));
-  if (h->ws) (void)hipFree(h->ws);
+  if (h->ws_captured) {
+    grand_cache::Kept *k = new (std::nothrow) grand_cache::Kept{h->ws, h->kept};
+    if (!k) return fail(h, GRAND_E_OOM, "no host memory");
+    h->kept = k;
+  } else if (h->ws) {
+    (void)hipFree(h->ws);
+  }
   h->ws = nullptr;
   h->ws_bytes = 0;
+  h->ws_captured = false;
   const size_t want = bytes + bytes / 4;
   if (hipMalloc((void **)&h->ws, want) != hipSuccess) {
     (void)hipGetLastError();
@@ -282,6 +296,11 @@ grand_status grand_cache_destroy(grand_cache *h) {
   (void)hipSetDevice(h->p.device);
   if (!h->poisoned) (void)hipStreamSynchronize(h->stream);
   if (h->ws) (void)hipFree(h->ws);
+  while (grand_cache::Kept *k = h->kept) {
+    h->kept = k->next;
+    (void)hipFree(k->p);
+    delete k;
+  }
   if (h->err) (void)hipFree(h->err);
   delete h;
   return GRAND_OK;

@@ -428,6 +428,46 @@ def test_capture_cannot_grow_the_workspace():
     cache.close()
 
 
+def test_graphs_outlive_a_larger_workspace():
+    """A graph's workspace is not given back when a later call needs more."""
+    import torch
+
+    c, big = make(qs=(1,), ks=(1800,)), make(qs=(1, 1, 1, 1), ks=(9000,) * 4, seed=1)
+    stream = torch.cuda.Stream()
+    cache = cache_for(c)
+    cache.set_stream(stream.cuda_stream)
+    s, q = seqs_for(cache, c), c["q"].cuda()
+    w = torch.zeros(1, 2, 1800, device="cuda")
+    wo = torch.zeros_like(w)
+    out, lse = torch.zeros_like(q), torch.zeros(1, 4, device="cuda")
+    torch.cuda.synchronize()
+
+    def step():
+        cache.attend(s, q, c["k_pages"], c["v_pages"], weights=w, weights_out=wo, out=out, lse=lse)
+
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    want = [x.clone() for x in (out, lse, wo)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    sb, qb, wb = seqs_for(cache, big), big["q"].cuda(), torch.zeros(4, 2, 9000, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(stream):
+            got = cache.attend(sb, qb, big["k_pages"], big["v_pages"], weights=wb, weights_out=torch.zeros_like(wb))
+        stream.synchronize()
+        compare(big, got[0], got[1], weights=got[2], before=wb)
+        out.zero_(), lse.zero_(), wo.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out, lse, wo), want))
+    del graph
+    cache.close()
+
+
 def test_offsets_above_32_bits():
     """Pages far beyond 2^32 bytes of a pool."""
     import torch
