@@ -420,7 +420,9 @@ class Sequences:
 class Cache:
     """The key/value-cache operators on one GPU (grand_cache_create ...
     grand_cache_destroy).  Every tensor is a torch tensor of that GPU; the
-    calls enqueue work on the cache's stream and return.
+    calls enqueue work on the cache's stream and return.  Results that a call
+    makes belong to that stream, as if allocated under it; memory that other
+    streams read or write is ordered, and kept until then, by the caller.
 
     Queries, results, new keys and values are (tokens, heads, head_dim), pages
     (pages, page_size, kv_heads, head_dim) views of any layout whose rows are
@@ -446,6 +448,8 @@ class Cache:
             raise GrandError(rc, "grand_cache_create failed")
         self.h = h
         self._torch, self._device = torch, torch.device("cuda", device)
+        self._current = torch._C._cuda_getCurrentRawStream  # 0.1 us, a Stream object 1
+        self._own_stream(stream)
         self._q, self._kv, self._dim, self._page = q_heads, kv_heads, head_dim, page_size
         self._page_shape = (page_size, kv_heads, head_dim)
         self._int = (torch.int32, torch.uint32)
@@ -475,6 +479,12 @@ class Cache:
 
     def set_stream(self, stream: int):
         self._check(self.lib.grand_cache_set_stream(self.h, ctypes.c_void_p(stream)))
+        self._own_stream(stream)
+
+    def _own_stream(self, stream):
+        self._raw = stream or 0
+        cuda = self._torch.cuda
+        self._stream = cuda.ExternalStream(stream, device=self._device) if stream else cuda.default_stream(self._device)
 
     def check(self):
         """Waits for the stream; raises if a kernel found an id, a length or
@@ -518,14 +528,20 @@ class Cache:
         a.p, a.seq_stride, a.head_stride = w.data_ptr(), w.stride(0), w.stride(1)
         return self._refs[name]
 
-    def _out(self, q, tokens):
-        if q.is_contiguous():
-            return self._torch.empty_like(q)
-        return self._torch.empty((tokens, self._q, self._dim), dtype=self.torch_dtype, device=self._device)
+    def _empty(self, shape, dtype):
+        """Memory for a result: of the cache's stream, as memory that the current
+        one has given back may still be in use there."""
+        if self._current(self._device.index) == self._raw:
+            return self._torch.empty(shape, dtype=dtype, device=self._device)
+        with self._torch.cuda.stream(self._stream):
+            return self._torch.empty(shape, dtype=dtype, device=self._device)
+
+    def _out(self, tokens):
+        return self._empty((tokens, self._q, self._dim), self.torch_dtype)
 
     def _lse(self, lse, tokens):
         if lse is None:
-            return self._torch.empty((tokens, self._q), dtype=self._torch.float32, device=self._device)
+            return self._empty((tokens, self._q), self._torch.float32)
         if lse.dtype != self._torch.float32 or lse.shape != (tokens, self._q) or not lse.is_contiguous() or not lse.is_cuda:
             raise ValueError(f"lse must be a contiguous ({tokens}, {self._q}) float32 tensor on the GPU")
         return lse
@@ -568,7 +584,7 @@ class Cache:
         n = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:
-            out = self._out(q, n)
+            out = self._out(n)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
         wi = wo = None
@@ -594,7 +610,7 @@ class Cache:
         k, stride = int(ids.shape[2]), ids.stride()
         self._ints("ids", ids, (n, self._q, k))
         if out is None:
-            out = self._out(q, n)
+            out = self._out(n)
         ro = self._rows("out", out, self._q, n)
         lse = self._lse(lse, n)
         rp = zp = None
@@ -613,10 +629,10 @@ class Cache:
         wi = self._weights("weights", weights, n, seqs.max_k)
         self._ints("budget", budget, (n,))
         heads, cap = weights.shape[1], weights.shape[2]
-        empty, i32, dev = self._torch.empty, self._torch.int32, self._device
-        table, freed = empty((n, pages), dtype=i32, device=dev), empty((n, pages), dtype=i32, device=dev)
-        lens, n_freed = empty(n, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
-        new = empty((n, heads, cap), dtype=self._torch.float32, device=dev)
+        empty, i32 = self._empty, self._torch.int32
+        table, freed = empty((n, pages), i32), empty((n, pages), i32)
+        lens, n_freed = empty(n, i32), empty(n, i32)
+        new = empty((n, heads, cap), self._torch.float32)
         wo = self._weights("weights_out", new, n, cap)
         self._check(self.lib.grand_cache_evict(self.h, seqs.ref, heads, cap, wi, budget.data_ptr(), sinks, recent, table.data_ptr(),
                                                wo, lens.data_ptr(), freed.data_ptr(), n_freed.data_ptr()))

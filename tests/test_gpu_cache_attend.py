@@ -359,6 +359,27 @@ def test_another_stream():
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
 
 
+def test_results_belong_to_the_caches_stream():
+    """Memory that the current stream's program has given back is not used
+    for results on another stream, where nothing orders the two."""
+    import torch
+
+    c = make(qs=(1, 1), ks=(2500, 300))
+    want = run(c)
+    side = torch.cuda.Stream()
+    cache = cache_for(c)
+    s, q = seqs_for(cache, c), c["q"].cuda()
+    torch.cuda.synchronize()
+    cache.set_stream(side.cuda_stream)
+    back = [torch.empty_like(want[0]), torch.empty_like(want[1])]
+    gone = [x.data_ptr() for x in back]
+    del back
+    out, lse = cache.attend(s, q, c["k_pages"], c["v_pages"])
+    side.synchronize()
+    assert out.data_ptr() not in gone and lse.data_ptr() not in gone
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_graph_replays():
     """A captured step gives the eager results on every replay, with other
     work between them and other contents of its inputs."""
