@@ -427,7 +427,8 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
  * of weights_out becomes entry j of weights_in plus the softmax weight that
  * the new tokens give to cached token j, summed over them and the query
  * heads of the key/value head; entries from lens[b] on are not written.
- * The two may be one buffer, but not overlap otherwise. */
+ * The two may be one buffer, but not overlap otherwise.  Without weights out
+ * may be q itself, with its strides; it overlaps no other buffer. */
 grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages,
                                 float scale, int causal, uint32_t window, const grand_rows *out, float *lse,
                                 const grand_weights *weights_in, const grand_weights *weights_out);

@@ -370,6 +370,8 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
     if (lse) TRY(check_mem(h, "lse", lse, (uint64_t)s->n_tokens * p.q_heads * 4, 4));
   }
   if (weights_out) {
+    // the weights are computed from q once out is written
+    if (s->n_tokens && out->p == q->p) return fail(h, GRAND_E_ARG, "out is q, which the weights still need");
     TRY(check_weights(h, "weights_in", weights_in, s->n_seq, p.kv_heads, s->max_k, false, &a.win));
     TRY(check_weights(h, "weights_out", weights_out, s->n_seq, p.kv_heads, s->max_k, true, &a.wout));
   }
