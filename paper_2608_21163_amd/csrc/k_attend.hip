@@ -971,7 +971,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
     lds_barrier();
     // (the last row's token is at most (RT - 1) / group + 1 on)
     const int p_lo = ch.p0 + (int)first_tok, p_hi = p_lo + (int)((RT - 1) / a.group) + 1;
-    const bool masked = (a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window);
+    // (rows past the last are zeros, which an infinite key makes NaN of)
+    const bool masked = (a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window) || r0 + RT > r_hi;
 #pragma unroll
     for (int rb = 0; rb < RT / 32; rb++) {
       v16f s[2] = {v16f{}, v16f{}};
@@ -985,13 +986,14 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
       if (masked) {
         int k0 = wkey;
         asm volatile("" : "+s"(k0));
-        const int pos = ch.p0 + (int)(min(r0 + rb * 32 + col, r_hi - 1) / a.group);
+        const uint32_t row = r0 + rb * 32 + col;
+        const int pos = ch.p0 + (int)(min(row, r_hi - 1) / a.group);
 #pragma unroll
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
-            const bool hidden = (a.causal && key > pos) || (a.window && key <= pos - (int)a.window);
+            const bool hidden = row >= r_hi || (a.causal && key > pos) || (a.window && key <= pos - (int)a.window);
             acc[kb][i] += hidden ? 0.f : ex2(__builtin_fmaf(s[kb][i], a.c, -z));
           }
       } else {
