@@ -22,7 +22,13 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float kLn2 = 0.69314718055994531f;
 
+// kUp, kLagUp: probabilities enter their product at 2^kUp times their size
+// where the largest is 1, at 2^kLagUp times where it may reach 2^8 (tile_step).
+// fp16 has steps of 2^-24 below 2^-14: the weight of tokens 2^-25 of the largest
+// and less would be lost from the results, though not from the sum that divides
+// them, however many they are.  Powers of two, taken back at the end.
 struct Bf16 {
+  static constexpr int kUp = 0, kLagUp = 0;
   static constexpr uint32_t kExp = 0x7F807F80u, kExpLow = 0x00800080u, kInf = 0x7F80u;  // exponent bits of two elements, their lowest bits, of one
   typedef __bf16 T;
   typedef v8bf V;
@@ -30,6 +36,7 @@ struct Bf16 {
   static __device__ __forceinline__ v4f mul16(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
+  static constexpr int kUp = 14, kLagUp = 7;
   static constexpr uint32_t kExp = 0x7C007C00u, kExpLow = 0x04000400u, kInf = 0x7C00u;
   typedef _Float16 T;
   typedef v8h V;
@@ -38,6 +45,7 @@ struct F16 {
 };
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+constexpr float down(int up) { return 1.f / (float)(1 << up); }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
 
@@ -157,7 +165,8 @@ template <class E, int DP>
 struct RowState {
   typename E::V q[DP / 16];
   v16f o[DP / 32];
-  float m, l;  // what scores are taken against (log2 units; -inf: no key seen), this lane's share of the sum
+  // what scores are taken against (log2 units, kLagUp below a maximum; -inf: no key seen), this lane's share of the sum
+  float m, l;
 
   __device__ __forceinline__ void init(const AttendArgs &a, bool valid, uint32_t token, uint32_t head, int half) {
     m = neg_inf();
@@ -251,8 +260,9 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
   // largest probability is then rounded too, not 1: bf16 results are 0.0023 off
   // on average instead of 0.0020 (their own rounding is 0.0017); following the
   // true maximum costs 1 to 6%.
-  if (__ballot(mx * c > st.m + 8.f)) {
-    const float mn = fmaxf(st.m, mx * c);
+  const float top = mx * c - E::kLagUp;
+  if (__ballot(top > st.m + 8.f)) {
+    const float mn = fmaxf(st.m, top);
     const float scale = st.m == neg_inf() ? 0.f : ex2(st.m - mn);
 #pragma unroll
     for (int d = 0; d < DP / 32; d++)
@@ -396,7 +406,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
     }
     if (__syncthreads_or(odd)) add_non_finite<E, DP>(a, table, kvh, begin, end, first, last, half, st.o);
   }
-  st.l = halves(st.l, fadd2);
+  st.l = halves(st.l, fadd2) * down(E::kLagUp);
+  st.m += E::kLagUp;
+#pragma unroll
+  for (int d = 0; d < DP / 32; d++) st.o[d] *= down(E::kLagUp);
   if (valid) write_row<E, DP>(a, st.o, st.m, st.l, ch.r0 + tok, head, split, direct, half);
 }
 
@@ -592,9 +605,9 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
         }
         float mx = fmaxf(fmaxf(fmaxf(sc[nb][0][0], sc[nb][0][1]), fmaxf(sc[nb][0][2], sc[nb][0][3])),
                          fmaxf(fmaxf(sc[nb][1][0], sc[nb][1][1]), fmaxf(sc[nb][1][2], sc[nb][1][3])));
-        mx = halves(rows16(mx, fmax2), fmax2) * a.c;
+        mx = halves(rows16(mx, fmax2), fmax2) * a.c - E::kUp;
         // the true maximum (unlike tile_step's): the largest probability is
-        // then 1, which 16 bits hold, and the loads hide the rescaling
+        // then a power of two, which 16 bits hold, and the loads hide the rescaling
         if (__ballot(mx > m[nb])) {
           const float mn = fmaxf(m[nb], mx), scale = m[nb] == neg_inf() ? 0.f : ex2(m[nb] - mn);
 #pragma unroll
@@ -666,10 +679,11 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
 #pragma unroll
       for (int w = 0; w < 4; w++) {
         const float2 y = ml[w][row];
-        const float f = y.x == neg_inf() ? 1.f : ex2(y.x - mm);
+        const float f = y.x == neg_inf() ? 1.f : ex2(y.x - mm) * down(E::kUp);
         ll += y.y * f;
         v += *(const v4f *)(sum + (w * 16 + row) * kSum + d) * f;
       }
+      mm += E::kUp;
       const bool some = ll > 0.f || ll != ll;
       const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
       const size_t at = (size_t)token * a.q_heads + head;
