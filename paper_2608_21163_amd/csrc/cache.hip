@@ -309,6 +309,7 @@ grand_status grand_cache_destroy(grand_cache *h) {
 grand_status grand_cache_set_stream(grand_cache *h, void *stream) {
   TRY(check_usable(h));
   if ((hipStream_t)stream == h->stream) return GRAND_OK;
+  HCHK(h, hipSetDevice(h->p.device));  // the default stream is the current GPU's
   HCHK(h, hipStreamSynchronize(h->stream));
   h->stream = (hipStream_t)stream;
   return GRAND_OK;
