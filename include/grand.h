@@ -340,6 +340,11 @@ const char *grand_last_error(const grand_index *h);
  *    GRAND_E_CAPACITY and nothing is done.  A workspace that a captured call
  *    uses is kept until the handle is destroyed, so its graph may be replayed
  *    after larger calls, ordered among the handle's calls as they are.
+ *    grand_cache_check and grand_cache_set_stream wait for the stream and
+ *    fail with GRAND_E_STATE while it is captured, as does a call that HIP
+ *    refuses because of a capture of another stream: the handle is as it was
+ *    (only GRAND_E_DEVICE poisons it).  Handles are created and destroyed
+ *    outside captures.
  *  - Sizes, strides, alignment and the extent of device buffers are checked
  *    before anything is enqueued.  What lies in device memory (page ids,
  *    lengths, chunk starts, slot ids) is checked by the kernels: nothing is

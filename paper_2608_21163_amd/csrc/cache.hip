@@ -47,6 +47,9 @@ grand_status fail(grand_cache *h, grand_status code, const char *fmt, ...) {
 
 grand_status fail_dev(grand_cache *h, hipError_t e, const char *what) {
   (void)hipGetLastError();  // the error stays with this handle
+  // refusals during a stream capture (the codes are consecutive): nothing was enqueued
+  if (e >= hipErrorStreamCaptureUnsupported && e <= hipErrorStreamCaptureWrongThread)
+    return fail(h, GRAND_E_STATE, "a stream capture does not allow %s: %s", what, hipGetErrorString(e));
   h->poisoned = true;
   return fail(h, GRAND_E_DEVICE, "HIP error in %s: %s", what, hipGetErrorString(e));
 }
@@ -68,6 +71,13 @@ grand_status check_usable(grand_cache *h) {
   h->msg[0] = 0;
   h->n_seen = 0;
   return GRAND_OK;
+}
+
+// Calls that wait for the handle's stream would break its capture.
+grand_status check_no_capture(grand_cache *h, const char *call) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  HCHK(h, hipStreamIsCapturing(h->stream, &cs));
+  return cs == hipStreamCaptureStatusNone ? GRAND_OK : fail(h, GRAND_E_STATE, "%s waits for the stream, which a capture does not allow", call);
 }
 
 // A buffer must lie in this GPU's memory, and its allocation must hold it.
@@ -310,6 +320,7 @@ grand_status grand_cache_set_stream(grand_cache *h, void *stream) {
   TRY(check_usable(h));
   if ((hipStream_t)stream == h->stream) return GRAND_OK;
   HCHK(h, hipSetDevice(h->p.device));  // the default stream is the current GPU's
+  TRY(check_no_capture(h, "grand_cache_set_stream"));
   HCHK(h, hipStreamSynchronize(h->stream));
   h->stream = (hipStream_t)stream;
   return GRAND_OK;
@@ -318,6 +329,7 @@ grand_status grand_cache_set_stream(grand_cache *h, void *stream) {
 grand_status grand_cache_check(grand_cache *h) {
   TRY(check_usable(h));
   HCHK(h, hipSetDevice(h->p.device));
+  TRY(check_no_capture(h, "grand_cache_check"));
   CacheErr e{};
   HCHK(h, hipMemcpyAsync(&e, h->err, sizeof e, hipMemcpyDeviceToHost, h->stream));
   HCHK(h, hipStreamSynchronize(h->stream));

@@ -87,9 +87,49 @@ def test_a_stream_is_waited_for_on_its_own_gpu(built):
     c = Host(built, device=3)
     built.fake_device(0)
     assert built.grand_cache_set_stream(c.h, 77) == grand.OK
-    assert c.log() == ["hipSetDevice on 3", "hipStreamSynchronize of stream 0 on 3"]
+    assert c.log() == ["hipSetDevice on 3", "hipStreamIsCapturing on 3", "hipStreamSynchronize of stream 0 on 3"]
     built.fake_device(0)
     assert built.grand_cache_set_stream(c.h, 77) == grand.OK and c.log() == []   # no change, no wait
     s, q, pages, out = c.seqs(), c.rows(), c.pages(), c.rows()
     assert c.attend(s, q, pages, out) == grand.OK
     assert all(x.endswith(" on 3") for x in c.log())
+
+
+IMPLICIT, LAUNCH_FAILURE = 906, 719   # hipErrorStreamCaptureImplicit, hipErrorLaunchFailure
+
+
+def test_calls_that_a_capture_does_not_allow(built):
+    """The check and a change of streams wait, which would break a capture of the
+    handle's stream: they are refused before that, and the handle goes on."""
+    c = Host(built, stream=5)
+    built.fake_capture(1, 5)
+    for call in (lambda: built.grand_cache_check(c.h), lambda: built.grand_cache_set_stream(c.h, 6)):
+        assert call() == grand.E_STATE and "capture" in c.error()
+        assert not any("Synchronize" in x or "Memcpy" in x for x in c.log())
+    assert built.grand_cache_set_stream(c.h, 5) == grand.OK
+    assert c.attend(c.seqs(), c.rows(), c.pages(), c.rows()) == grand.OK
+    built.fake_capture(0, None)
+    assert built.grand_cache_check(c.h) == grand.OK
+    assert built.grand_cache_set_stream(c.h, 6) == grand.OK
+    assert c.attend(c.seqs(), c.rows(), c.pages(), c.rows()) == grand.OK
+
+
+def test_a_capture_elsewhere_does_not_end_the_handle(built):
+    """A handle on the default stream while another stream is captured: HIP
+    refuses what is done there, and the handle is as it was afterwards."""
+    c = Host(built)
+    args = c.seqs(max_k=4000), c.rows(), c.pages(600), c.rows()
+    for call in (b"hipStreamIsCapturing", b"attend", b"join"):
+        built.fake_fail(call, IMPLICIT)
+        assert c.attend(*args) == grand.E_STATE and "capture" in c.error()
+        built.fake_fail(call, 0)
+        assert c.attend(*args) == grand.OK
+    for call in (b"hipStreamIsCapturing", b"hipMemcpyAsync", b"hipStreamSynchronize"):
+        built.fake_fail(call, IMPLICIT)
+        assert built.grand_cache_check(c.h) == grand.E_STATE
+        built.fake_fail(call, 0)
+        assert built.grand_cache_check(c.h) == grand.OK
+    built.fake_fail(b"attend", LAUNCH_FAILURE)     # any other failure does end it
+    assert c.attend(*args) == grand.E_DEVICE
+    built.fake_fail(b"attend", 0)
+    assert c.attend(*args) == grand.E_STATE

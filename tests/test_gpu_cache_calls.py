@@ -172,3 +172,38 @@ def test_lists_longer_than_a_round():
     one, z = cache.attend_ids(q, kp, vp, ids[:, :, :1].contiguous())
     cache.check()
     assert torch.equal(out, one) and abs(float(lse - z) - math.log(5000)) < 1e-5
+
+
+def test_waiting_calls_inside_a_capture():
+    """The check and a change of streams are refused while the stream is
+    captured; the capture and the handle go on."""
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_STATE
+
+    c = make(qs=(1, 1), ks=(300, 40))
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    cache = cache_for(c)
+    cache.set_stream(stream.cuda_stream)
+    s, q = seqs_for(cache, c), c["q"].cuda()
+    out, lse = torch.zeros_like(q), torch.zeros(2, 4, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        cache.attend(s, q, c["k_pages"], c["v_pages"], out=out, lse=lse)
+        for call in (cache.check, lambda: cache.set_stream(other.cuda_stream)):
+            with pytest.raises(GrandError) as e:
+                call()
+            assert e.value.code == E_STATE and "capture" in str(e.value)
+    for _ in range(3):
+        out.zero_(), lse.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        compare(c, out, lse)
+    cache.check()
+    cache.set_stream(other.cuda_stream)
+    cache.check()
+    del graph
+    cache.close()
