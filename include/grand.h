@@ -433,7 +433,10 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
  * the new tokens give to cached token j, summed over them and the query
  * heads of the key/value head; entries from lens[b] on are not written.
  * The two may be one buffer, but not overlap otherwise.  Without weights out
- * may be q itself, with its strides; it overlaps no other buffer. */
+ * may be q itself, with its strides; it overlaps neither otherwise, nor the
+ * pages (GRAND_E_ARG; rows of equal strides may lie between each other's,
+ * rows of different strides may not lie inside each other's extent), nor any
+ * other buffer. */
 grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages,
                                 float scale, int causal, uint32_t window, const grand_rows *out, float *lse,
                                 const grand_weights *weights_in, const grand_weights *weights_out);
@@ -447,7 +450,8 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
  * prior, prior_lse: null, or another attention's result of the same rows
  * over other tokens (out and lse of grand_cache_attend): the call returns
  * what attention over both would.  lse: n_seq x q_heads, or null.
- * out and lse may be prior (with its strides) and prior_lse themselves. */
+ * out and lse may be prior (with its strides) and prior_lse themselves, out
+ * may be q; they overlap them in no other way, nor the pages. */
 grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_rows *q, const grand_pages *pages,
                                     const uint32_t *ids, uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride,
                                     float scale, const grand_rows *prior, const float *prior_lse,
@@ -461,7 +465,7 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
  * head token by token, of its entries of `weights` (`heads` heads, rows of
  * `cap` entries); equal scores stay lowest index first, NaN counts as
  * -inf.  The order of the pages is kept.
- * Outputs, which overlap no input: out_table (n_seq x max_pages, packed; the
+ * Outputs, which overlap no input and not each other: out_table (n_seq x max_pages, packed; the
  * kept pages, then GRAND_INVALID), out_weights (`cap` entries a row: the
  * kept tokens' weights, then zeros), out_lens, freed (n_seq x max_pages: the
  * freed page ids in table order, then GRAND_INVALID), n_freed.  The pages'

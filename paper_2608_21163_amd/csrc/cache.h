@@ -23,6 +23,7 @@ struct PagesView {
   uint32_t page, slot, head; // strides in bytes; a page's rows lie within 2^32 bytes of its start
   uint32_t n_pages;
   uint32_t shift;            // log2 of the page size
+  uint64_t bytes;            // up to the last page's last row
 };
 
 struct SeqsView {

@@ -114,6 +114,46 @@ bool extent(uint64_t n0, int64_t s0, uint64_t n1, int64_t s1, uint64_t n2, int64
   return true;
 }
 
+// Rows of len bytes at p + i0 * s0 + i1 * s1, and what two of them share.
+struct Region {
+  uintptr_t p;
+  uint64_t n0, n1;
+  int64_t s0, s1;
+  uint64_t len;
+};
+Region region(const RowsView &r, uint64_t tokens, uint64_t heads, uint32_t dim) {
+  return {(uintptr_t)r.p, tokens, heads, r.token, r.head, dim * 2ull};
+}
+Region region(const WeightsView &w, uint64_t n_seq, uint64_t heads, uint64_t cap) {
+  return {(uintptr_t)w.p, n_seq, heads, w.seq * 4, w.head * 4, cap * 4};
+}
+Region region(const void *p, uint64_t bytes) { return {(uintptr_t)p, 1, 1, 0, 0, bytes}; }
+
+bool same_rows(const Region &a, const Region &b) {
+  return a.p == b.p && (a.n0 == 1 || a.s0 == b.s0) && (a.n1 == 1 || a.s1 == b.s1);
+}
+int64_t floor_div(int64_t x, int64_t y) { return x / y - (x % y < 0); }  // y > 0
+// Rows of like strides may lie between each other's; rows of other strides
+// share memory if one's lies inside the other's extent at all.
+bool overlap(Region a, Region b) {
+  if (!a.len || !b.len) return false;
+  if (a.p + (a.n0 - 1) * a.s0 + (a.n1 - 1) * a.s1 + a.len <= b.p || b.p + (b.n0 - 1) * b.s0 + (b.n1 - 1) * b.s1 + b.len <= a.p) return false;
+  // the stride of an axis of one row says nothing
+  if (a.n0 == 1) a.s0 = b.s0;
+  if (b.n0 == 1) b.s0 = a.s0;
+  if (a.n1 == 1) a.s1 = b.s1;
+  if (b.n1 == 1) b.s1 = a.s1;
+  if (a.s0 != b.s0 || a.s1 != b.s1) return true;
+  for (int64_t i1 = 1 - (int64_t)a.n1; i1 < (int64_t)b.n1; i1++) {
+    // rows of a at 0 and of b at d + i0 * s0: some i0 of theirs with -len(b) < that < len(a)
+    const int64_t d = (int64_t)(b.p - a.p) + i1 * a.s1, la = (int64_t)a.len, lb = (int64_t)b.len;
+    if (a.s0 == 0 ? d < la && -d < lb
+                  : std::max(floor_div(-lb - d, a.s0) + 1, 1 - (int64_t)a.n0) <= std::min(-floor_div(d - la, a.s0) - 1, (int64_t)b.n0 - 1))
+      return true;
+  }
+  return false;
+}
+
 grand_status check_rows(grand_cache *h, const char *name, const grand_rows *r, uint64_t tokens, uint32_t heads, bool written,
                         RowsView *out) {
   if (!r) return fail(h, GRAND_E_ARG, "%s is null", name);
@@ -155,9 +195,14 @@ grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
   out->page = (uint32_t)g->page_stride * 2;
   out->slot = (uint32_t)g->slot_stride * 2;
   out->head = (uint32_t)g->head_stride * 2;
+  out->bytes = e * 2;
   out->n_pages = g->n_pages;
   out->shift = h->shift;
   return GRAND_OK;
+}
+
+grand_status check_apart(grand_cache *h, const Region &out, const PagesView &pg) {
+  return overlap(out, region(pg.k, pg.bytes)) || overlap(out, region(pg.v, pg.bytes)) ? fail(h, GRAND_E_ARG, "out overlaps pages") : GRAND_OK;
 }
 
 grand_status check_seqs(grand_cache *h, const grand_seqs *s, bool chunks, SeqsView *out) {
@@ -382,11 +427,18 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
     TRY(check_rows(h, "out", out, s->n_tokens, p.q_heads, true, &a.out));
     if (lse) TRY(check_mem(h, "lse", lse, (uint64_t)s->n_tokens * p.q_heads * 4, 4));
   }
-  if (weights_out) {
+  if (s->n_tokens) {
+    const Region rq = region(a.q, s->n_tokens, p.q_heads, p.head_dim), ro = region(a.out, s->n_tokens, p.q_heads, p.head_dim);
     // the weights are computed from q once out is written
-    if (s->n_tokens && out->p == q->p) return fail(h, GRAND_E_ARG, "out is q, which the weights still need");
+    if (overlap(rq, ro) && (weights_out || !same_rows(rq, ro)))
+      return fail(h, GRAND_E_ARG, same_rows(rq, ro) ? "out is q, which the weights still need" : "out overlaps q");
+    TRY(check_apart(h, ro, a.pg));
+  }
+  if (weights_out) {
     TRY(check_weights(h, "weights_in", weights_in, s->n_seq, p.kv_heads, s->max_k, false, &a.win));
     TRY(check_weights(h, "weights_out", weights_out, s->n_seq, p.kv_heads, s->max_k, true, &a.wout));
+    const Region ri = region(a.win, s->n_seq, p.kv_heads, s->max_k), ro = region(a.wout, s->n_seq, p.kv_heads, s->max_k);
+    if (!same_rows(ri, ro) && overlap(ri, ro)) return fail(h, GRAND_E_ARG, "weights_out overlaps weights_in");
   }
   a.lse = lse;
   a.q_heads = p.q_heads;
@@ -492,6 +544,15 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
     TRY(check_rows(h, "prior", prior, n_seq, p.q_heads, false, &a.prior));
     TRY(check_mem(h, "prior_lse", prior_lse, (uint64_t)n_seq * p.q_heads * 4, 4));
   }
+  const Region rq = region(a.q, n_seq, p.q_heads, p.head_dim), ro = region(a.out, n_seq, p.q_heads, p.head_dim);
+  if (!same_rows(rq, ro) && overlap(rq, ro)) return fail(h, GRAND_E_ARG, "out overlaps q");
+  TRY(check_apart(h, ro, a.pg));
+  if (prior) {
+    const Region rp = region(a.prior, n_seq, p.q_heads, p.head_dim);
+    if (!same_rows(rp, ro) && overlap(rp, ro)) return fail(h, GRAND_E_ARG, "out overlaps prior");
+    const uint64_t bytes = (uint64_t)n_seq * p.q_heads * 4;
+    if (lse && lse != prior_lse && overlap(region(lse, bytes), region(prior_lse, bytes))) return fail(h, GRAND_E_ARG, "lse overlaps prior_lse");
+  }
   uint64_t e = 0;
   if (!extent(n_seq, ids_seq_stride, p.q_heads, ids_head_stride, 1, 0, k, &e)) return fail(h, GRAND_E_ARG, "strides of ids are negative");
   if (k) TRY(check_mem(h, "ids", ids, e * 4, 4));
@@ -535,6 +596,16 @@ grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t hea
   }
   TRY(check_mem(h, "out_lens", out_lens, (uint64_t)s->n_seq * 4, 4));
   TRY(check_mem(h, "n_freed", n_freed, (uint64_t)s->n_seq * 4, 4));
+  const Region results[] = {region(out_table, cells * 4), region(a.wout, s->n_seq, heads, cap), region(out_lens, s->n_seq * 4ull),
+                            region(freed, cells * 4), region(n_freed, s->n_seq * 4ull)};
+  const Region inputs[] = {{(uintptr_t)s->table, s->n_seq, 1, s->table_stride * 4, 0, s->max_pages * 4ull}, region(s->lens, s->n_seq * 4ull),
+                           region(a.win, s->n_seq, heads, cap), region(budget, s->n_seq * 4ull)};
+  for (const Region &r : results) {
+    for (const Region &x : inputs)
+      if (overlap(r, x)) return fail(h, GRAND_E_ARG, "a result overlaps an argument");
+    for (const Region *x = results; x != &r; x++)
+      if (overlap(r, *x)) return fail(h, GRAND_E_ARG, "results overlap");
+  }
   Parts w;
   const int w_keys = w.add(cells * 4);
   int w_hist = -1, w_blk = -1, w_state = -1;

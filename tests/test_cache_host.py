@@ -56,7 +56,7 @@ class Host:
         return self.lib.grand_cache_last_error(self.h).decode()
 
     def memory(self, size):
-        return self.lib.fake_memory(size, self.device)
+        return self.lib.fake_memory(size + 256, self.device)   # (more than it is, as allocators give)
 
     def seqs(self, n=2, max_q=1, max_k=40, q_start=False):
         pages = -(-max_k // self.p.page_size)
@@ -133,3 +133,93 @@ def test_a_capture_elsewhere_does_not_end_the_handle(built):
     assert c.attend(*args) == grand.E_DEVICE
     built.fake_fail(b"attend", 0)
     assert c.attend(*args) == grand.E_STATE
+
+
+def moved(r, elements, **strides):
+    """The same rows, pages or weights further on, with other strides."""
+    out = type(r)()
+    ctypes.pointer(out)[0] = r
+    size = 4 if isinstance(r, grand.Weights) else 2
+    out.p += elements * size
+    for k, v in strides.items():
+        setattr(out, k, v)
+    return out
+
+
+def test_results_beside_and_over_the_queries(built):
+    """out may be q itself, or lie between its rows; every other way of sharing
+    memory races with the rows still to be read."""
+    c = Host(built)
+    n, d = 6, 64
+    s, pages = c.seqs(2, max_q=3), c.pages()
+    wide = grand.Rows(c.memory(2 * n * 12 * d * 2), 12 * d, d)     # the first six of twelve tokens of 12 heads
+    wi = c.weights()
+    ok, bad = grand.OK, grand.E_ARG
+    for q, out, want, weighted in (
+            (wide, wide, ok, bad),                                                  # in place
+            (wide, moved(wide, 4 * d), ok, ok),                                     # the next heads of the same rows
+            (moved(wide, 8 * d), wide, ok, ok),
+            (wide, moved(wide, 3 * d), bad, bad),                                   # one head in common
+            (wide, moved(wide, 8), bad, bad),                                       # a few elements in common
+            (wide, moved(wide, 12 * d), bad, bad),                                  # a token on
+            (wide, moved(wide, 12 * d + 4 * d), ok, ok),                            # a token on, the next heads
+            (wide, moved(wide, 0, token_stride=4 * d), bad, bad),                   # the same start, other strides
+            (wide, moved(wide, 0, token_stride=d, head_stride=6 * d), bad, bad),
+            (wide, moved(wide, 6 * 12 * d // 2, token_stride=4 * d), bad, bad)):    # packed, in the second half
+        assert c.attend(s, q, pages, out) == want, (out.p - q.p, c.error())
+        assert c.attend(s, q, pages, out, wi=wi, wo=wi) == weighted, (out.p - q.p, c.error())
+    one = c.seqs(1)
+    q = grand.Rows(c.memory(12 * d * 2), 12 * d, d)
+    assert c.attend(one, q, pages, moved(q, 0, token_stride=8 * d)) == ok       # one token: its stride says nothing
+    assert c.attend(one, q, pages, moved(q, 4 * d, token_stride=8 * d)) == ok
+    assert c.attend(one, q, pages, moved(q, 2 * d, token_stride=8 * d)) == bad
+    q, row = c.rows(n), c.p.kv_heads * d
+    assert c.attend(s, q, pages, grand.Rows(pages.k + 4 * row * 2, 4 * d, d)) == bad and "pages" in c.error()
+    assert c.attend(s, q, pages, grand.Rows(pages.v, 4 * d, d)) == bad
+
+
+def test_weights_in_place_or_apart(built):
+    c = Host(built)
+    s, q, pages, out = c.seqs(), c.rows(), c.pages(), c.rows()
+    w = grand.Weights(c.memory(4 * 6 * 100 * 4), 600, 100)     # rows of 40 of 100 entries, two of six heads
+    ok, bad = grand.OK, grand.E_ARG
+    for wo, want in ((w, ok), (moved(w, 200), ok), (moved(w, 40), ok), (moved(w, 39), bad), (moved(w, 100), bad), (moved(w, 600), bad),
+                     (moved(w, 0, head_stride=200), bad), (moved(w, 600, seq_stride=100, head_stride=200), bad), (moved(w, 1200), ok)):
+        assert c.attend(s, q, pages, out, wi=w, wo=wo) == want, ((wo.p - w.p) // 4, c.error())
+
+
+def test_listed_attention_in_place_or_apart(built):
+    c = Host(built)
+    n, d = 5, 64
+    pages, ids = c.pages(), c.memory(n * 4 * 7 * 4)
+    q, prior = c.rows(n), grand.Rows(c.memory(n * 12 * d * 2), 12 * d, d)
+    lse, prior_lse = c.memory(n * 4 * 4), c.memory(2 * n * 4 * 4)
+
+    def call(out, q=q, lse=lse):
+        return built.grand_cache_attend_ids(c.h, n, ctypes.byref(q), ctypes.byref(pages), ids, 7, 28, 7, 0.125, ctypes.byref(prior), prior_lse,
+                                            ctypes.byref(out), lse)
+    assert call(prior) == call(c.rows(n)) == call(q) == call(moved(prior, 4 * d)) == grand.OK
+    assert call(prior, lse=prior_lse) == call(prior, lse=prior_lse + n * 16) == grand.OK
+    assert call(moved(prior, 2 * d)) == call(moved(prior, 0, token_stride=8 * d)) == call(moved(q, 8, token_stride=4 * d)) == grand.E_ARG
+    assert call(prior, lse=prior_lse + 16) == grand.E_ARG and "lse" in c.error()
+    assert call(grand.Rows(pages.v, 4 * d, d)) == grand.E_ARG
+
+
+def test_evictions_write_over_nothing_they_read(built):
+    c = Host(built)
+    s = c.seqs(2, max_k=64)
+    buffers = dict(budget=c.memory(8), out_table=c.memory(32), out_lens=c.memory(8), freed=c.memory(32), n_freed=c.memory(8))
+    w, wo = c.weights(2, 64), c.weights(2, 64)
+
+    def call(wo=wo, **kw):
+        b = dict(buffers, **kw)
+        return built.grand_cache_evict(c.h, ctypes.byref(s), 2, 64, ctypes.byref(w), b["budget"], 1, 1, b["out_table"], ctypes.byref(wo),
+                                       b["out_lens"], b["freed"], b["n_freed"])
+    assert call() == grand.OK
+    for kw in (dict(out_table=s.table), dict(out_table=s.table + 28), dict(freed=s.table), dict(out_lens=s.lens), dict(n_freed=s.lens + 4),
+               dict(out_lens=buffers["budget"]), dict(freed=buffers["out_table"] + 16), dict(n_freed=buffers["out_lens"]), dict(wo=w),
+               dict(wo=moved(w, 32)), dict(out_table=wo.p), dict(freed=w.p)):
+        assert call(**kw) == grand.E_ARG and "overlap" in c.error(), kw
+    wide = grand.Weights(c.memory(2 * 6 * 64 * 4), 6 * 64, 64)
+    w = wide
+    assert call(wo=moved(wide, 2 * 64)) == grand.OK and call(wo=moved(wide, 64)) == grand.E_ARG
