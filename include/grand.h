@@ -414,7 +414,8 @@ const char *grand_cache_last_error(const grand_cache *h);
 
 /* Writes the new tokens' keys and values (n_tokens rows by kv_heads) to their
  * places in the pages: new token i of sequence b is cached token
- * lens[b] - chunk length + i.  No other slot is touched. */
+ * lens[b] - chunk length + i.  No other slot is touched.  No two slots of
+ * the pages may share memory. */
 grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand_rows *k, const grand_rows *v,
                                 const grand_pages *pages);
 

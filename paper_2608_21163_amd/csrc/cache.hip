@@ -201,6 +201,20 @@ grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
   return GRAND_OK;
 }
 
+// No two slots, heads or pages of pools that are written share memory: every
+// axis steps over all that the shorter steps reach.
+bool slots_apart(const grand_cache_params &p, const grand_pages *g) {
+  struct { uint64_t n; int64_t s; } axes[] = {{g->n_pages, g->page_stride}, {p.page_size, g->slot_stride}, {p.kv_heads, g->head_stride}};
+  std::sort(axes, axes + 3, [](const auto &a, const auto &b) { return a.s < b.s; });
+  uint64_t reach = p.head_dim;
+  for (const auto &x : axes) {
+    if (x.n == 1) continue;
+    if ((uint64_t)x.s < reach) return false;
+    reach += (x.n - 1) * x.s;
+  }
+  return true;
+}
+
 grand_status check_apart(grand_cache *h, const Region &out, const PagesView &pg) {
   return overlap(out, region(pg.k, pg.bytes)) || overlap(out, region(pg.v, pg.bytes)) ? fail(h, GRAND_E_ARG, "out overlaps pages") : GRAND_OK;
 }
@@ -399,8 +413,11 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
   AppendArgs a{};
   TRY(check_seqs(h, s, true, &a.s));
   TRY(check_pages(h, pages, &a.pg));
+  if (!slots_apart(h->p, pages)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
   TRY(check_rows(h, "k", k, s->n_tokens, h->p.kv_heads, false, &a.k));
   TRY(check_rows(h, "v", v, s->n_tokens, h->p.kv_heads, false, &a.v));
+  if (pages->k == pages->v && !same_rows(region(a.k, s->n_tokens, h->p.kv_heads, h->p.head_dim), region(a.v, s->n_tokens, h->p.kv_heads, h->p.head_dim)))
+    return fail(h, GRAND_E_ARG, "pages.k is pages.v, but k is not v");
   if ((uint64_t)a.s.max_q * h->p.kv_heads * (h->p.head_dim / 8) >= 1ull << 31)
     return fail(h, GRAND_E_CAPACITY, "max_q is too large");
   a.kv_heads = h->p.kv_heads;

@@ -223,3 +223,24 @@ def test_evictions_write_over_nothing_they_read(built):
     wide = grand.Weights(c.memory(2 * 6 * 64 * 4), 6 * 64, 64)
     w = wide
     assert call(wo=moved(wide, 2 * 64)) == grand.OK and call(wo=moved(wide, 64)) == grand.E_ARG
+
+
+def test_new_tokens_go_into_slots_of_their_own(built):
+    """Pages whose slots share memory may be read, but not appended to; keys
+    and values go to one pool only if they are the same rows."""
+    c = Host(built)
+    s, k, v, pages, q, out = c.seqs(), c.rows(heads=2), c.rows(heads=2), c.pages(), c.rows(), c.rows()
+
+    def append(pages, k=k, v=v):
+        r = [ctypes.byref(x) for x in (s, k, v, pages)]
+        return built.grand_cache_append(c.h, *r)
+    assert append(pages) == grand.OK
+    for kw in (dict(slot_stride=0), dict(page_stride=0), dict(head_stride=0), dict(slot_stride=64), dict(head_stride=56), dict(page_stride=2000)):
+        shared = grand.Pages(*[kw.get(f, getattr(pages, f)) for f, _ in grand.Pages._fields_])
+        assert c.attend(s, q, shared, out) == grand.OK
+        assert append(shared) == grand.E_ARG and "overlap" in c.error(), kw
+    heads_outside = grand.Pages(pages.k, pages.v, 8, 16 * 2 * 64, 64, 16 * 64)
+    assert append(heads_outside) == grand.OK
+    one = grand.Pages(pages.k, pages.k, 8, pages.page_stride, pages.slot_stride, pages.head_stride)
+    assert append(one) == grand.E_ARG and append(one, k, k) == grand.OK
+    assert c.attend(s, q, one, out) == grand.OK
