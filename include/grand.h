@@ -390,7 +390,8 @@ typedef struct {
  * q_start[b] .. q_start[b + 1] - 1 of the call's n_tokens rows (q_start
  * null: row b only, n_tokens = n_seq); lens[b] tokens are cached, the new ones
  * included (they are the last).  max_q and max_k bound the new and the
- * cached tokens of a sequence: work is laid out by them. */
+ * cached tokens of a sequence: work is laid out by them (attention and appends:
+ * max_k and min(max_q, n_tokens) together at most 2^31 - 64). */
 typedef struct {
   uint32_t n_seq, n_tokens, max_q, max_k;
   const uint32_t *table;   /* n_seq rows of max_pages page ids, table_stride apart */

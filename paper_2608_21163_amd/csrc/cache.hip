@@ -228,6 +228,9 @@ grand_status check_seqs(grand_cache *h, const grand_seqs *s, bool chunks, SeqsVi
   if (chunks) {
     if (!s->q_start && (s->n_tokens != s->n_seq || s->max_q != 1))
       return fail(h, GRAND_E_ARG, "without q_start every sequence has one new token (n_tokens = n_seq, max_q = 1)");
+    // positions are ints: to a tile of 64 keys past the last, and a window before a chunk longer than its cache
+    if ((uint64_t)s->max_k + std::min(s->max_q, s->n_tokens) > (1u << 31) - 64)
+      return fail(h, GRAND_E_CAPACITY, "max_k and max_q must be at most 2^31 - 64 together");
     if (s->q_start) TRY(check_mem(h, "q_start", s->q_start, ((uint64_t)s->n_seq + 1) * 4, 4));
   }
   uint64_t e = 0;

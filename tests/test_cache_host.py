@@ -244,3 +244,19 @@ def test_new_tokens_go_into_slots_of_their_own(built):
     one = grand.Pages(pages.k, pages.k, 8, pages.page_stride, pages.slot_stride, pages.head_stride)
     assert append(one) == grand.E_ARG and append(one, k, k) == grand.OK
     assert c.attend(s, q, one, out) == grand.OK
+
+
+def test_positions_fit_31_bits(built):
+    """Kernels compute positions in signed 32 bits: up to a tile of 64 keys past
+    the last cached token, and a window before a chunk that is longer than
+    its cache."""
+    c = Host(built, page_size=1024)
+    q, pages, out = c.rows(4096), c.pages(2), c.rows(4096)
+    for max_k, max_q, want in (((1 << 31) - 65, 1, grand.OK), ((1 << 31) - 64, 1, grand.E_CAPACITY), ((1 << 31) - 1, 1, grand.E_CAPACITY),
+                               ((1 << 31) - 4160, 4096, grand.OK), ((1 << 31) - 4159, 4096, grand.E_CAPACITY)):
+        s = c.seqs(1, max_q=max_q, max_k=max_k)
+        assert c.attend(s, q, pages, out, window=(1 << 31) - 5000) == want, (max_k, max_q)
+    s = c.seqs(1, max_q=1, max_k=(1 << 31) - 65)
+    s.max_q = 0xFFFFFFFF                      # a loose bound: there is one new token
+    s.q_start = c.memory(8)
+    assert c.attend(s, q, pages, out) == grand.OK
