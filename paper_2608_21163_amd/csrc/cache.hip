@@ -454,7 +454,7 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
       return fail(h, GRAND_E_ARG, same_rows(rq, ro) ? "out is q, which the weights still need" : "out overlaps q");
     TRY(check_apart(h, ro, a.pg));
   }
-  if (weights_out) {
+  if (weights_out && s->max_k) {
     TRY(check_weights(h, "weights_in", weights_in, s->n_seq, p.kv_heads, s->max_k, false, &a.win));
     TRY(check_weights(h, "weights_out", weights_out, s->n_seq, p.kv_heads, s->max_k, true, &a.wout));
     const Region ri = region(a.win, s->n_seq, p.kv_heads, s->max_k), ro = region(a.wout, s->n_seq, p.kv_heads, s->max_k);

@@ -260,3 +260,11 @@ def test_positions_fit_31_bits(built):
     s.max_q = 0xFFFFFFFF                      # a loose bound: there is one new token
     s.q_start = c.memory(8)
     assert c.attend(s, q, pages, out) == grand.OK
+
+
+def test_weights_of_no_cached_tokens(built):
+    """max_k 0: weights have no entries and, as empty tensors, no memory."""
+    c = Host(built)
+    none = grand.Weights(None, 0, 0)
+    assert c.attend(c.seqs(2, max_k=0), c.rows(), c.pages(), c.rows(), wi=none, wo=none) == grand.OK
+    assert c.attend(c.seqs(2, max_k=1), c.rows(), c.pages(), c.rows(), wi=none, wo=none) == grand.E_ARG

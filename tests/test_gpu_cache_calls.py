@@ -207,3 +207,13 @@ def test_waiting_calls_inside_a_capture():
     cache.check()
     del graph
     cache.close()
+
+
+def test_weights_of_no_cached_tokens():
+    """Nothing cached and weights without entries: empty rows as without them."""
+    import torch
+
+    c = make(qs=(2, 1), ks=(0, 0))
+    w = torch.zeros(2, 2, 0, device="cuda")
+    out, lse, got = run(c, weights=w)
+    assert got is w and not out.any() and torch.isneginf(lse).all()
