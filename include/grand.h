@@ -350,8 +350,9 @@ const char *grand_last_error(const grand_index *h);
  *    lengths, chunk starts, slot ids) is checked by the kernels: nothing is
  *    read or written outside the buffers, the results of the sequence
  *    concerned are unspecified, and grand_cache_check reports it.
- *  - Strides are in elements.  The elements of one head's row are
- *    contiguous; rows start at multiples of 16 bytes (8 elements).
+ *  - Strides are in elements; that of an axis of one element is not looked at.
+ *    The elements of one head's row are contiguous; rows start at multiples
+ *    of 16 bytes (8 elements).
  */
 typedef struct grand_cache grand_cache;
 enum { GRAND_BF16 = 2, GRAND_F16 = 3 };

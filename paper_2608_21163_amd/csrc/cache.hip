@@ -104,6 +104,9 @@ grand_status check_mem(grand_cache *h, const char *name, const void *p, uint64_t
   return GRAND_OK;
 }
 
+// The stride of an axis of one element says nothing (views may have any).
+int64_t step(uint64_t n, int64_t stride) { return n > 1 ? stride : 0; }
+
 // Elements up to which rows n0 x n1 x n2 at these strides reach; false when
 // a stride is negative or the extent does not fit 62 bits.
 bool extent(uint64_t n0, int64_t s0, uint64_t n1, int64_t s1, uint64_t n2, int64_t s2, uint64_t row, uint64_t *out) {
@@ -158,20 +161,21 @@ grand_status check_rows(grand_cache *h, const char *name, const grand_rows *r, u
                         RowsView *out) {
   if (!r) return fail(h, GRAND_E_ARG, "%s is null", name);
   uint64_t e = 0;
-  if (r->token_stride % 8 || r->head_stride % 8 || !extent(tokens, r->token_stride, heads, r->head_stride, 1, 0, h->p.head_dim, &e))
+  const int64_t token = step(tokens, r->token_stride), head = step(heads, r->head_stride);
+  if (token % 8 || head % 8 || !extent(tokens, token, heads, head, 1, 0, h->p.head_dim, &e))
     return fail(h, GRAND_E_ARG, "strides of %s must be multiples of 8 elements, not negative", name);
   // rows that are written must not overlap: one head's rows lie inside the
   // other stride
   if (written) {
-    const uint64_t d = h->p.head_dim, ts = (uint64_t)r->token_stride, hs = (uint64_t)r->head_stride;
+    const uint64_t d = h->p.head_dim, ts = (uint64_t)token, hs = (uint64_t)head;
     const bool ok = (heads == 1 || hs >= d) && (tokens == 1 || ts >= d) &&
                     (tokens == 1 || heads == 1 || ts >= (heads - 1) * hs + d || hs >= (tokens - 1) * ts + d);
     if (!ok) return fail(h, GRAND_E_ARG, "rows of %s overlap", name);
   }
   TRY(check_mem(h, name, r->p, e * 2, 16));
   out->p = static_cast<uint8_t *>(r->p);
-  out->token = r->token_stride * 2;
-  out->head = r->head_stride * 2;
+  out->token = token * 2;
+  out->head = head * 2;
   return GRAND_OK;
 }
 
@@ -180,21 +184,22 @@ grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
   uint64_t e = 0;
   if (g->n_pages == 0) return fail(h, GRAND_E_ARG, "the pool has no pages");
   if ((uint64_t)g->n_pages << h->shift > 0xFFFFFFFFull) return fail(h, GRAND_E_CAPACITY, "a pool holds fewer than 2^32 slots");
-  if (g->page_stride % 8 || g->slot_stride % 8 || g->head_stride % 8 ||
-      !extent(g->n_pages, g->page_stride, h->p.page_size, g->slot_stride, h->p.kv_heads, g->head_stride, h->p.head_dim, &e))
+  const int64_t page = step(g->n_pages, g->page_stride), slot = step(h->p.page_size, g->slot_stride), head = step(h->p.kv_heads, g->head_stride);
+  if (page % 8 || slot % 8 || head % 8 ||
+      !extent(g->n_pages, page, h->p.page_size, slot, h->p.kv_heads, head, h->p.head_dim, &e))
     return fail(h, GRAND_E_ARG, "strides of pages must be multiples of 8 elements, not negative");
   // offsets inside a page are computed in 32 bits
   uint64_t in_page = 0;
-  if (!extent(1, 0, h->p.page_size, g->slot_stride, h->p.kv_heads, g->head_stride, h->p.head_dim, &in_page) || in_page >= 1ull << 31 ||
-      g->page_stride >= 1ll << 31 || g->slot_stride >= 1ll << 31 || g->head_stride >= 1ll << 31)
+  if (!extent(1, 0, h->p.page_size, slot, h->p.kv_heads, head, h->p.head_dim, &in_page) || in_page >= 1ull << 31 ||
+      page >= 1ll << 31 || slot >= 1ll << 31 || head >= 1ll << 31)
     return fail(h, GRAND_E_CAPACITY, "a page and its strides must stay below 2^31 elements");
   TRY(check_mem(h, "pages.k", g->k, e * 2, 16));
   TRY(check_mem(h, "pages.v", g->v, e * 2, 16));
   out->k = static_cast<const uint8_t *>(g->k);
   out->v = static_cast<const uint8_t *>(g->v);
-  out->page = (uint32_t)g->page_stride * 2;
-  out->slot = (uint32_t)g->slot_stride * 2;
-  out->head = (uint32_t)g->head_stride * 2;
+  out->page = (uint32_t)page * 2;
+  out->slot = (uint32_t)slot * 2;
+  out->head = (uint32_t)head * 2;
   out->bytes = e * 2;
   out->n_pages = g->n_pages;
   out->shift = h->shift;
@@ -203,13 +208,14 @@ grand_status check_pages(grand_cache *h, const grand_pages *g, PagesView *out) {
 
 // No two slots, heads or pages of pools that are written share memory: every
 // axis steps over all that the shorter steps reach.
-bool slots_apart(const grand_cache_params &p, const grand_pages *g) {
-  struct { uint64_t n; int64_t s; } axes[] = {{g->n_pages, g->page_stride}, {p.page_size, g->slot_stride}, {p.kv_heads, g->head_stride}};
+bool slots_apart(const grand_cache_params &p, const PagesView &g) {
+  const uint64_t n = p.page_size;
+  struct { uint64_t n, s; } axes[] = {{g.n_pages, g.page}, {n, g.slot}, {p.kv_heads, g.head}};
   std::sort(axes, axes + 3, [](const auto &a, const auto &b) { return a.s < b.s; });
-  uint64_t reach = p.head_dim;
+  uint64_t reach = p.head_dim * 2;
   for (const auto &x : axes) {
     if (x.n == 1) continue;
-    if ((uint64_t)x.s < reach) return false;
+    if (x.s < reach) return false;
     reach += (x.n - 1) * x.s;
   }
   return true;
@@ -222,7 +228,8 @@ grand_status check_apart(grand_cache *h, const Region &out, const PagesView &pg)
 grand_status check_seqs(grand_cache *h, const grand_seqs *s, bool chunks, SeqsView *out) {
   if (!s) return fail(h, GRAND_E_ARG, "seqs is null");
   if (s->n_seq > 65535) return fail(h, GRAND_E_CAPACITY, "at most 65535 sequences a call");
-  if (s->table_stride < (int64_t)s->max_pages) return fail(h, GRAND_E_ARG, "table_stride is below max_pages");
+  const int64_t stride = s->n_seq > 1 ? s->table_stride : s->max_pages;
+  if (stride < (int64_t)s->max_pages) return fail(h, GRAND_E_ARG, "table_stride is below max_pages");
   if (s->max_k > (uint64_t)s->max_pages << h->shift) return fail(h, GRAND_E_ARG, "max_k tokens do not fit max_pages pages");
   if (s->max_k >= 1u << 31) return fail(h, GRAND_E_CAPACITY, "max_k must be below 2^31");
   if (chunks) {
@@ -234,11 +241,11 @@ grand_status check_seqs(grand_cache *h, const grand_seqs *s, bool chunks, SeqsVi
     if (s->q_start) TRY(check_mem(h, "q_start", s->q_start, ((uint64_t)s->n_seq + 1) * 4, 4));
   }
   uint64_t e = 0;
-  if (!extent(s->n_seq, s->table_stride, 1, 0, 1, 0, s->max_pages, &e)) return fail(h, GRAND_E_ARG, "table_stride is too large");
+  if (!extent(s->n_seq, stride, 1, 0, 1, 0, s->max_pages, &e)) return fail(h, GRAND_E_ARG, "table_stride is too large");
   if (s->max_pages) TRY(check_mem(h, "table", s->table, e * 4, 4));
   TRY(check_mem(h, "lens", s->lens, (uint64_t)s->n_seq * 4, 4));
   out->table = s->table;
-  out->table_stride = s->table_stride;
+  out->table_stride = stride;
   out->q_start = s->q_start;
   out->lens = s->lens;
   out->n_seq = s->n_seq;
@@ -253,17 +260,18 @@ grand_status check_weights(grand_cache *h, const char *name, const grand_weights
                            bool written, WeightsView *out) {
   if (!w) return fail(h, GRAND_E_ARG, "%s is null", name);
   uint64_t e = 0;
-  if (!extent(n_seq, w->seq_stride, heads, w->head_stride, 1, 0, cap, &e)) return fail(h, GRAND_E_ARG, "strides of %s are negative", name);
+  const int64_t seq = step(n_seq, w->seq_stride), head = step(heads, w->head_stride);
+  if (!extent(n_seq, seq, heads, head, 1, 0, cap, &e)) return fail(h, GRAND_E_ARG, "strides of %s are negative", name);
   if (written) {
-    const uint64_t ss = (uint64_t)w->seq_stride, hs = (uint64_t)w->head_stride, c = cap;
+    const uint64_t ss = (uint64_t)seq, hs = (uint64_t)head, c = cap;
     const bool ok = (heads == 1 || hs >= c) && (n_seq == 1 || ss >= c) &&
                     (n_seq == 1 || heads == 1 || ss >= (heads - 1) * hs + c || hs >= (n_seq - 1) * ss + c);
     if (!ok) return fail(h, GRAND_E_ARG, "rows of %s overlap", name);
   }
   TRY(check_mem(h, name, w->p, e * 4, 4));
   out->p = w->p;
-  out->seq = w->seq_stride;
-  out->head = w->head_stride;
+  out->seq = seq;
+  out->head = head;
   return GRAND_OK;
 }
 
@@ -416,7 +424,7 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
   AppendArgs a{};
   TRY(check_seqs(h, s, true, &a.s));
   TRY(check_pages(h, pages, &a.pg));
-  if (!slots_apart(h->p, pages)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
+  if (!slots_apart(h->p, a.pg)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
   TRY(check_rows(h, "k", k, s->n_tokens, h->p.kv_heads, false, &a.k));
   TRY(check_rows(h, "v", v, s->n_tokens, h->p.kv_heads, false, &a.v));
   if (pages->k == pages->v && !same_rows(region(a.k, s->n_tokens, h->p.kv_heads, h->p.head_dim), region(a.v, s->n_tokens, h->p.kv_heads, h->p.head_dim)))
@@ -574,14 +582,14 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
     if (lse && lse != prior_lse && overlap(region(lse, bytes), region(prior_lse, bytes))) return fail(h, GRAND_E_ARG, "lse overlaps prior_lse");
   }
   uint64_t e = 0;
-  if (!extent(n_seq, ids_seq_stride, p.q_heads, ids_head_stride, 1, 0, k, &e)) return fail(h, GRAND_E_ARG, "strides of ids are negative");
+  a.ids_seq = step(n_seq, ids_seq_stride);
+  a.ids_head = step(p.q_heads, ids_head_stride);
+  if (!extent(n_seq, a.ids_seq, p.q_heads, a.ids_head, 1, 0, k, &e)) return fail(h, GRAND_E_ARG, "strides of ids are negative");
   if (k) TRY(check_mem(h, "ids", ids, e * 4, 4));
   if (lse) TRY(check_mem(h, "lse", lse, (uint64_t)n_seq * p.q_heads * 4, 4));
   a.prior_lse = prior_lse;
   a.lse = lse;
   a.ids = ids;
-  a.ids_seq = ids_seq_stride;
-  a.ids_head = ids_head_stride;
   a.n_seq = n_seq;
   a.k = k;
   a.q_heads = p.q_heads;
@@ -618,7 +626,7 @@ grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t hea
   TRY(check_mem(h, "n_freed", n_freed, (uint64_t)s->n_seq * 4, 4));
   const Region results[] = {region(out_table, cells * 4), region(a.wout, s->n_seq, heads, cap), region(out_lens, s->n_seq * 4ull),
                             region(freed, cells * 4), region(n_freed, s->n_seq * 4ull)};
-  const Region inputs[] = {{(uintptr_t)s->table, s->n_seq, 1, s->table_stride * 4, 0, s->max_pages * 4ull}, region(s->lens, s->n_seq * 4ull),
+  const Region inputs[] = {{(uintptr_t)s->table, s->n_seq, 1, a.s.table_stride * 4, 0, s->max_pages * 4ull}, region(s->lens, s->n_seq * 4ull),
                            region(a.win, s->n_seq, heads, cap), region(budget, s->n_seq * 4ull)};
   for (const Region &r : results) {
     for (const Region &x : inputs)

@@ -513,7 +513,7 @@ class Cache:
                 or not k.is_cuda or not v.is_cuda or stride[3] != 1):
             raise ValueError(f"k_pages and v_pages must be (pages, {self._page}, {self._kv}, {self._dim}) {self.torch_dtype} on the "
                              "GPU, contiguous along their last axis")
-        if v.stride() != stride:
+        if v.stride() != stride and any(n > 1 and a != b for n, a, b in zip(shape, stride, v.stride())):
             raise ValueError("k_pages and v_pages must have the same strides")
         g = self._args["pages"]
         g.k, g.v, g.n_pages = k.data_ptr(), v.data_ptr(), shape[0]

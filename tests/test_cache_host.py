@@ -268,3 +268,28 @@ def test_weights_of_no_cached_tokens(built):
     none = grand.Weights(None, 0, 0)
     assert c.attend(c.seqs(2, max_k=0), c.rows(), c.pages(), c.rows(), wi=none, wo=none) == grand.OK
     assert c.attend(c.seqs(2, max_k=1), c.rows(), c.pages(), c.rows(), wi=none, wo=none) == grand.E_ARG
+
+
+def test_steps_along_axes_of_one_say_nothing(built):
+    """A view's stride along an axis of length one may be anything."""
+    c = Host(built, q_heads=1, kv_heads=1, page_size=1)
+    s = c.seqs(1, max_k=6)
+    q, out, pages = c.rows(1), c.rows(1), c.pages(1)
+    w = c.weights(1, 6)
+    s.table_stride = 1
+    for x in (q, out):
+        x.token_stride, x.head_stride = 1, -3
+    pages.page_stride, pages.slot_stride, pages.head_stride = 3, -1, 1 << 40
+    w.seq_stride = w.head_stride = -1
+    assert c.attend(s, q, pages, out, wi=w, wo=w) == grand.OK, c.error()
+    r = [ctypes.byref(x) for x in (s, q, out, pages)]
+    assert built.grand_cache_append(c.h, *r) == grand.OK, c.error()
+    ids = c.memory(24)
+    assert built.grand_cache_attend_ids(c.h, 1, ctypes.byref(q), ctypes.byref(pages), ids, 6, -5, -7, 0.5, None, None, ctypes.byref(out), None) == grand.OK
+    assert built.grand_cache_evict(c.h, ctypes.byref(s), 1, 6, ctypes.byref(w), c.memory(4), 0, 0, c.memory(24), ctypes.byref(c.weights(1, 6)),
+                                   c.memory(4), c.memory(24), c.memory(4)) == grand.OK, c.error()
+    two = c.seqs(2, max_k=6)                     # of more they are judged as before
+    two.table_stride = 1
+    assert c.attend(two, c.rows(2), c.pages(2), c.rows(2)) == grand.E_ARG
+    assert c.attend(c.seqs(2), moved(c.rows(3), 0, token_stride=60), c.pages(2), c.rows(2)) == grand.E_ARG
+    assert c.attend(c.seqs(2), c.rows(2), c.pages(2), moved(c.rows(2), 0, token_stride=-64)) == grand.E_ARG

@@ -217,3 +217,24 @@ def test_weights_of_no_cached_tokens():
     w = torch.zeros(2, 2, 0, device="cuda")
     out, lse, got = run(c, weights=w)
     assert got is w and not out.any() and torch.isneginf(lse).all()
+
+
+def test_axes_of_one_in_any_layout():
+    """One head, one sequence, one token: views whose strides there are not
+    what a packed tensor has."""
+    import torch
+
+    c = make("f16", 1, 1, 64, 16, qs=(1,), ks=(130,), seed=6)
+    want = run(c)
+    k = c["k_pages"].transpose(1, 2).contiguous().transpose(1, 2)      # heads outermost: the same memory, another stride
+    assert k.stride() != c["v_pages"].stride()
+    table = c["table"].t().contiguous().t()                            # a column of ids, one apart
+    q = c["q"].cuda().view(64, 1).t().unsqueeze(1)
+    assert table.stride(0) == 1 and q.stride(0) == 1
+    cache = cache_for(c)
+    s = cache.sequences(table, c["lens"], max_k=130)
+    out, lse = cache.attend(s, q, k, c["v_pages"])
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    cache.append(s, q, q, k, c["v_pages"])
+    cache.check()
+    assert torch.equal(k[int(table[0, 129 // 16]), 129 % 16, 0], q[0, 0])
