@@ -406,13 +406,14 @@ class GrandIndex:
 
 
 class Sequences:
-    """The sequences of cache calls (grand_seqs); holds the tensors it names."""
+    """The sequences of cache calls (grand_seqs); holds the tensors it names.
+    Calls do not change it.  n_tokens is None where each call's rows say."""
 
-    def __init__(self, table, lens, q_start, n_tokens: int, max_q: int, max_k: int):
+    def __init__(self, table, lens, q_start, n_tokens: Optional[int], max_q: int, max_k: int):
         self.tensors = (table, lens, q_start)
         self.n_seq, self.max_pages, self.n_tokens = table.shape[0], table.shape[1], n_tokens
         self.max_q, self.max_k = max_q, max_k
-        self.c = Seqs(table.shape[0], n_tokens, max_q, max_k, table.data_ptr(), table.stride(0), table.shape[1],
+        self.c = Seqs(table.shape[0], n_tokens or 0, max_q, max_k, table.data_ptr(), table.stride(0), table.shape[1],
                       None if q_start is None else q_start.data_ptr(), lens.data_ptr())
         self.ref = ctypes.byref(self.c)
 
@@ -457,6 +458,8 @@ class Cache:
         self._args = {n: Rows() for n in ("q", "out", "k", "v", "prior")}
         self._args.update(pages=Pages(), weights=Weights(), weights_out=Weights())
         self._refs = {n: ctypes.byref(a) for n, a in self._args.items()}
+        self._seqs = Seqs()
+        self._seqs_ref, self._seqs_at = ctypes.byref(self._seqs), ctypes.addressof(self._seqs)
 
     def close(self):
         if getattr(self, "h", None):
@@ -552,8 +555,9 @@ class Cache:
         """Describes the sequences of the calls that follow: table (sequences,
         pages) page ids, lens cached tokens (new ones included), q_start
         (sequences + 1) the new tokens' rows, or None for one each; max_q and
-        max_k bound new and cached tokens of a sequence.  n_tokens (the rows
-        of q) is taken from the rows themselves if not given."""
+        max_k bound new and cached tokens of a sequence.  n_tokens is the number
+        of rows that q, k and v must have; if not given, with q_start, it is
+        that of each call's rows."""
         n = int(lens.shape[0])
         self._ints("lens", lens, (n,))
         if table.dim() != 2 or table.shape[0] != n:
@@ -563,25 +567,31 @@ class Cache:
             self._ints("q_start", q_start, (n + 1,))
         if max_k is None:
             max_k = int(table.shape[1]) * self._page
-        return Sequences(table, lens, q_start, n if q_start is None else (n_tokens or 0), max_q, max_k)
+        if n_tokens is not None and (n_tokens < 0 or (q_start is None and n_tokens != n)):
+            raise ValueError("n_tokens must be the number of sequences without q_start, and not negative")
+        return Sequences(table, lens, q_start, n if q_start is None else n_tokens, max_q, max_k)
 
-    @staticmethod
-    def _tokens(s: Sequences, rows) -> int:
-        if s.tensors[2] is not None:
-            s.c.n_tokens = s.n_tokens = int(rows.shape[0])
-        return s.n_tokens
+    def _tokens(self, s: Sequences, rows):
+        """The rows of a call and its grand_seqs: the description itself, or a
+        copy with their number."""
+        if s.n_tokens is not None:
+            return s.n_tokens, s.ref
+        n = int(rows.shape[0])
+        ctypes.memmove(self._seqs_at, s.ref, ctypes.sizeof(Seqs))
+        self._seqs.n_tokens = n
+        return n, self._seqs_ref
 
     def append(self, seqs: Sequences, k, v, k_pages, v_pages):
         """grand_cache_append: the new tokens' keys and values go into their pages."""
-        n = self._tokens(seqs, k)
-        self._check(self.lib.grand_cache_append(self.h, seqs.ref, self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n),
+        n, ref = self._tokens(seqs, k)
+        self._check(self.lib.grand_cache_append(self.h, ref, self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n),
                                                 self._pages(k_pages, v_pages)))
 
     def attend(self, seqs: Sequences, q, k_pages, v_pages, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                weights=None, weights_out=None, out=None, lse=None):
         """grand_cache_attend: (out, lse), and with weights (sequences,
         kv_heads, at least max_k) also weights_out (weights itself if not given)."""
-        n = self._tokens(seqs, q)
+        n, ref = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:
             out = self._out(n)
@@ -595,7 +605,7 @@ class Cache:
         elif weights_out is not None:
             raise ValueError("weights_out needs weights")
         self._check(self.lib.grand_cache_attend(
-            self.h, seqs.ref, rq, self._pages(k_pages, v_pages), self._dim ** -0.5 if scale is None else scale,
+            self.h, ref, rq, self._pages(k_pages, v_pages), self._dim ** -0.5 if scale is None else scale,
             1 if causal else 0, window, ro, lse.data_ptr(), wi, wo))
         return (out, lse) if weights is None else (out, lse, weights_out)
 

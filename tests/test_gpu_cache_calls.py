@@ -237,3 +237,32 @@ def test_axes_of_one_in_any_layout():
     cache.append(s, q, q, k, c["v_pages"])
     cache.check()
     assert torch.equal(k[int(table[0, 129 // 16]), 129 % 16, 0], q[0, 0])
+
+
+def test_described_sequences_are_not_written_to():
+    """n_tokens is what the rows must have, where it is given; where not, it is
+    the rows' of each call, and the description stays as it is for others."""
+    import torch
+
+    c = make(qs=(2, 1), ks=(30, 40))
+    want = run(c)
+    cache = cache_for(c)
+    q = c["q"].cuda()
+    more = torch.cat([q, q])                      # rows of no sequence behind
+    loose = seqs_for(cache, c)
+    before = bytes(loose.c)
+    for rows in (q, more, q):
+        out, lse = cache.attend(loose, rows, c["k_pages"], c["v_pages"])
+        assert torch.equal(out[:3], want[0]) and torch.equal(lse[:3], want[1])
+    assert bytes(loose.c) == before
+    fixed = cache.sequences(c["table"], c["lens"], c["q_start"], n_tokens=3, max_q=2, max_k=40)
+    assert torch.equal(cache.attend(fixed, q, c["k_pages"], c["v_pages"])[0], want[0])
+    kv = torch.zeros(6, 2, 64, dtype=torch.bfloat16, device="cuda")
+    one = cache.sequences(c["table"], c["lens"], n_tokens=2, max_k=40)
+    for bad in (lambda: cache.attend(fixed, more, c["k_pages"], c["v_pages"]), lambda: cache.append(fixed, kv, kv, c["k_pages"], c["v_pages"]),
+                lambda: cache.attend(one, q, c["k_pages"], c["v_pages"]),
+                lambda: cache.sequences(c["table"], c["lens"], n_tokens=3, max_k=40),
+                lambda: cache.sequences(c["table"], c["lens"], c["q_start"], n_tokens=-1)):
+        with pytest.raises(ValueError):
+            bad()
+    cache.check()
