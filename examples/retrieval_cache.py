@@ -95,6 +95,7 @@ class RetrievalLayer:
         Returns the joined result, and attention over the whole cache beside
         it for comparison."""
         s = self._grow(k, v)
+        self._index_old()        # the new token has pushed one out of the window
         near = self.cache.attend(s, q, self.k_pages, self.v_pages, window=self.window)
         ids = torch.full((1, self.hq, self.k + self.sinks), INVALID, dtype=torch.int32, device="cuda")
         group = self.hq // self.hk
@@ -103,11 +104,10 @@ class RetrievalLayer:
             dists = torch.empty(group, self.k, device="cuda")
             index.search(q[0, h * group:(h + 1) * group].float().contiguous(), self.k, self.beam, found, dists)
             ids[0, h * group:(h + 1) * group, :self.k] = found
-        if self.length - self.window >= self.sinks:
-            ids[0, :, self.k:] = self.table[0, :self.sinks]
+        out_of_window = min(self.sinks, max(0, self.length - self.window))
+        ids[0, :, self.k:self.k + out_of_window] = self.table[0, :out_of_window]
         got = self.cache.attend_ids(q, self.k_pages, self.v_pages, ids, prior=near)
         whole = self.cache.attend(s, q, self.k_pages, self.v_pages)
-        self._index_old()
         self._evict()
         self.cache.check()
         return got, whole
