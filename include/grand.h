@@ -428,18 +428,20 @@ grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand
  * s_j = scale <q, k_j>, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and
  * lse = ln sum_j exp(s_j), by (token, q_head); a row that sees nothing has
  * out = 0 and lse = -inf.  Hidden tokens have no influence, whatever their
- * keys and values hold, and pages that no row sees may have any id.  Query head h uses key/value head
- * h / (q_heads / kv_heads).  scale > 0.
+ * keys and values hold, and pages that no row sees may have any id.  Query
+ * head h uses key/value head h / (q_heads / kv_heads).  scale > 0.
+ * Scores, sums, lse and weights are computed in 32 bits; the probabilities are
+ * rounded to the type of the values for their product, and out at the end.
  * lse: n_tokens x q_heads, or null.  Rows of no sequence are not written.
  * weights_in, weights_out: null, or rows of at least max_k entries: entry j
  * of weights_out becomes entry j of weights_in plus the softmax weight that
  * the new tokens give to cached token j, summed over them and the query
  * heads of the key/value head; entries from lens[b] on are not written.
  * The two may be one buffer, but not overlap otherwise.  Without weights out
- * may be q itself, with its strides; it overlaps neither otherwise, nor the
- * pages (GRAND_E_ARG; rows of equal strides may lie between each other's,
- * rows of different strides may not lie inside each other's extent), nor any
- * other buffer. */
+ * may be q itself, with its strides; out shares no memory with q otherwise,
+ * nor with the pages (GRAND_E_ARG; rows of equal strides may lie between
+ * each other's, rows of different strides may not lie inside each other's
+ * extent), nor with any other buffer. */
 grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages,
                                 float scale, int causal, uint32_t window, const grand_rows *out, float *lse,
                                 const grand_weights *weights_in, const grand_weights *weights_out);

@@ -486,15 +486,16 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   // Keys a row tile sees at most, and the splits of them.  A split costs a
   // workgroup's start and end (about 6 us, behind the others' loads) and a
   // row of sums to join; too few leave the last workgroups alone.  64 single
-  // tokens over 1 to 8,192 cached ones, 8 heads: 1,024 workgroups 222 us,
-  // 4,096 212 us, 8,192 216 us; two over 131,072: 211, 215, 222 us.  Chunks
-  // of one or two sequences, whose tiles are alike, fill the chip once (512
-  // over 8,192: 512 workgroups 93 us, 1,024 123; two of up to 1,024 over up to
-  // 20,000: 498, 566), of more, whose lengths differ, twice (four of up to 512
-  // over up to 8,192: 188, 163).  Few rows:
-  // up to 512 keys are one launch (a token over 300: 10.9 us, in two splits
-  // 13.4); splits have 256 keys while that leaves CUs idle (a token over
-  // 1,000 waited for: 28.5 us, with 512 30.4), else 512 (16,000: 35.9, 35.0).
+  // tokens over 1 to 8,192 cached ones, 8 heads: 1,024 workgroups 216 us,
+  // 4,096 209 us, 8,192 212 us; two over 131,072: 180, 184, 184 us.  Chunks
+  // of one or two sequences fill the chip once (one of 512 over 8,192: 512
+  // workgroups 91 us, 1,024 117; two 164, 171; two of up to 1,024 over up to
+  // 20,000, by their lengths: 480, 555; 491, 560; 587, 552; 633, 563; 441, 398),
+  // of more twice, for where their lengths differ (four of up to 512 over up to
+  // 8,192: 182, 151; 204, 164; 190, 191; four of 512 over 8,192 298, 314).  Few
+  // rows: up to 512 keys are one launch (a token over 300: 12.1 us, in two splits
+  // 14.6); splits have 256 keys while that leaves CUs idle (a token over
+  // 1,000 waited for: 29.5 us, with 512 31.5), else 512 (16,000: 37.3, 36.8).
   // (a tile's rows see up to its last token, or up to the chunk's if not causal)
   const uint64_t tokens = causal ? std::min<uint64_t>(a.s.max_q, tile_rows / a.group + 2) : a.s.max_q;
   const uint64_t span = std::min<uint64_t>(s->max_k, a.window ? (uint64_t)a.window + tokens + 31 : s->max_k);
@@ -503,6 +504,8 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
   const uint64_t least = !few || (span > 512 && base * ((span + 255) / 256) <= 256) ? 256 : 512;
   uint64_t split = std::max<uint64_t>(least, (span + want - 1) / want);
   split = (split + kKeysStep - 1) / kKeysStep * kKeysStep;
+  // (31: a window's first key is rounded down to a tile; without one the last
+  // split has no keys where the split length divides max_k)
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   if (span <= split) a.n_splits = 1, split = span + 31;
   a.split = (uint32_t)split;

@@ -193,10 +193,12 @@ __device__ __forceinline__ v8s v_operand(const uint8_t *lv, int t, int d, int la
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Adds the infinite and NaN values of the keys [begin, end) to the rows that see them.  Tiles with a key that is hidden
-// from some row hold zeros in their place, as a hidden key's weight of zero
-// would make NaN of them; in other tiles the product took them already, and
-// adding them again changes nothing.
+// Adds the infinite and NaN values of the keys [begin, end) to the rows that
+// see them.  Tiles with a key that is hidden from some row hold zeros in their
+// place, as a hidden key's weight of zero would make NaN of them; in other
+// tiles the product took them already, and what is infinite or NaN stays so.
+// (There a probability that 16 bits round to 0 makes NaN of an infinite value,
+// where a tile with hidden keys gives the infinity.)
 template <class E, int DP>
 __device__ __forceinline__ void add_non_finite(const AttendArgs &a, const uint32_t *table, uint32_t kvh, uint32_t begin, uint32_t end,
                                                int first, int last, int half, v16f *o) {
@@ -419,10 +421,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
 // many loads are in flight and that each takes whole cache lines, past which
 // the caches are told not to keep them (an instruction reads whole rows of 2
 // to 8 keys).  A tile's keys, then its values pass through the same LDS.
-// 64 tokens over 1 to 8,192 cached ones, 1.15 GB: 200 us, 5.8 TB/s, where a
-// plain read of as much takes 174 (past the caches) to 195.  The whole call, 213
-// us, takes 239 with loads that the caches keep, 258 with 64 bytes of 16 rows an
-// instruction.
+// 64 tokens over 1 to 8,192 cached ones, 1.15 GB: 196 to 205 us, 5.6 to 5.9
+// TB/s, where a plain read of as much takes 174 (past the caches) to 195.  The
+// whole call takes 210 to 213 us, 239 with loads that the caches keep, 258
+// with 64 bytes of 16 rows an instruction.
 template <class E, int DP, int NB>
 __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 128 || NB > 1 ? 2 : 3) void k_attend_few(AttendArgs a) {
   typedef typename E::V V;
@@ -707,7 +709,7 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
 }
 
 // Joins the splits of one row: LQ lanes read one split's sums, 16 bytes each.
-// A launch of its own (4 to 8 us): with the last workgroup of a row's splits
+// A launch of its own (7 us at 9 to 257 splits): with the last workgroup of a row's splits
 // joining them, the fences that carry sums between XCDs made a token over
 // 1,000 cached ones 14 us instead of 7 + 4, a step of 64 sequences 820 instead
 // of 210.
@@ -784,7 +786,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, uint32_t tile
 }
 
 // The same for few splits and many rows: LQ lanes a row.  Seven chunks of up
-// to 300 tokens in three splits: 4.4 us, a workgroup a row 26.
+// to 300 tokens, 12 heads, in up to five splits: 4.3 to 5.1 us, a workgroup a row 26.
 constexpr uint32_t kShortSplits = 8;
 template <class E, int LQ>
 __global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_t tile_rows) {
@@ -830,7 +832,7 @@ __global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_
 }
 
 // Weights from stored scores: a thread sums four keys' weights over the rows.
-// 50 MB of scores and weights in 11 us; computing the scores again would read
+// 50 MB of scores and weights in 12 us; computing the scores again would read
 // half of the cache.
 __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
   __shared__ float z[kFewRows];
@@ -873,8 +875,8 @@ __global__ __launch_bounds__(256) void k_weights_stored(AttendArgs a) {
 // rows of the chunk pass by in tiles of 64 (32 where rows are long).  Every score costs an
 // exponential, a product and a sum, about 23 cycles of a SIMD for 64 scores,
 // against 16 for its matrix product: the vector unit bounds it.  2,048 tokens
-// of 32 heads over 32,768: 0.65 to 0.70 ms (32 keys a wave 0.80, tiles of 32
-// rows 0.70 to 0.75).
+// of 32 heads over 32,768: 0.60 to 0.65 ms (beside 0.65 to 0.70 in the same
+// runs: 32 keys a wave 0.80, tiles of 32 rows 0.70 to 0.75).
 // Where that gives too few workgroups the rows are split, and their sums are
 // added by another launch.
 struct AgainRows {

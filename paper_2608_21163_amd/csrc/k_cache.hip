@@ -40,8 +40,9 @@ __device__ __forceinline__ float part_scale(float m, float top) { return m == ne
 // 16 bytes of it, and a lane group runs its own softmax over every
 // (4 x groups)-th id; the groups are joined at the end.  Rows lie anywhere,
 // so the time is that of their bytes: 256 x 32 lists of 256 ids (1.09 GB)
-// 177 us, 6.1 TB/s; 8 x 32 lists of 100 take 6 us, launch and two dependent loads.
-// Few lists share a row, so nothing is gained by taking a head's lists together.
+// 178 us, 6.1 TB/s; 8 x 32 lists of 100 take 6 us, launch and two dependent loads.
+// Lists of a large pool that were found apart share few rows; where the heads of a
+// group name one list, each of them reads its rows, through the caches.
 template <class E, int DP>
 __global__ __launch_bounds__(256) void k_attend_ids(IdsArgs a) {
   constexpr int LPR = DP / 8, GROUPS = 64 / LPR, U = 4;
@@ -379,7 +380,7 @@ __device__ __forceinline__ void evict_tails(const EvictArgs &a, const EvictSeq &
 // Tables of up to kEvictSmall pages: every workgroup of a sequence takes all
 // its keys into LDS, finds the threshold by four passes of eight bits, and
 // moves its slice of the pages.  Finding it once per slice costs no launch.
-// 64 histories of 512 pages of 16, 8 heads: 12.6 us (17 MB), of which the moves
+// 64 histories of 512 pages of 16, 8 heads: 13 us (17 MB), of which the moves
 // take 4; a chain of dependent loads and about 30 barriers bounds it.
 __global__ __launch_bounds__(512) void k_evict_small(EvictArgs a) {
   extern __shared__ uint32_t keys[];

@@ -428,7 +428,9 @@ class Cache:
     Queries, results, new keys and values are (tokens, heads, head_dim), pages
     (pages, page_size, kv_heads, head_dim) views of any layout whose rows are
     contiguous and 16-byte aligned.  Ids, lengths and starts are 32-bit
-    integers; INVALID is -1 in an int32 tensor."""
+    integers; INVALID is -1 in an int32 tensor.  The operators serve: there is
+    no backward pass, and results carry no gradient, whatever the arguments
+    require."""
 
     def __init__(self, dtype: str = "bf16", q_heads: int = 32, kv_heads: int = 8, head_dim: int = 128, page_size: int = 16,
                  device: int = 0, stream: Optional[int] = None):
