@@ -370,6 +370,10 @@ __device__ __forceinline__ uint64_t rdlane64(uint64_t v, int l) {
 // gives every key its position in the merged order; keys at positions below
 // `keep` are written to the LDS scratch (ld, li: 64*N entries each) and read
 // back in order.  More than kBatchMax survivors take the sort-and-merge path.
+// A list may name an id twice (one that is rewritten while a reader loads
+// it is seen partly old and partly new): of equal new keys the first counts.
+// Two at one position would leave the next one unwritten, and what LDS
+// happens to hold there would become an id.
 constexpr int kBatchMax = 32;
 template <int N>
 __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N], float nd, uint32_t ni, int keep,
@@ -388,7 +392,14 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
   const uint64_t m = ballot(in);
   if (!m) return;
   if (popc(m) > kBatchMax) {
-    wave_merge_new<N>(cd, ci, in ? nd : finf(), in ? ni : kInvalid, keep);
+    uint64_t once = 0, left = m;
+    while (left) {
+      const int l = ffs64(left);
+      once |= 1ull << l;
+      left &= ~ballot(nk == rdlane64(nk, l));
+    }
+    const bool first = (once >> ln) & 1;
+    wave_merge_new<N>(cd, ci, first ? nd : finf(), first ? ni : kInvalid, keep);
     return;
   }
   uint32_t cnt[N];
@@ -398,8 +409,8 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
   uint64_t live = 0, mm = m;
   while (mm) {
     const int l = ffs64(mm);
-    mm &= mm - 1;
     const uint64_t xk = rdlane64(nk, l);
+    mm &= ~ballot(nk == xk);
     bool lt[N];
     int below = 0;
     bool dup = false;
