@@ -371,9 +371,10 @@ __device__ __forceinline__ uint64_t rdlane64(uint64_t v, int l) {
 // `keep` are written to the LDS scratch (ld, li: 64*N entries each) and read
 // back in order.  More than kBatchMax survivors take the sort-and-merge path.
 // A list may name an id twice (one that is rewritten while a reader loads
-// it is seen partly old and partly new): of equal new keys the first counts.
+// it is seen partly old and partly new): equal new keys take that path too.
 // Two at one position would leave the next one unwritten, and what LDS
-// happens to hold there would become an id.
+// happens to hold there would become an id.  (Looked for beside the loop's
+// chain: dropping them in it made the searches 7% slower.)
 constexpr int kBatchMax = 32;
 template <int N>
 __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N], float nd, uint32_t ni, int keep,
@@ -392,25 +393,19 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
   const uint64_t m = ballot(in);
   if (!m) return;
   if (popc(m) > kBatchMax) {
-    uint64_t once = 0, left = m;
-    while (left) {
-      const int l = ffs64(left);
-      once |= 1ull << l;
-      left &= ~ballot(nk == rdlane64(nk, l));
-    }
-    const bool first = (once >> ln) & 1;
-    wave_merge_new<N>(cd, ci, first ? nd : finf(), first ? ni : kInvalid, keep);
+    wave_merge_new<N>(cd, ci, in ? nd : finf(), in ? ni : kInvalid, keep);
     return;
   }
   uint32_t cnt[N];
 #pragma unroll
   for (int r = 0; r < N; r++) cnt[r] = 0;
   uint32_t ltc = 0, rk = 0;
-  uint64_t live = 0, mm = m;
+  uint64_t live = 0, mm = m, twice = 0;
   while (mm) {
     const int l = ffs64(mm);
     const uint64_t xk = rdlane64(nk, l);
-    mm &= ~ballot(nk == xk);
+    mm &= mm - 1;
+    twice |= ballot(nk == xk) ^ (1ull << l);
     bool lt[N];
     int below = 0;
     bool dup = false;
@@ -426,6 +421,10 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
     for (int r = 0; r < N; r++) cnt[r] += lt[r] ? 0u : 1u;
     rk += xk < nk ? 1u : 0u;
     ltc = ln == l ? (uint32_t)below : ltc;
+  }
+  if (twice) {
+    wave_merge_new<N>(cd, ci, in ? nd : finf(), in ? ni : kInvalid, keep);
+    return;
   }
 #pragma unroll
   for (int r = 0; r < N; r++) {
