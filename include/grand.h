@@ -375,6 +375,22 @@ typedef struct {
   int64_t page_stride, slot_stride, head_stride;
 } grand_pages;
 
+/* A pool held in 4 bits.  A row's blocks of 32 elements (the last may be
+ * shorter) are 16 bytes of codes each, rows side by side in `k` and `v`, and a
+ * scale byte s each in `k_scales` and `v_scales`.  A code is a sign (bit 3) and a
+ * magnitude of 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0 to 2), elements of even index in a
+ * byte's low half; an element is its code times 2^(s - 127).  Blocks with s
+ * above 252 (bf16) or 140 (fp16) count as NaN; values below the type's
+ * range are rounded to it.  Strides are in bytes: of codes multiples of 16 and
+ * rows aligned to 16, of scales any.  The four arrays may be one buffer's
+ * parts (rows whose scales follow their codes). */
+typedef struct {
+  uint8_t *k, *v, *k_scales, *v_scales;
+  uint32_t n_pages;
+  int64_t page_stride, slot_stride, head_stride;
+  int64_t scale_page_stride, scale_slot_stride, scale_head_stride;
+} grand_packed;
+
 /* Rows by (token, head). */
 typedef struct {
   void *p;
@@ -409,8 +425,10 @@ grand_status grand_cache_destroy(grand_cache *h);
 /* Waits for the old stream's work, as the workspaces are shared. */
 grand_status grand_cache_set_stream(grand_cache *h, void *stream);
 /* Waits for the stream and reports what kernels found wrong in device memory
- * since the last check: GRAND_E_ID (a page or slot id outside the pool) or
- * GRAND_E_ARG (lengths or chunk starts out of range), else GRAND_OK. */
+ * since the last check: GRAND_E_ID (a page or slot id, or an entry of a list of
+ * pages, outside the pool), GRAND_E_ARG (lengths, chunk starts or parents out of range, a page
+ * with more names than its count says) or GRAND_E_CAPACITY (a pool without
+ * enough free pages for grand_pages_grow), else GRAND_OK. */
 grand_status grand_cache_check(grand_cache *h);
 const char *grand_cache_last_error(const grand_cache *h);
 
@@ -446,6 +464,27 @@ grand_status grand_cache_attend(grand_cache *h, const grand_seqs *s, const grand
                                 float scale, int causal, uint32_t window, const grand_rows *out, float *lse,
                                 const grand_weights *weights_in, const grand_weights *weights_out);
 
+/* grand_cache_attend with first tokens that stay visible: beside its window
+ * (window > 0) a row sees the tokens j < sinks, as far as it would without a window. */
+grand_status grand_cache_attend_sinks(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_pages *pages,
+                                      float scale, int causal, uint32_t window, uint32_t sinks, const grand_rows *out, float *lse,
+                                      const grand_weights *weights_in, const grand_weights *weights_out);
+
+/* The same over packed pages (sinks may be 0): the attention over the values
+ * that the codes stand for.  A hidden token has no influence whatever its
+ * codes and scales are. */
+grand_status grand_cache_attend_packed(grand_cache *h, const grand_seqs *s, const grand_rows *q, const grand_packed *pages,
+                                       float scale, int causal, uint32_t window, uint32_t sinks, const grand_rows *out, float *lse,
+                                       const grand_weights *weights_in, const grand_weights *weights_out);
+
+/* grand_cache_append into packed pages.  A block's scale is the smallest power of
+ * two at which no element is 7 times it or more, from 2^-125 to 2^125 (bf16) or
+ * 2^-23 to 2^13 (fp16); its codes are the nearest to the elements, the even code on a
+ * tie, 6 at most.  A block that holds an infinity or NaN has scale 255 and codes of 0.
+ * Codes past head_dim are 0.  No two rows of codes or scales may share memory. */
+grand_status grand_cache_append_packed(grand_cache *h, const grand_seqs *s, const grand_rows *k, const grand_rows *v,
+                                       const grand_packed *pages);
+
 /* Attention of one token per sequence (n_seq rows) over listed slots: row
  * (b, query head h) over the k ids at ids + b * ids_seq_stride +
  * h * ids_head_stride, in any order; GRAND_INVALID entries are passed over,
@@ -461,6 +500,18 @@ grand_status grand_cache_attend_ids(grand_cache *h, uint32_t n_seq, const grand_
                                     const uint32_t *ids, uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride,
                                     float scale, const grand_rows *prior, const float *prior_lse,
                                     const grand_rows *out, float *lse);
+
+/* The same over packed pages. */
+grand_status grand_cache_attend_ids_packed(grand_cache *h, uint32_t n_seq, const grand_rows *q, const grand_packed *pages,
+                                           const uint32_t *ids, uint32_t k, int64_t ids_seq_stride, int64_t ids_head_stride,
+                                           float scale, const grand_rows *prior, const float *prior_lse, const grand_rows *out,
+                                           float *lse);
+
+/* The keys and values of listed slots of packed pages, as the cache holds them
+ * (an index of the keys takes them from here): rows n x kv_heads of the cache's
+ * type.  GRAND_INVALID entries give rows of zeros.  k or v may be null. */
+grand_status grand_packed_read(grand_cache *h, uint32_t n, const uint32_t *slots, const grand_packed *pages,
+                               const grand_rows *k, const grand_rows *v);
 
 /* Eviction by accumulated weight, in pages.  Of the n = ceil(lens[b] /
  * page_size) pages of sequence b stay: the first `sinks`, the last
@@ -480,6 +531,61 @@ grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t hea
                                const grand_weights *weights, const uint32_t *budget, uint32_t sinks, uint32_t recent,
                                uint32_t *out_table, const grand_weights *out_weights, uint32_t *out_lens,
                                uint32_t *freed, uint32_t *n_freed);
+
+/* Pages that sequences share.  refs: for every page of the pool the number of
+ * entries of page tables that name it (rows' first ceil(lens[b] / page_size)
+ * entries); a page with refs 0 is free.  The calls keep that so, on the GPU: a
+ * program forks, grows and drops sequences without waiting for it.  refs_out may
+ * be refs_in, and shares no memory with it otherwise.  Tables, lengths, counts and lists share no
+ * memory with each other.  Keys and values stay where they are, except where
+ * grand_pages_copy and grand_packed_copy move them, which is for each layer's pool.
+ * Of s only the table, lens, max_k, max_pages and n_seq are used. */
+
+/* New sequences that go on from others: row i of out_table (n_out x max_pages,
+ * packed) names the pages of row parents[i] and then GRAND_INVALID, out_lens[i] is its
+ * length, and their refs are counted.  A parent may be named often or never; GRAND_INVALID
+ * gives an empty sequence.  drop: the names in s's table are given up in the
+ * same call (a step of a beam).  out_table shares no memory with s's table. */
+grand_status grand_pages_fork(grand_cache *h, const grand_seqs *s, uint32_t n_out, const uint32_t *parents, int drop,
+                              uint32_t n_pages, const uint32_t *refs_in, uint32_t *refs_out, uint32_t *out_table,
+                              uint32_t *out_lens);
+
+/* Room for n_new[b] more tokens a sequence: s's table and lens are brought up to
+ * date in place (table and lens: the same memory as in s).  A sequence whose
+ * last page is partly filled and named elsewhere too gets a page of its
+ * own in its place, src[b] and dst[b] being the old page and the new one, else
+ * GRAND_INVALID: grand_pages_copy(n_seq, src, dst) then copies them.  Free
+ * pages are given out in ascending order, to the sequences in order and in a sequence to
+ * its tokens in order.  A sequence that needs more pages than are left stays as it was, and so does
+ * every later one that needs any (reported by grand_cache_check, and
+ * to be seen from lens); so does one whose tokens would not fit max_pages. */
+grand_status grand_pages_grow(grand_cache *h, const grand_seqs *s, const uint32_t *n_new, uint32_t n_pages, const uint32_t *refs_in,
+                              uint32_t *refs_out, uint32_t *table, uint32_t *lens, uint32_t *src, uint32_t *dst);
+
+/* Names given up: the entries of n_rows rows of ids (row_stride apart), the
+ * first counts[i] of each (counts null: `width`; tokens != 0: counts are
+ * tokens, and pages of page_size are meant), GRAND_INVALID entries passed over.  Rows are tables
+ * of sequences that have ended, or the freed pages of grand_cache_evict.  freed (min(n_pages,
+ * n_rows * width) entries): the pages that nothing names any more, ascending,
+ * then GRAND_INVALID; n_freed their number. */
+grand_status grand_pages_release(grand_cache *h, uint32_t n_rows, uint32_t width, const uint32_t *ids, int64_t row_stride,
+                                 const uint32_t *counts, int tokens, uint32_t n_pages, const uint32_t *refs_in, uint32_t *refs_out,
+                                 uint32_t *freed, uint32_t *n_freed);
+
+/* The pages in use become the pool's first: of n pages in use those with ids from n on
+ * move, in ascending order, to the free ids below n, in ascending order.  src and dst (n_pages entries):
+ * from where to where, then GRAND_INVALID (grand_pages_copy moves the data); n_moves their
+ * number.  out_table (n_seq x max_pages, packed; or s's table itself, with its stride): the
+ * table with the new ids, and where it is not s's own GRAND_INVALID after each row's pages.
+ * s names every sequence that has pages. */
+grand_status grand_pages_compact(grand_cache *h, const grand_seqs *s, uint32_t n_pages, const uint32_t *refs_in, uint32_t *refs_out,
+                                 uint32_t *out_table, uint32_t *src, uint32_t *dst, uint32_t *n_moves);
+
+/* Copies keys and values of page src[i] to page dst[i], all slots, i < n; entries with
+ * GRAND_INVALID in either are passed over.  A page that is named in dst is named there
+ * once, and not in src. */
+grand_status grand_pages_copy(grand_cache *h, uint32_t n, const uint32_t *src, const uint32_t *dst, const grand_pages *pages);
+grand_status grand_packed_copy(grand_cache *h, uint32_t n, const uint32_t *src, const uint32_t *dst, const grand_packed *pages);
 
 #ifdef __cplusplus
 }

@@ -9,10 +9,10 @@ namespace gr {
 
 // What a kernel found wrong in device-resident arguments; grand_cache_check
 // reports it.  Nothing is read or written out of bounds because of it.
-enum { kCacheOk = 0, kCachePage = 1, kCacheLen = 2, kCacheStart = 3, kCacheId = 4 };
+enum { kCacheOk = 0, kCachePage = 1, kCacheLen = 2, kCacheStart = 3, kCacheId = 4, kCacheParent = 5, kCacheFull = 6, kCacheRefs = 7, kCacheList = 8 };
 struct CacheErr {
   uint32_t code;
-  uint32_t where;  // the sequence (or list) it was found in
+  uint32_t where;  // the sequence (list, page) it was found in
 };
 __device__ __forceinline__ void cache_err(CacheErr *e, uint32_t code, uint32_t where) {
   if (atomicCAS(&e->code, (uint32_t)kCacheOk, code) == kCacheOk) e->where = where;
@@ -24,6 +24,12 @@ struct PagesView {
   uint32_t n_pages;
   uint32_t shift;            // log2 of the page size
   uint64_t bytes;            // up to the last page's last row
+};
+
+// Scales of packed pages: bytes, strides in bytes; k null: the pages are not packed.
+struct ScalesView {
+  const uint8_t *k, *v;
+  uint32_t page, slot, head;
 };
 
 struct SeqsView {
@@ -47,6 +53,7 @@ struct WeightsView {
 struct AttendArgs {
   SeqsView s;
   PagesView pg;
+  ScalesView sc;
   RowsView q, out;
   float *lse;                // n_tokens x q_heads, may be null
   WeightsView win, wout;     // wout.p null: no weights
@@ -54,6 +61,8 @@ struct AttendArgs {
   float c;                   // scale * log2(e)
   uint32_t window;           // keys a row sees, its own included; 0: all; below 2^31
   int causal;
+  uint32_t sinks;            // first tokens that rows see beside their window (0 without one)
+  uint32_t sink_keys;        // that rounded up to whole tiles
   // plan
   uint32_t row_tiles;        // row tiles of the longest chunk
   uint32_t split;            // keys of one split (a multiple of the keys a workgroup takes at once)
@@ -70,6 +79,7 @@ struct AttendArgs {
 
 struct IdsArgs {
   PagesView pg;
+  ScalesView sc;
   RowsView q, out, prior;    // prior.p null: none
   const float *prior_lse;
   float *lse;
@@ -83,8 +93,10 @@ struct IdsArgs {
 struct AppendArgs {
   SeqsView s;
   PagesView pg;
+  ScalesView sc;
   RowsView k, v;
   uint32_t kv_heads, dim;
+  bool f16;                  // packed pages: what the rows hold
   CacheErr *err;
 };
 
@@ -109,6 +121,62 @@ struct EvictArgs {
   CacheErr *err;
 };
 
+struct ReadArgs {
+  PagesView pg;
+  ScalesView sc;
+  RowsView k, v;             // p null: not wanted
+  const uint32_t *slots;
+  uint32_t n, kv_heads, dim;
+  bool f16;
+  CacheErr *err;
+};
+
+// Page handling.  refs_in and refs_out may be the same memory.
+struct RefArgs {
+  SeqsView s;                // the old sequences
+  uint32_t shift, n_pages;
+  const uint32_t *refs_in;
+  uint32_t *refs_out;
+  // fork
+  const uint32_t *parents;
+  uint32_t n_out;
+  int drop;
+  uint32_t *out_table, *out_lens;
+  int64_t out_stride;        // of out_table's rows
+  // grow
+  const uint32_t *n_new;
+  uint32_t *lens;
+  // grow: by sequence; compact: lists of n_pages
+  uint32_t *src, *dst;
+  // release
+  const uint32_t *ids, *counts;
+  int64_t row_stride;
+  uint32_t n_rows, width, cap;
+  int tokens;
+  uint32_t *freed, *n_freed; // compact: n_freed counts its moves
+  // workspace
+  uint32_t *count;           // release: names given up, by page
+  uint64_t *bits;            // a bit a page: free (grow), in use (compact), freed (release)
+  uint32_t *blk;             // set bits by block of kRefPages pages
+  uint32_t *rank, *total;    // compact: a moving page's place in the lists; pages in use
+  uint32_t *need;            // grow: pages a sequence needs, bit 31: one of them for a copy
+  uint64_t *start;           // grow: pages that the sequences before it need
+  CacheErr *err;
+};
+constexpr uint32_t kRefPages = 2048;  // pages of a workgroup
+
+struct CopyArgs {
+  PagesView pg;
+  ScalesView sc;
+  const uint32_t *src, *dst;
+  uint32_t n;
+  uint32_t row, slots, heads;      // bytes of a head's row, slots of a page
+  bool flat;                       // a page's rows lie side by side
+  uint32_t scale_row;
+  uint32_t pieces;                 // of 16 bytes, of a page's keys
+  CacheErr *err;
+};
+
 // Pages: tables up to kEvictSmall are handled by one launch whose workgroups
 // all find the threshold (8 x 8,000 pages of 16: 36 us, by tiles 44; 8 x 16,000:
 // 62 and 51).
@@ -117,9 +185,24 @@ constexpr uint32_t kEvictSmall = 8192, kEvictTile = 2048;
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.
 constexpr uint32_t kFewRows = 32, kManyRows = 128;
+// keys of a tile of many rows
+constexpr uint32_t rows_tile(uint32_t dim) { return dim > 128 ? 32 : 64; }
 constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again
 constexpr uint32_t kKeysStep = 128;  // keys that a workgroup of few rows takes at once (four waves of 32)
 
+// (16-bit pages without first tokens; the others are called from there)
+hipError_t launch_attend_sinks(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);
+hipError_t launch_attend_packed(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);
+hipError_t launch_weights_sinks(bool f16, const AttendArgs &a, hipStream_t st);
+hipError_t launch_weights_packed(bool f16, const AttendArgs &a, hipStream_t st);
+hipError_t launch_ids_packed(bool f16, const IdsArgs &a, hipStream_t st);
+hipError_t launch_append_packed(const AppendArgs &a, hipStream_t st);
+hipError_t launch_read(const ReadArgs &a, hipStream_t st);
+hipError_t launch_fork(const RefArgs &a, hipStream_t st);
+hipError_t launch_grow(const RefArgs &a, hipStream_t st);
+hipError_t launch_release(const RefArgs &a, hipStream_t st);
+hipError_t launch_compact(const RefArgs &a, hipStream_t st);
+hipError_t launch_copy(const CopyArgs &a, hipStream_t st);
 hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipStream_t st);
 hipError_t launch_attend_join(bool f16, const AttendArgs &a, uint32_t tile_rows, hipStream_t st);
 hipError_t launch_attend_weights(bool f16, const AttendArgs &a, hipStream_t st);

@@ -600,10 +600,12 @@ hipError_t ids_type(const IdsArgs &a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_attend_ids(bool f16, const IdsArgs &a, hipStream_t st) {
+  if (a.sc.k) return launch_ids_packed(f16, a, st);
   return f16 ? ids_type<F16>(a, st) : ids_type<Bf16>(a, st);
 }
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
+  if (a.sc.k) return launch_append_packed(a, st);
   const uint64_t n = (uint64_t)a.s.max_q * a.kv_heads * (a.dim / 8);
   k_append<<<dim3((uint32_t)((n + 255) / 256), a.s.n_seq), 256, 0, st>>>(a);
   return hipGetLastError();

@@ -1,0 +1,461 @@
+// k_pages.hip -- pages that sequences share: counts of the table entries that
+// name a page (0: free), kept on the GPU.  Which free page goes where, and
+// the order of lists, follow from ranks among the pages' bits in ascending order,
+// never from the order in which workgroups run.  Integer atomics count
+// names; their order does not show.  Pools of 10,000s of pages and tables of 100s of rows are
+// a few hundred KB: what counts is the number of launches that depend on one
+// another.
+#include "cache.h"
+#include "wave.h"
+
+namespace gr {
+namespace {
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+constexpr uint32_t kOneCopy = 0x80000000u;
+
+// Entries of a sequence's row.
+__device__ __forceinline__ uint32_t row_pages(const RefArgs &a, uint32_t b, uint32_t &len) {
+  len = a.s.lens[b];
+  if (len > a.s.max_k) {
+    cache_err(a.err, kCacheLen, b);
+    len = a.s.max_k;
+  }
+  return (uint32_t)(((uint64_t)len + (1u << a.shift) - 1) >> a.shift);
+}
+
+__global__ __launch_bounds__(256) void k_copy_refs(RefArgs a) {
+  const uint64_t p = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (p < a.n_pages) a.refs_out[p] = a.refs_in[p];
+}
+
+// A workgroup per 256 entries of a new row (or, behind those, of an old one
+// whose names are dropped).
+__global__ __launch_bounds__(256) void k_fork(RefArgs a) {
+  const uint32_t chunks = max((a.s.max_pages + 255) / 256, 1u), row = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
+  uint32_t b = row - a.n_out, len = 0, n = 0;
+  const bool fresh = row < a.n_out;
+  if (fresh) {
+    b = a.parents[row];
+    if (b != kInvalid && b >= a.s.n_seq) cache_err(a.err, kCacheParent, row);
+    if (b < a.s.n_seq) n = row_pages(a, b, len);
+    if (i == 0) a.out_lens[row] = len;
+  } else {
+    n = row_pages(a, b, len);
+  }
+  const uint32_t id = i < n ? a.s.table[(int64_t)b * a.s.table_stride + i] : kInvalid;
+  if (fresh && i < a.s.max_pages) a.out_table[(int64_t)row * a.out_stride + i] = id;
+  if (i >= n) return;
+  if (id >= a.n_pages) cache_err(a.err, kCachePage, b);
+  else atomicAdd(&a.refs_out[id], fresh ? 1u : 0xFFFFFFFFu);
+}
+
+// A thread's eight pages of a workgroup's 2,048 are 256 apart, so that a wave's
+// ballot is a word of the bits.  The workgroup's number of set bits goes to blk.
+template <class F>
+__device__ __forceinline__ void block_bits(const RefArgs &a, uint32_t blk, F set) {
+  __shared__ uint32_t sum[4];
+  const uint32_t t = threadIdx.x;
+  uint32_t n = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kRefPages / 256; i++) {
+    const uint64_t p = (uint64_t)blk * kRefPages + i * 256 + t;
+    const uint64_t m = ballot(p < a.n_pages && set((uint32_t)p));
+    if (t % 64 == 0 && p < a.n_pages) a.bits[p / 64] = m;
+    n += popc(m);
+  }
+  if (t % 64 == 0) sum[t / 64] = n;
+  __syncthreads();
+  if (t == 0) a.blk[blk] = sum[0] + sum[1] + sum[2] + sum[3];
+}
+
+// Sums of blk[0 .. n) before and in all, by a workgroup of 256.
+__device__ __forceinline__ void blk_sums(const RefArgs &a, uint32_t n, uint32_t before, uint32_t &sum_before, uint32_t &sum_all) {
+  __shared__ uint32_t tmp[4][2];
+  const uint32_t t = threadIdx.x;
+  uint32_t x = 0, y = 0;
+  for (uint32_t i = t; i < n; i += 256) {
+    const uint32_t c = a.blk[i];
+    y += c;
+    if (i < before) x += c;
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) {
+    x += (uint32_t)__shfl_xor((int)x, j, 64);
+    y += (uint32_t)__shfl_xor((int)y, j, 64);
+  }
+  if (t % 64 == 0) tmp[t / 64][0] = x, tmp[t / 64][1] = y;
+  __syncthreads();
+  sum_before = tmp[0][0] + tmp[1][0] + tmp[2][0] + tmp[3][0];
+  sum_all = tmp[0][1] + tmp[1][1] + tmp[2][1] + tmp[3][1];
+  __syncthreads();
+}
+
+// Calls f(page, is its bit set, set bits of the workgroup before it) for every page
+// of a workgroup.  The 32 words' counts are summed up by one wave.
+template <class F>
+__device__ __forceinline__ void each_bit(const RefArgs &a, uint32_t blk, F f) {
+  __shared__ uint32_t before[kRefPages / 64];
+  const uint32_t t = threadIdx.x, words = kRefPages / 64;
+  if (t < 64) {
+    const uint64_t w = (uint64_t)blk * words + t;
+    uint32_t n = t < words && w * 64 < a.n_pages ? popc(a.bits[w]) : 0, s = n;
+#pragma unroll
+    for (int j = 1; j < 64; j <<= 1) {
+      const uint32_t x = (uint32_t)__shfl_up((int)s, j, 64);
+      if ((int)t >= j) s += x;
+    }
+    if (t < words) before[t] = s - n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < kRefPages / 256; i++) {
+    const uint64_t p = (uint64_t)blk * kRefPages + i * 256 + t;
+    if (p < a.n_pages) {
+      const uint64_t m = a.bits[p / 64];
+      f((uint32_t)p, (bool)(m >> (p % 64) & 1), before[(i * 256 + t) / 64] + popc(m & ((1ull << (p % 64)) - 1)));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- grow
+struct GrowSeq {
+  uint32_t len, n0, n1;  // tokens, pages before and after
+  bool fits;
+};
+__device__ __forceinline__ GrowSeq grow_seq(const RefArgs &a, uint32_t b) {
+  GrowSeq g;
+  g.n0 = row_pages(a, b, g.len);
+  const uint64_t after = (uint64_t)g.len + a.n_new[b];
+  g.fits = (after + (1u << a.shift) - 1) >> a.shift <= a.s.max_pages && after <= 0xFFFFFFFFull;
+  g.n1 = g.fits ? (uint32_t)((after + (1u << a.shift) - 1) >> a.shift) : g.n0;
+  return g;
+}
+
+// Free pages, and the pages that sequences need.
+__global__ __launch_bounds__(256) void k_grow_need(RefArgs a) {
+  const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + kRefPages - 1) / kRefPages);
+  if (blockIdx.x < blocks) {
+    block_bits(a, blockIdx.x, [&](uint32_t p) {
+      const uint32_t r = a.refs_in[p];
+      if (a.refs_out != a.refs_in) a.refs_out[p] = r;
+      return r == 0;
+    });
+    return;
+  }
+  const uint32_t b = (blockIdx.x - blocks) * 256 + threadIdx.x;
+  if (b >= a.s.n_seq) return;
+  const GrowSeq g = grow_seq(a, b);
+  if (!g.fits) cache_err(a.err, kCacheLen, b);
+  uint32_t need = g.n1 - g.n0;
+  if (g.fits && a.n_new[b] && (g.len & ((1u << a.shift) - 1))) {
+    const uint32_t id = a.s.table[(int64_t)b * a.s.table_stride + g.n0 - 1];
+    if (id >= a.n_pages) cache_err(a.err, kCachePage, b);
+    else if (a.refs_in[id] > 1) need = (need + 1) | kOneCopy;
+  }
+  a.need[b] = need;
+}
+
+// Where each sequence's pages begin among the free ones.
+__global__ __launch_bounds__(1024) void k_grow_start(RefArgs a) {
+  __shared__ uint64_t sum[16];
+  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  uint64_t base = 0;
+  for (uint32_t b0 = 0; b0 < a.s.n_seq; b0 += 1024) {
+    const uint32_t b = b0 + t;
+    const uint64_t n = b < a.s.n_seq ? a.need[b] & ~kOneCopy : 0;
+    uint64_t s = n;
+#pragma unroll
+    for (int j = 1; j < 64; j <<= 1) {
+      const uint64_t x = __shfl_up((unsigned long long)s, j, 64);
+      if ((int)lane >= j) s += x;
+    }
+    if (lane == 63) sum[wave] = s;
+    __syncthreads();
+    uint64_t before = base;
+    for (uint32_t w = 0; w < 16; w++) {
+      if (w < wave) before += sum[w];
+      base += sum[w];
+    }
+    if (b < a.s.n_seq) a.start[b] = before + s - n;
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(256) void k_grow_give(RefArgs a) {
+  const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + kRefPages - 1) / kRefPages);
+  uint32_t before, all;
+  blk_sums(a, blocks, min(blockIdx.x, blocks), before, all);
+  uint32_t *table = a.out_table;
+  if (blockIdx.x < blocks) {
+    const uint64_t wanted = a.start[a.s.n_seq - 1] + (a.need[a.s.n_seq - 1] & ~kOneCopy);
+    if (before >= wanted) return;
+    each_bit(a, blockIdx.x, [&](uint32_t p, bool free, uint32_t rank) {
+      const uint64_t r = before + rank;
+      if (!free || r >= wanted) return;
+      // the last sequence that starts at r or before it
+      uint32_t lo = 0, hi = a.s.n_seq;
+      while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (a.start[mid] <= r) lo = mid;
+        else hi = mid;
+      }
+      const uint32_t b = lo, need = a.need[b];
+      if (a.start[b] + (need & ~kOneCopy) > all) return;
+      const uint32_t j = (uint32_t)(r - a.start[b]);
+      uint32_t n0 = (uint32_t)(((uint64_t)min(a.s.lens[b], a.s.max_k) + (1u << a.shift) - 1) >> a.shift);
+      if (need & kOneCopy) {
+        n0--;
+        // (the page before it is left by its thread below, which reads it first)
+        if (j == 0) {
+          a.dst[b] = p;
+          a.refs_out[p] = 1;
+          return;
+        }
+      }
+      a.refs_out[p] = 1;
+      table[(int64_t)b * a.s.table_stride + n0 + j] = p;
+    });
+    return;
+  }
+  const uint32_t b = (blockIdx.x - blocks) * 256 + threadIdx.x;
+  if (b >= a.s.n_seq) return;
+  const uint32_t need = a.need[b];
+  const bool served = (need & ~kOneCopy) == 0 || a.start[b] + (need & ~kOneCopy) <= all;
+  if (!served) cache_err(a.err, kCacheFull, b);
+  uint32_t from = kInvalid;
+  if (served && (need & kOneCopy)) {
+    const uint32_t n0 = (uint32_t)(((uint64_t)min(a.s.lens[b], a.s.max_k) + (1u << a.shift) - 1) >> a.shift);
+    from = a.s.table[(int64_t)b * a.s.table_stride + n0 - 1];
+    atomicSub(&a.refs_out[from], 1u);
+  } else {
+    a.dst[b] = kInvalid;
+  }
+  a.src[b] = from;
+}
+
+// The last step, once every page is given: copies' places in the table, lengths.
+__global__ __launch_bounds__(256) void k_grow_end(RefArgs a) {
+  const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + kRefPages - 1) / kRefPages);
+  uint32_t before, all;
+  blk_sums(a, blocks, 0, before, all);
+  const uint32_t b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.s.n_seq) return;
+  const uint32_t need = a.need[b];
+  const bool served = (need & ~kOneCopy) == 0 || a.start[b] + (need & ~kOneCopy) <= all;
+  if (!served) return;
+  const GrowSeq g = grow_seq(a, b);
+  if (need & kOneCopy) a.out_table[(int64_t)b * a.s.table_stride + g.n0 - 1] = a.dst[b];
+  if (g.fits) a.lens[b] = g.len + a.n_new[b];
+}
+
+// ---------------------------------------------------------------- release
+__global__ __launch_bounds__(256) void k_release_clear(RefArgs a) {
+  const uint64_t p = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (p < a.n_pages) a.count[p] = 0;
+}
+
+__global__ __launch_bounds__(256) void k_release_count(RefArgs a) {
+  const uint32_t chunks = (a.width + 255) / 256, row = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
+  uint32_t n = a.width;
+  if (a.counts) {
+    uint64_t c = a.counts[row];
+    if (a.tokens) c = (c + (1u << a.shift) - 1) >> a.shift;
+    if (c > a.width) {
+      cache_err(a.err, kCacheLen, row);
+      c = a.width;
+    }
+    n = (uint32_t)c;
+  }
+  if (i >= n) return;
+  const uint32_t id = a.ids[(int64_t)row * a.row_stride + i];
+  if (id == kInvalid) return;
+  if (id >= a.n_pages) cache_err(a.err, kCachePage, row);
+  else atomicAdd(&a.count[id], 1u);
+}
+
+__global__ __launch_bounds__(256) void k_release_refs(RefArgs a) {
+  block_bits(a, blockIdx.x, [&](uint32_t p) {
+    const uint32_t old = a.refs_in[p], gone = a.count[p];
+    if (gone > old) cache_err(a.err, kCacheRefs, p);
+    a.refs_out[p] = old - min(gone, old);
+    return old && gone >= old;
+  });
+}
+
+__global__ __launch_bounds__(256) void k_release_list(RefArgs a) {
+  uint32_t before, all;
+  blk_sums(a, gridDim.x, blockIdx.x, before, all);
+  each_bit(a, blockIdx.x, [&](uint32_t p, bool freed, uint32_t rank) {
+    if (freed) a.freed[before + rank] = p;
+    if (p >= all && p < a.cap) a.freed[p] = kInvalid;
+  });
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_freed = all;
+}
+
+// ---------------------------------------------------------------- compact
+__global__ __launch_bounds__(256) void k_compact_bits(RefArgs a) {
+  block_bits(a, blockIdx.x, [&](uint32_t p) { return a.refs_in[p] != 0; });
+}
+
+// Set bits before page n.
+__device__ __forceinline__ uint32_t bits_before(const RefArgs &a, uint32_t blocks, uint32_t n) {
+  __shared__ uint32_t tmp[4];
+  uint32_t before, all;
+  blk_sums(a, blocks, n / kRefPages, before, all);
+  uint32_t x = 0;
+  const uint32_t t = threadIdx.x, from = n / kRefPages * kRefPages;
+  if (from + t * 64 < n) {
+    const uint64_t m = a.bits[(from + t * 64) / 64];
+    const uint32_t left = n - (from + t * 64);
+    x = popc(left >= 64 ? m : m & ((1ull << left) - 1));
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) x += (uint32_t)__shfl_xor((int)x, j, 64);
+  if (t % 64 == 0) tmp[t / 64] = x;
+  __syncthreads();
+  return before + tmp[0] + tmp[1] + tmp[2] + tmp[3];
+}
+
+__global__ __launch_bounds__(256) void k_compact_lists(RefArgs a) {
+  uint32_t before, live;
+  blk_sums(a, gridDim.x, blockIdx.x, before, live);
+  const uint32_t front = bits_before(a, gridDim.x, live), moves = live - front;
+  each_bit(a, blockIdx.x, [&](uint32_t p, bool used, uint32_t rank) {
+    rank += before;
+    if (used && p >= live) {
+      a.src[rank - front] = p;
+      a.rank[p] = rank - front;
+    }
+    if (!used && p < live) a.dst[p - rank] = p;
+    if (p >= moves) a.src[p] = a.dst[p] = kInvalid;
+    if (a.refs_out != a.refs_in) a.refs_out[p] = a.refs_in[p];
+  });
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_freed = moves, *a.total = live;
+}
+
+// Counts move with their pages, and the tables get the new ids.
+__global__ __launch_bounds__(256) void k_compact_apply(RefArgs a) {
+  const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + 255) / 256);
+  if (blockIdx.x < blocks) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= *a.n_freed) return;
+    const uint32_t s = a.src[i], d = a.dst[i];
+    a.refs_out[d] = a.refs_in[s];
+    a.refs_out[s] = 0;
+    return;
+  }
+  const uint32_t chunks = (a.s.max_pages + 255) / 256, x = blockIdx.x - blocks, b = x / chunks, i = x % chunks * 256 + threadIdx.x;
+  uint32_t len;
+  const uint32_t n = row_pages(a, b, len);
+  if (i >= a.s.max_pages) return;
+  uint32_t *to = a.out_table + (int64_t)b * a.out_stride + i;
+  if (i >= n) {
+    if (a.out_table != a.s.table) *to = kInvalid;
+    return;
+  }
+  uint32_t id = a.s.table[(int64_t)b * a.s.table_stride + i];
+  if (id >= a.n_pages) {
+    cache_err(a.err, kCachePage, b);
+  } else if (!(a.bits[id / 64] >> (id % 64) & 1)) {
+    cache_err(a.err, kCacheRefs, id);  // named, though its count is 0
+  } else {
+    if (id >= *a.total) id = a.dst[a.rank[id]];
+  }
+  *to = id;
+}
+
+// ---------------------------------------------------------------- copies
+// 16 bytes a thread and step, keys first, then values; small pages share a
+// workgroup, large ones are several workgroups'.
+__global__ __launch_bounds__(256) void k_copy_pages(CopyArgs a, uint32_t per, uint32_t chunks) {
+  const uint32_t both = 2 * a.pieces, t = threadIdx.x;
+  const uint64_t wg = blockIdx.x;
+  const uint64_t i = per > 1 ? wg * per + t / both : wg / chunks;
+  if (i >= a.n || (per > 1 && t >= per * both)) return;
+  const uint32_t s = a.src[i], d = a.dst[i];
+  if (s == kInvalid || d == kInvalid) return;
+  if (s >= a.pg.n_pages || d >= a.pg.n_pages) {
+    cache_err(a.err, kCacheList, (uint32_t)i);
+    return;
+  }
+  const uint64_t from = (uint64_t)s * a.pg.page, to = (uint64_t)d * a.pg.page;
+  const uint32_t first = per > 1 ? t % both : wg % chunks * 1024 + t;
+  v4u x[4];
+  uint64_t at[4];
+  uint32_t n = 0;
+  const uint32_t most = per > 1 ? 1 : 4, line = a.row / 16;
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) {
+    const uint32_t y = first + j * 256;
+    if (j < most && y < both) {
+      const uint32_t z = y < a.pieces ? y : y - a.pieces;
+      at[j] = a.flat ? z * 16u : (uint64_t)(z / line / a.heads) * a.pg.slot + (uint64_t)(z / line % a.heads) * a.pg.head + z % line * 16;
+      x[j] = *(const v4u *)((y < a.pieces ? a.pg.k : a.pg.v) + from + at[j]);
+      n = j + 1;
+    }
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++)
+    if (j < n) *(v4u *)(const_cast<uint8_t *>(first + j * 256 < a.pieces ? a.pg.k : a.pg.v) + to + at[j]) = x[j];
+  if (!a.sc.k) return;
+  // scales: the entry's first threads, a byte at a time
+  const uint32_t bytes = a.slots * a.heads * a.scale_row, step = per > 1 ? both : 256;
+  if (per == 1 && wg % chunks) return;
+  for (uint32_t y = per > 1 ? t % both : t; y < bytes; y += step) {
+    const uint32_t r = y / a.scale_row;
+    const uint64_t off = (uint64_t)(r / a.heads) * a.sc.slot + (uint64_t)(r % a.heads) * a.sc.head + y % a.scale_row;
+    const_cast<uint8_t *>(a.sc.k)[(uint64_t)d * a.sc.page + off] = a.sc.k[(uint64_t)s * a.sc.page + off];
+    const_cast<uint8_t *>(a.sc.v)[(uint64_t)d * a.sc.page + off] = a.sc.v[(uint64_t)s * a.sc.page + off];
+  }
+}
+
+}  // namespace
+
+static uint32_t groups(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 1) / per); }
+
+hipError_t launch_fork(const RefArgs &a, hipStream_t st) {
+  if (a.refs_out != a.refs_in) k_copy_refs<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
+  const uint32_t chunks = a.s.max_pages ? groups(a.s.max_pages, 256) : 1, rows = a.n_out + (a.drop ? a.s.n_seq : 0);
+  if (rows) k_fork<<<chunks * rows, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_grow(const RefArgs &a, hipStream_t st) {
+  const uint32_t blocks = groups(a.n_pages, kRefPages), seqs = groups(a.s.n_seq, 256);
+  if (!a.s.n_seq) {
+    if (a.refs_out != a.refs_in) k_copy_refs<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  k_grow_need<<<blocks + seqs, 256, 0, st>>>(a);
+  k_grow_start<<<1, 1024, 0, st>>>(a);
+  k_grow_give<<<blocks + seqs, 256, 0, st>>>(a);
+  k_grow_end<<<seqs, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_release(const RefArgs &a, hipStream_t st) {
+  const uint32_t blocks = groups(a.n_pages, kRefPages);
+  k_release_clear<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
+  if (a.n_rows && a.width) k_release_count<<<groups(a.width, 256) * a.n_rows, 256, 0, st>>>(a);
+  k_release_refs<<<blocks, 256, 0, st>>>(a);
+  k_release_list<<<blocks, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const RefArgs &a, hipStream_t st) {
+  const uint32_t blocks = groups(a.n_pages, kRefPages);
+  k_compact_bits<<<blocks, 256, 0, st>>>(a);
+  k_compact_lists<<<blocks, 256, 0, st>>>(a);
+  k_compact_apply<<<groups(a.n_pages, 256) + groups(a.s.max_pages, 256) * a.s.n_seq, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_copy(const CopyArgs &a, hipStream_t st) {
+  const uint32_t both = 2 * a.pieces, per = both < 256 ? 256 / both : 1, chunks = per > 1 ? 1 : groups(both, 1024);
+  const uint64_t wgs = per > 1 ? groups(a.n, per) : (uint64_t)a.n * chunks;
+  k_copy_pages<<<(uint32_t)wgs, 256, 0, st>>>(a, per, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace gr

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import Any, NamedTuple, Optional
 
 import numpy as np
 
@@ -36,7 +36,10 @@ EXPORTED = ["grand_default_params", "grand_create", "grand_destroy", "grand_set_
             "grand_reader_search", "grand_reader_destroy", "grand_reader_last_error", "grand_export_graph", "grand_import_graph", "grand_set_timing",
             "grand_set_counting", "grand_stats", "grand_reset_stats", "grand_last_error",
             "grand_default_cache_params", "grand_cache_create", "grand_cache_destroy", "grand_cache_set_stream", "grand_cache_check",
-            "grand_cache_last_error", "grand_cache_append", "grand_cache_attend", "grand_cache_attend_ids", "grand_cache_evict"]
+            "grand_cache_last_error", "grand_cache_append", "grand_cache_attend", "grand_cache_attend_ids", "grand_cache_evict",
+            "grand_cache_append_packed", "grand_cache_attend_sinks", "grand_cache_attend_packed", "grand_cache_attend_ids_packed",
+            "grand_packed_read", "grand_packed_copy", "grand_pages_fork", "grand_pages_grow", "grand_pages_release", "grand_pages_compact",
+            "grand_pages_copy"]
 
 
 class GrandError(RuntimeError):
@@ -78,6 +81,12 @@ class CacheParams(ctypes.Structure):
 class Pages(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_uint32),
                 ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class PackedPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_uint32), ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("scale_page_stride", ctypes.c_int64), ("scale_slot_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
 
 
 class Rows(ctypes.Structure):
@@ -151,6 +160,17 @@ def load_library(path: str = LIB_PATH):
     lib.grand_cache_attend.argtypes = [P, P, P, P, F, I32, U32, P, P, P, P]
     lib.grand_cache_attend_ids.argtypes = [P, U32, P, P, P, U32, I64, I64, F, P, P, P, P]
     lib.grand_cache_evict.argtypes = [P, P, U32, U32, P, P, U32, U32, P, P, P, P, P]
+    lib.grand_cache_append_packed.argtypes = [P, P, P, P, P]
+    lib.grand_cache_attend_sinks.argtypes = [P, P, P, P, F, I32, U32, U32, P, P, P, P]
+    lib.grand_cache_attend_packed.argtypes = [P, P, P, P, F, I32, U32, U32, P, P, P, P]
+    lib.grand_cache_attend_ids_packed.argtypes = [P, U32, P, P, P, U32, I64, I64, F, P, P, P, P]
+    lib.grand_packed_read.argtypes = [P, U32, P, P, P, P]
+    lib.grand_packed_copy.argtypes = [P, U32, P, P, P]
+    lib.grand_pages_fork.argtypes = [P, P, U32, P, I32, U32, P, P, P, P]
+    lib.grand_pages_grow.argtypes = [P, P, P, U32, P, P, P, P, P, P]
+    lib.grand_pages_release.argtypes = [P, U32, U32, P, I64, P, I32, U32, P, P, P, P]
+    lib.grand_pages_compact.argtypes = [P, P, U32, P, P, P, P, P, P]
+    lib.grand_pages_copy.argtypes = [P, U32, P, P, P]
     for name in EXPORTED:
         if name not in ("grand_default_params", "grand_last_error", "grand_reader_last_error",
                         "grand_default_cache_params", "grand_cache_last_error"):
@@ -418,6 +438,15 @@ class Sequences:
         self.ref = ctypes.byref(self.c)
 
 
+class Packed(NamedTuple):
+    """Keys or values of a pool held in 4 bits (grand_packed): codes (pages,
+    page_size, kv_heads, 16 * blocks) and scales (pages, page_size, kv_heads,
+    blocks), uint8 views of any layout whose last axis is contiguous, rows of codes aligned to
+    16 bytes; blocks = ceil(head_dim / 32)."""
+    codes: Any
+    scales: Any
+
+
 class Cache:
     """The key/value-cache operators on one GPU (grand_cache_create ...
     grand_cache_destroy).  Every tensor is a torch tensor of that GPU; the
@@ -427,7 +456,7 @@ class Cache:
 
     Queries, results, new keys and values are (tokens, heads, head_dim), pages
     (pages, page_size, kv_heads, head_dim) views of any layout whose rows are
-    contiguous and 16-byte aligned.  Ids, lengths and starts are 32-bit
+    contiguous and 16-byte aligned, or two Packed.  Ids, lengths and starts are 32-bit
     integers; INVALID is -1 in an int32 tensor.  The operators serve: there is
     no backward pass, and results carry no gradient, whatever the arguments
     require."""
@@ -455,10 +484,12 @@ class Cache:
         self._own_stream(stream)
         self._q, self._kv, self._dim, self._page = q_heads, kv_heads, head_dim, page_size
         self._page_shape = (page_size, kv_heads, head_dim)
+        blocks = -(-head_dim // 32)
+        self._code_shape, self._scale_shape = (page_size, kv_heads, 16 * blocks), (page_size, kv_heads, blocks)
         self._int = (torch.int32, torch.uint32)
         # argument structs, filled anew by every call
         self._args = {n: Rows() for n in ("q", "out", "k", "v", "prior")}
-        self._args.update(pages=Pages(), weights=Weights(), weights_out=Weights())
+        self._args.update(pages=Pages(), packed=PackedPages(), weights=Weights(), weights_out=Weights())
         self._refs = {n: ctypes.byref(a) for n, a in self._args.items()}
         self._seqs = Seqs()
         self._seqs_ref, self._seqs_at = ctypes.byref(self._seqs), ctypes.addressof(self._seqs)
@@ -512,7 +543,28 @@ class Cache:
         r.p, r.token_stride, r.head_stride = x.data_ptr(), stride[0], stride[1]
         return self._refs[name]
 
+    def _packed(self, k, v):
+        if not isinstance(v, Packed):
+            raise ValueError("k_pages and v_pages must both be Packed")
+        g, u8 = self._args["packed"], self._torch.uint8
+        for what, a, b, shape in (("codes", k.codes, v.codes, self._code_shape), ("scales", k.scales, v.scales, self._scale_shape)):
+            if (a.dtype != u8 or b.dtype != u8 or a.shape != b.shape or a.shape[1:] != shape or not a.is_cuda or not b.is_cuda
+                    or (shape[2] > 1 and (a.stride(3) != 1 or b.stride(3) != 1))):
+                raise ValueError(f"{what} of k_pages and v_pages must be (pages, {', '.join(map(str, shape))}) uint8 on the GPU, contiguous "
+                                 "along their last axis")
+            if a.stride() != b.stride() and any(n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride())):
+                raise ValueError(f"{what} of k_pages and v_pages must have the same strides")
+        if k.codes.shape[0] != k.scales.shape[0]:
+            raise ValueError("codes and scales must have as many pages")
+        g.k, g.v, g.k_scales, g.v_scales = k.codes.data_ptr(), v.codes.data_ptr(), k.scales.data_ptr(), v.scales.data_ptr()
+        g.n_pages = k.codes.shape[0]
+        g.page_stride, g.slot_stride, g.head_stride = k.codes.stride()[:3]
+        g.scale_page_stride, g.scale_slot_stride, g.scale_head_stride = k.scales.stride()[:3]
+        return self._refs["packed"]
+
     def _pages(self, k, v):
+        if isinstance(v, Packed):
+            raise ValueError("k_pages and v_pages must both be Packed")
         shape, stride = k.shape, k.stride()
         if (k.dtype != self.torch_dtype or v.dtype != self.torch_dtype or shape[1:] != self._page_shape or v.shape != shape
                 or not k.is_cuda or not v.is_cuda or stride[3] != 1):
@@ -583,16 +635,29 @@ class Cache:
         self._seqs.n_tokens = n
         return n, self._seqs_ref
 
+    def packed_pages(self, n_pages: int):
+        """Keys and values of a new pool held in 4 bits: two Packed of zeros,
+        heads outermost in a page."""
+        def zeros(shape):
+            with self._torch.cuda.stream(self._stream):
+                return self._torch.zeros((n_pages, shape[1], shape[0], shape[2]), dtype=self._torch.uint8, device=self._device).transpose(1, 2)
+        return tuple(Packed(zeros(self._code_shape), zeros(self._scale_shape)) for _ in range(2))
+
     def append(self, seqs: Sequences, k, v, k_pages, v_pages):
-        """grand_cache_append: the new tokens' keys and values go into their pages."""
+        """grand_cache_append, grand_cache_append_packed: the new tokens' keys and values go into their pages."""
         n, ref = self._tokens(seqs, k)
-        self._check(self.lib.grand_cache_append(self.h, ref, self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n),
-                                                self._pages(k_pages, v_pages)))
+        rk, rv = self._rows("k", k, self._kv, n), self._rows("v", v, self._kv, n)
+        if isinstance(k_pages, Packed):
+            self._check(self.lib.grand_cache_append_packed(self.h, ref, rk, rv, self._packed(k_pages, v_pages)))
+        else:
+            self._check(self.lib.grand_cache_append(self.h, ref, rk, rv, self._pages(k_pages, v_pages)))
 
     def attend(self, seqs: Sequences, q, k_pages, v_pages, scale: Optional[float] = None, causal: bool = True, window: int = 0,
-               weights=None, weights_out=None, out=None, lse=None):
-        """grand_cache_attend: (out, lse), and with weights (sequences,
-        kv_heads, at least max_k) also weights_out (weights itself if not given)."""
+               weights=None, weights_out=None, out=None, lse=None, sinks: int = 0):
+        """grand_cache_attend, grand_cache_attend_sinks, grand_cache_attend_packed:
+        (out, lse), and with weights (sequences, kv_heads, at least max_k)
+        also weights_out (weights itself if not given).  With a window every
+        row sees the first `sinks` tokens too."""
         n, ref = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:
@@ -606,13 +671,16 @@ class Cache:
             wo = self._weights("weights_out", weights_out, seqs.n_seq, seqs.max_k, self._kv)
         elif weights_out is not None:
             raise ValueError("weights_out needs weights")
-        self._check(self.lib.grand_cache_attend(
-            self.h, ref, rq, self._pages(k_pages, v_pages), self._dim ** -0.5 if scale is None else scale,
-            1 if causal else 0, window, ro, lse.data_ptr(), wi, wo))
+        if isinstance(k_pages, Packed):
+            call, pages = self.lib.grand_cache_attend_packed, self._packed(k_pages, v_pages)
+        else:
+            call, pages = self.lib.grand_cache_attend_sinks, self._pages(k_pages, v_pages)
+        self._check(call(self.h, ref, rq, pages, self._dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, sinks, ro,
+                         lse.data_ptr(), wi, wo))
         return (out, lse) if weights is None else (out, lse, weights_out)
 
     def attend_ids(self, q, k_pages, v_pages, ids, scale: Optional[float] = None, prior=None, out=None, lse=None):
-        """grand_cache_attend_ids: one token per sequence over ids (sequences,
+        """grand_cache_attend_ids(_packed): one token per sequence over ids (sequences,
         q_heads, k), e.g. the results of GrandIndex.search; prior: (out, lse)
         of the same rows over other tokens.  Returns (out, lse)."""
         n = int(q.shape[0])
@@ -629,8 +697,12 @@ class Cache:
         if prior is not None:
             rp = self._rows("prior", prior[0], self._q, n)
             zp = self._lse(prior[1], n).data_ptr()
-        self._check(self.lib.grand_cache_attend_ids(
-            self.h, n, rq, self._pages(k_pages, v_pages), ids.data_ptr(), k, stride[0], stride[1],
+        if isinstance(k_pages, Packed):
+            call, pages = self.lib.grand_cache_attend_ids_packed, self._packed(k_pages, v_pages)
+        else:
+            call, pages = self.lib.grand_cache_attend_ids, self._pages(k_pages, v_pages)
+        self._check(call(
+            self.h, n, rq, pages, ids.data_ptr(), k, stride[0], stride[1],
             self._dim ** -0.5 if scale is None else scale, rp, zp, ro, lse.data_ptr()))
         return out, lse
 
@@ -649,3 +721,86 @@ class Cache:
         self._check(self.lib.grand_cache_evict(self.h, seqs.ref, heads, cap, wi, budget.data_ptr(), sinks, recent, table.data_ptr(),
                                                wo, lens.data_ptr(), freed.data_ptr(), n_freed.data_ptr()))
         return table, new, lens, freed, n_freed
+
+    def read(self, slots, k_pages, v_pages):
+        """grand_packed_read: (keys, values), rows of listed slots as packed
+        pages hold them; INVALID entries are rows of zeros."""
+        n = int(slots.shape[0])
+        self._ints("slots", slots, (n,))
+        k, v = self._empty((n, self._kv, self._dim), self.torch_dtype), self._empty((n, self._kv, self._dim), self.torch_dtype)
+        self._check(self.lib.grand_packed_read(self.h, n, slots.data_ptr(), self._packed(k_pages, v_pages), self._rows("k", k, self._kv, n),
+                                               self._rows("v", v, self._kv, n)))
+        return k, v
+
+    # ------------------------------------------------------------ shared pages
+    def _counts(self, refs, refs_out):
+        """refs, and where they go: themselves if no other memory is given."""
+        if refs.dim() != 1:
+            raise ValueError("refs must have one entry for each page")
+        refs_out = refs if refs_out is None else refs_out
+        for name, x in (("refs", refs), ("refs_out", refs_out)):
+            self._ints(name, x, refs.shape)
+        return refs_out
+
+    def fork(self, seqs: Sequences, parents, refs, drop: bool = False, refs_out=None):
+        """grand_pages_fork: (table, lens, refs_out) of new sequences that go on
+        from the rows `parents`; drop: the old ones are given up."""
+        n = int(parents.shape[0])
+        self._ints("parents", parents, (n,))
+        refs_out = self._counts(refs, refs_out)
+        table, lens = self._empty((n, seqs.max_pages), self._torch.int32), self._empty(n, self._torch.int32)
+        self._check(self.lib.grand_pages_fork(self.h, seqs.ref, n, parents.data_ptr(), 1 if drop else 0, refs.shape[0], refs.data_ptr(),
+                                              refs_out.data_ptr(), table.data_ptr(), lens.data_ptr()))
+        return table, lens, refs_out
+
+    def grow(self, seqs: Sequences, n_new, refs, refs_out=None):
+        """grand_pages_grow: pages for n_new more tokens a sequence, in place in
+        the table and the lens that seqs was made of: (table, lens, src, dst),
+        src and dst for copy_pages."""
+        n = seqs.n_seq
+        self._ints("n_new", n_new, (n,))
+        refs_out = self._counts(refs, refs_out)
+        table, lens, _ = seqs.tensors
+        src, dst = self._empty(n, self._torch.int32), self._empty(n, self._torch.int32)
+        self._check(self.lib.grand_pages_grow(self.h, seqs.ref, n_new.data_ptr(), refs.shape[0], refs.data_ptr(), refs_out.data_ptr(),
+                                              table.data_ptr(), lens.data_ptr(), src.data_ptr(), dst.data_ptr()))
+        return table, lens, src, dst
+
+    def release(self, ids, refs, counts=None, tokens: bool = False, refs_out=None):
+        """grand_pages_release: (refs_out, freed, n_freed).  ids (rows, width):
+        tables of ended sequences (counts their lens, with tokens) or the freed
+        pages of evict (counts its n_freed), INVALID entries passed over."""
+        if ids.dim() != 2:
+            raise ValueError("ids must be (rows, width)")
+        rows, width = int(ids.shape[0]), int(ids.shape[1])
+        self._ints("ids", ids, (rows, width))
+        if counts is not None:
+            self._ints("counts", counts, (rows,))
+        refs_out = self._counts(refs, refs_out)
+        freed, n_freed = self._empty(min(refs.shape[0], rows * width), self._torch.int32), self._empty(1, self._torch.int32)
+        self._check(self.lib.grand_pages_release(self.h, rows, width, ids.data_ptr(), ids.stride(0), None if counts is None else counts.data_ptr(),
+                                                 1 if tokens else 0, refs.shape[0], refs.data_ptr(), refs_out.data_ptr(), freed.data_ptr(),
+                                                 n_freed.data_ptr()))
+        return refs_out, freed, n_freed
+
+    def compact(self, seqs: Sequences, refs, refs_out=None):
+        """grand_pages_compact: (table, refs_out, src, dst, n_moves), src and dst
+        for copy_pages."""
+        refs_out = self._counts(refs, refs_out)
+        n, empty, i32 = int(refs.shape[0]), self._empty, self._torch.int32
+        table, src, dst, moves = empty((seqs.n_seq, seqs.max_pages), i32), empty(n, i32), empty(n, i32), empty(1, i32)
+        self._check(self.lib.grand_pages_compact(self.h, seqs.ref, n, refs.data_ptr(), refs_out.data_ptr(), table.data_ptr(), src.data_ptr(),
+                                                 dst.data_ptr(), moves.data_ptr()))
+        return table, refs_out, src, dst, moves
+
+    def copy_pages(self, k_pages, v_pages, src, dst):
+        """grand_pages_copy, grand_packed_copy: pages src go to pages dst, keys and
+        values; INVALID entries are passed over."""
+        n = int(src.shape[0])
+        self._ints("src", src, (n,))
+        self._ints("dst", dst, (n,))
+        if isinstance(k_pages, Packed):
+            call, pages = self.lib.grand_packed_copy, self._packed(k_pages, v_pages)
+        else:
+            call, pages = self.lib.grand_pages_copy, self._pages(k_pages, v_pages)
+        self._check(call(self.h, n, src.data_ptr(), dst.data_ptr(), pages))

@@ -1,0 +1,429 @@
+"""The operators of caches held in 4 bits, and attention with first tokens
+that stay visible, against the definitions in 64 bits: types, head layouts,
+page sizes and orders, lengths from nothing to several splits, windows, blocks
+of NaN, what unused slots hold, offsets above 32 bits, weights, lists."""
+import math
+
+import numpy as np
+import pytest
+
+from cache_ref import INVALID, ids_ref
+from packed_ref import EXPONENTS, attend_ref, pack, unpack, visible
+from parity import say
+from test_gpu_cache_attend import LENGTHS, cache_for, make, seqs_for
+
+pytestmark = pytest.mark.gpu
+
+
+def packed(c, layout="head", seed=0):
+    """The cache of make() in 4 bits: its pools, and the values that they
+    stand for in place of the keys and values.  Unused slots hold any codes
+    and scales."""
+    import torch
+
+    from paper_2608_21163_amd import Packed
+
+    r = np.random.default_rng(seed)
+    pages, blocks = c["k_pages"].shape[0], -(-c["dim"] // 32)
+    res = dict(c)
+    for pool, rows in (("k_pages", "keys"), ("v_pages", "vals")):
+        codes = r.integers(0, 256, (pages, c["page"], c["hk"], 16 * blocks), dtype=np.uint8)
+        scales = r.integers(0, 256, (pages, c["page"], c["hk"], blocks), dtype=np.uint8)
+        values = []
+        for b, x in enumerate(c[rows]):
+            pc, ps = pack(x.double().numpy(), c["dtype"])
+            pos = np.arange(len(x))
+            table = c["table"][b].cpu().numpy()
+            codes[table[pos // c["page"]], pos % c["page"]], scales[table[pos // c["page"]], pos % c["page"]] = pc, ps
+            values.append(torch.from_numpy(unpack(pc, ps, c["dim"], c["dtype"])))
+        res[rows], res[pool] = values, as_packed(codes, scales, layout)
+        res[pool + "_np"] = codes, scales
+    return res
+
+
+def as_packed(codes, scales, layout):
+    """token: slots of all heads; head: heads outermost in a page; rows: a row's
+    scales behind its codes, in one buffer."""
+    import torch
+
+    from paper_2608_21163_amd import Packed
+
+    codes, scales = torch.from_numpy(codes), torch.from_numpy(scales)
+    if layout == "rows":
+        n, blocks = codes.shape[-1], scales.shape[-1]
+        both = torch.zeros(*codes.shape[:3], n + (blocks + 15) // 16 * 16, dtype=torch.uint8)
+        both[..., :n], both[..., n:n + blocks] = codes, scales
+        both = both.cuda()
+        return Packed(both[..., :n], both[..., n:n + blocks])
+    if layout == "head":
+        return Packed(*(x.transpose(1, 2).contiguous().cuda().transpose(1, 2) for x in (codes, scales)))
+    return Packed(codes.cuda(), scales.cuda())
+
+
+def compare(c, out, lse, causal=True, window=0, sinks=0, scale=None, weights=None, before=None):
+    scale = c["dim"] ** -0.5 if scale is None else scale
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b, (ql, kl) in enumerate(zip(c["qs"], c["ks"])):
+        r0 = int(c["starts"][b])
+        ro, rz, rw, bound, z_err, w_err = attend_ref(c["q"][r0:r0 + ql].double().numpy(), c["keys"][b].double().numpy(),
+                                                     c["vals"][b].double().numpy(), kl - ql, scale, causal, window, sinks)
+        o, z = out[r0:r0 + ql], lse[r0:r0 + ql]
+        empty = np.isneginf(rz)
+        assert np.array_equal(np.isneginf(z), empty), f"sequence {b}: rows that see nothing"
+        assert not o[empty].any()
+        err, lim = np.abs(o - ro), bound(c["dtype"])
+        assert (err <= lim).all(), f"sequence {b}: out off by {err.max()} (bound there {lim.flat[err.argmax()]})"
+        zerr = np.abs(np.where(empty, 0, z) - np.where(empty, 0, rz))
+        assert (zerr <= z_err + 1e-30).all(), f"sequence {b}: lse off by {zerr.max()} (bound {z_err.flat[zerr.argmax()]})"
+        if weights is not None:
+            old, new = before[b].double().cpu().numpy(), weights[b].double().cpu().numpy()
+            werr = np.abs(new[:, :kl] - old[:, :kl] - rw)
+            lim = w_err + 2.0 ** -23 * (np.abs(old[:, :kl]) + rw)
+            assert (werr <= lim + 1e-30).all(), f"sequence {b}: weights off by {werr.max()}"
+            assert np.array_equal(new[:, kl:], old[:, kl:]), "entries past the length changed"
+
+
+def run(c, max_q=None, max_k=None, **kw):
+    cache = cache_for(c)
+    out = cache.attend(seqs_for(cache, c, max_q, max_k), c["q"].cuda(), c["k_pages"], c["v_pages"], **kw)
+    cache.check()
+    cache.close()
+    return out
+
+
+def weighted(c, **kw):
+    import torch
+
+    before = torch.rand(len(c["ks"]), c["hk"], max(max(c["ks"]), 1) + 3, device="cuda")
+    after = before.clone()
+    out, lse, _ = run(c, weights=after, **kw)
+    compare(c, out, lse, weights=after, before=before, **kw)
+
+
+# ------------------------------------------------------------ packed pages
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("layout", ["token", "head", "rows"])
+@pytest.mark.parametrize("hq,hk,dim,page", [(4, 2, 64, 16), (8, 8, 128, 1), (14, 2, 80, 8), (5, 1, 256, 64), (3, 3, 8, 2),
+                                            (6, 2, 192, 32), (4, 4, 104, 128), (40, 1, 64, 16), (2, 1, 96, 1024), (2, 2, 40, 4)])
+def test_heads_and_layouts(dtype, layout, hq, hk, dim, page):
+    say(f"[packed heads] {dtype} {layout} {hq}/{hk} x {dim}, pages of {page}")
+    c = packed(make(dtype, hq, hk, dim, page, qs=(3, 1, 9), ks=(70, 33, 9), seed=hq * dim), layout)
+    compare(c, *run(c))
+
+
+@pytest.mark.parametrize("name", LENGTHS)
+@pytest.mark.parametrize("dtype,hq,hk,dim", [("bf16", 4, 2, 64), ("f16", 6, 1, 128)])
+def test_lengths(name, dtype, hq, hk, dim):
+    say(f"[packed lengths] {name} {dtype} {hq}/{hk} x {dim}")
+    qs, ks = LENGTHS[name]
+    c = packed(make(dtype, hq, hk, dim, 16, qs=qs, ks=ks, seed=len(name)))
+    compare(c, *run(c))
+
+
+@pytest.mark.parametrize("dim", [72, 96, 136, 192, 256])
+def test_chunks_of_other_rows(dim):
+    say(f"[packed chunks] {dim}")
+    c = packed(make("bf16", 6, 2, dim, 4, qs=(50, 7, 1), ks=(333, 130, 64), seed=dim))
+    weighted(c)
+    weighted(c, window=40, sinks=3)
+
+
+@pytest.mark.parametrize("qs,ks,window,sinks", [((1, 1, 1), (1, 90, 1400), 0, 0), ((3, 1), (200, 65), 0, 0), ((40, 0, 70), (300, 9, 70), 0, 0),
+                                                ((2, 50), (100, 50), 20, 2), ((1, 1), (500, 60), 33, 40), ((4, 9), (2, 3), 0, 0)])
+@pytest.mark.parametrize("dtype,hq,hk,dim", [("bf16", 4, 2, 64), ("f16", 8, 8, 128), ("bf16", 5, 1, 256)])
+def test_weights(qs, ks, window, sinks, dtype, hq, hk, dim):
+    say(f"[packed weights] {qs} {ks} window {window} {sinks} {dtype} {hq}/{hk} x {dim}")
+    c = packed(make(dtype, hq, hk, dim, qs=qs, ks=ks, seed=sum(ks)))
+    weighted(c, window=window, sinks=sinks)
+
+
+def nan_block(c, which, pos, block, head=slice(None)):
+    """A block of a token becomes NaN, in one of the ways that count as it."""
+    page = int(c["table"][0, pos // c["page"]])
+    scales = c[which].scales
+    scales[page, pos % c["page"], head, block] = 255 if pos % 2 else EXPONENTS[c["dtype"]][1] + 128
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("qs,ks,window,sinks", [((4,), (40,), 0, 0), ((70,), (150,), 0, 0), ((3,), (90,), 8, 4), ((60,), (190,), 16, 5)])
+def test_blocks_of_nan(dtype, dim, qs, ks, window, sinks):
+    """Rows that do not see such a token are as without it; of those that do, the
+    elements of a value's block, or the whole row of a key's, are NaN."""
+    import torch
+
+    say(f"[packed nan] {dtype} {dim} {qs} {ks} window {window} {sinks}")
+    c = packed(make(dtype, qs=qs, ks=ks, dim=dim, seed=5))
+    clean = run(c, window=window, sinks=sinks)
+    bad = [ks[0] - 1, ks[0] - 2] + ([ks[0] - qs[0] - window] if window else [])
+    rows = np.arange(qs[0]) + ks[0] - qs[0]
+    for pos in bad:
+        nan_block(c, "v_pages", pos, 1)
+    sees = np.array([visible(p, ks[0], True, window, sinks)[bad].any() for p in rows])
+    assert sees.any() and not sees.all()
+    sees = torch.from_numpy(sees).cuda()
+    out, lse = run(c, window=window, sinks=sinks)
+    assert torch.equal(lse, clean[1]) and torch.equal(out[~sees], clean[0][~sees])
+    assert torch.isnan(out[sees][..., 32:64]).all() and torch.equal(out[..., :32], clean[0][..., :32]) and torch.equal(out[..., 64:], clean[0][..., 64:])
+    for pos in bad:
+        nan_block(c, "k_pages", pos, 0)
+    out, lse = run(c, window=window, sinks=sinks)
+    assert torch.equal(out[~sees], clean[0][~sees]) and torch.equal(lse[~sees], clean[1][~sees]) and torch.isnan(out[sees]).all()
+    w = torch.zeros(1, c["hk"], ks[0], device="cuda")
+    run(c, window=window, sinks=sinks, weights=w)
+    only = np.any([visible(p, ks[0], True, window, sinks) for p in rows[sees.cpu().numpy()]], 0)
+    assert torch.isnan(w[0, :, torch.from_numpy(only).cuda()]).all() and torch.isfinite(w[0, :, torch.from_numpy(~only).cuda()]).all()
+
+
+def test_not_causal_and_scales():
+    c = packed(make("f16", qs=(5, 60), ks=(5, 200)))
+    compare(c, *run(c, causal=False), causal=False)
+    compare(c, *run(c, scale=3.5), scale=3.5)
+
+
+def test_pages_outside_the_pool_are_reported():
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ID
+
+    for qs, ks in (((1, 1), (301, 90)), ((70, 3), (301, 90))):
+        c = packed(make(qs=qs, ks=ks))
+        c["table"][1, 2] = c["k_pages"].codes.shape[0]
+        with pytest.raises(GrandError) as e:
+            run(c)
+        assert e.value.code == E_ID
+
+
+def test_offsets_above_32_bits():
+    """Pages more than 4 GiB apart: tokens lie in the first and the last."""
+    import torch
+
+    from paper_2608_21163_amd import Cache, Packed
+
+    pages, hk, dim = 700_000, 8, 128
+    codes = torch.zeros(pages, hk, 16, 64, dtype=torch.uint8, device="cuda").transpose(1, 2)
+    scales = torch.full((pages, hk, 16, 4), 127, dtype=torch.uint8, device="cuda").transpose(1, 2)
+    assert codes.numel() > 5 << 30
+    cache = Cache("bf16", 8, hk, dim, 16, stream=torch.cuda.current_stream().cuda_stream)
+    g = torch.Generator().manual_seed(1)
+    k, v, q = (torch.randn(40, hk, dim, generator=g).bfloat16() for _ in range(3))
+    table = torch.tensor([[0, pages - 1, pages - 2]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([40], dtype=torch.int32, device="cuda")
+    s = cache.sequences(table, lens, torch.tensor([0, 40], dtype=torch.int32, device="cuda"), max_q=40, max_k=40)
+    both = Packed(codes, scales)
+    rows = k.cuda()
+    cache.append(s, rows, rows, both, both)
+    held = torch.from_numpy(unpack(*pack(k.double().numpy(), "bf16"), dim, "bf16"))
+    out, lse = cache.attend(s, q.cuda(), both, both)
+    slots = torch.tensor([(pages - 2) * 16 + 7, 3], dtype=torch.int32, device="cuda")
+    rk, _ = cache.read(slots, both, both)
+    cache.check()
+    cache.close()
+    assert torch.equal(rk.cpu().double(), held[[39, 3]])
+    compare(dict(dtype="bf16", dim=dim, q=q, keys=[held], vals=[held], qs=(40,), ks=(40,), starts=[0]), out, lse)
+
+
+# ------------------------------------------------------------ append and read
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("layout", ["token", "head", "rows"])
+@pytest.mark.parametrize("hk,dim,page", [(2, 64, 16), (8, 128, 1), (2, 80, 8), (1, 256, 64), (3, 8, 2), (5, 104, 4)])
+def test_append_and_read(dtype, layout, hk, dim, page):
+    """Codes and scales are the definition's; nothing else in the pools
+    changes; reading gives their values."""
+    import torch
+
+    say(f"[packed append] {dtype} {layout} {hk} x {dim}, pages of {page}")
+    qs, ks = (3, 0, 20, 1), (40, 9, 20, 65)
+    c = packed(make(dtype, hk, hk, dim, page, qs=qs, ks=ks, seed=dim), layout, seed=3)
+    r = np.random.default_rng(dim)
+    rows = []
+    for _ in range(2):
+        x = r.standard_normal((sum(qs), hk, dim)) * 2.0 ** r.integers(-6, 6, (sum(qs), hk, 1))
+        x[0, 0] = 0
+        x[1, 0, :4] = [-0.0, 0.25, -0.75, 1.25]
+        if dim > 32:
+            x[2, -1, 32:] = 0
+        rows.append(torch.from_numpy(x).to(c["q"].dtype))
+    cache = cache_for(c)
+    cache.append(seqs_for(cache, c), rows[0].cuda(), rows[1].cuda(), c["k_pages"], c["v_pages"])
+    slots = []
+    for b, (ql, kl) in enumerate(zip(qs, ks)):
+        for pos in range(kl - ql, kl):
+            slots.append(int(c["table"][b, pos // page]) * page + pos % page)
+    read = cache.read(torch.tensor(slots + [-1], dtype=torch.int32, device="cuda"), c["k_pages"], c["v_pages"])
+    cache.check()
+    cache.close()
+    for name, x, got in (("k_pages", rows[0], read[0]), ("v_pages", rows[1], read[1])):
+        codes, scales = (y.copy() for y in c[name + "_np"])
+        pc, ps = pack(x.double().numpy(), dtype)
+        for i, s in enumerate(slots):
+            codes[s // page, s % page], scales[s // page, s % page] = pc[i], ps[i]
+        assert np.array_equal(c[name].codes.cpu().numpy(), codes) and np.array_equal(c[name].scales.cpu().numpy(), scales)
+        assert np.array_equal(got[:-1].double().cpu().numpy(), unpack(pc, ps, dim, dtype)) and not got[-1].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_number_packs(dtype):
+    """Every finite 16-bit number as the largest of a block and beside a
+    larger one, and blocks with infinities and NaN."""
+    import torch
+
+    from paper_2608_21163_amd import Cache
+
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    x = bits.view({"bf16": torch.bfloat16, "f16": torch.float16}[dtype])
+    x = torch.cat([x.repeat(2), x.flip(0)])[:3 * 65536]
+    step = torch.arange(len(x)) % 31 + 1
+    rows = torch.zeros(len(x), 32, dtype=x.dtype)
+    rows[:, 0] = x
+    rows[65536:, 1] = (x[65536:].float() * (1 + step[65536:] / 8)).to(x.dtype)
+    rows = rows.view(-1, 1, 32)
+    n = len(rows)
+    cache = Cache(dtype, 1, 1, 32, 1024, stream=torch.cuda.current_stream().cuda_stream)
+    k, v = cache.packed_pages(n // 1024)
+    table = torch.arange(n // 1024, dtype=torch.int32, device="cuda")[None]
+    s = cache.sequences(table, torch.tensor([n], dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda"),
+                        max_q=n, max_k=n)
+    cache.append(s, rows.cuda(), rows.cuda(), k, v)
+    cache.check()
+    codes, scales = pack(rows.double().numpy(), dtype)
+    assert np.array_equal(k.scales.reshape(n, 1, 1).cpu().numpy(), scales)
+    assert np.array_equal(k.codes.reshape(n, 1, 16).cpu().numpy(), codes) and torch.equal(v.codes, k.codes)
+    got, _ = cache.read(torch.arange(n, dtype=torch.int32, device="cuda"), k, v)
+    want = unpack(codes, scales, 32, dtype)
+    assert np.array_equal(got.double().cpu().numpy(), want, equal_nan=True)
+    fine = np.isfinite(want).all(-1)[:, 0]
+    err = np.abs(want - rows.double().numpy())[fine, 0]
+    top = np.abs(rows.double().numpy())[fine, 0].max(-1, keepdims=True)
+    # half a step where steps are largest, 2^e with 3.5 * 2^e at most the largest element; fp16 ends at 6 * 2^13
+    ordinary = top[:, 0] < 7 * 2.0 ** EXPONENTS[dtype][1]
+    assert (err[ordinary] <= np.maximum(top[ordinary] / 3.5, 2.0 ** (EXPONENTS[dtype][0] - 2))).all()
+    cache.close()
+
+
+# ------------------------------------------------------------ listed slots
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("layout", ["token", "head", "rows"])
+@pytest.mark.parametrize("hq,hk,dim,page,n", [(4, 2, 64, 1, 37), (8, 8, 128, 16, 300), (6, 2, 80, 8, 1), (5, 1, 256, 4, 700), (3, 3, 8, 2, 5),
+                                              (8, 4, 192, 1, 64)])
+@pytest.mark.parametrize("prior", [False, True])
+def test_listed_slots(dtype, layout, hq, hk, dim, page, n, prior):
+    import torch
+
+    say(f"[packed ids] {dtype} {layout} {hq}/{hk} x {dim} pages of {page}, lists of {n}, prior {prior}")
+    c = packed(make(dtype, hq, hk, dim, page, qs=(1,), ks=(600,), seed=n), layout)
+    r = np.random.default_rng(n)
+    slots = np.array([int(c["table"][0, p // page]) * page + p % page for p in range(600)])
+    b = 3
+    q = torch.from_numpy(r.standard_normal((b, hq, dim)) * 2).to(c["q"].dtype)
+    pick = r.integers(0, 600, (b, hq, n))
+    ids = slots[pick].astype(np.uint32)
+    ids[r.random(ids.shape) < 0.1] = INVALID
+    ids[1, 0] = INVALID
+    po = torch.from_numpy(r.standard_normal((b, hq, dim))).to(q.dtype)
+    pz = torch.from_numpy(r.standard_normal((b, hq))).float()
+    pz[1, 1], pz[1, 0] = -math.inf, -math.inf
+    cache = cache_for(c)
+    got = cache.attend_ids(q.cuda(), c["k_pages"], c["v_pages"], torch.from_numpy(ids.astype(np.int32)).cuda(),
+                           prior=(po.cuda(), pz.cuda()) if prior else None)
+    cache.check()
+    cache.close()
+    total = c["k_pages"].codes.shape[0] * page
+    flat = [np.zeros((total, hk, dim)) for _ in range(2)]
+    for x, rows in zip(flat, (c["keys"], c["vals"])):
+        x[slots] = rows[0].numpy()
+    want, z, bound, z_err = ids_ref(q.double().numpy(), *flat, ids, dim ** -0.5, (po.double().numpy(), pz.double().numpy()) if prior else None)
+    o, l = got[0].double().cpu().numpy(), got[1].double().cpu().numpy()
+    assert (np.abs(o - want) <= bound(dtype)).all()
+    empty = np.isneginf(z)
+    assert np.array_equal(np.isneginf(l), empty) and empty.any()
+    assert (np.abs(np.where(empty, 0, l) - np.where(empty, 0, z)) <= z_err + 1e-30).all()
+
+
+# ------------------------------------------------------------ first tokens
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+@pytest.mark.parametrize("window,sinks", [(1, 1), (7, 4), (32, 32), (33, 64), (100, 5), (40, 65), (100000, 3), (40, 100000)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("qs,ks", [((1, 1, 1), (700, 40, 3)), ((50, 33, 2), (500, 33, 260)), ((3, 5, 0), (2, 900, 7)), ((300,), (1111,))])
+def test_first_tokens(kind, window, sinks, causal, qs, ks):
+    say(f"[sinks] {kind} window {window} {sinks} causal {causal} {qs} {ks}")
+    c = make(qs=qs, ks=ks, seed=window + sinks)
+    c = packed(c) if kind == "packed" else c
+    weighted(c, window=window, sinks=sinks, causal=causal)
+
+
+@pytest.mark.parametrize("dtype,hq,hk,dim,page", [("f16", 12, 12, 64, 1), ("bf16", 4, 1, 192, 8), ("f16", 5, 1, 256, 16), ("bf16", 8, 8, 96, 64),
+                                                  ("bf16", 32, 1, 80, 16)])
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+def test_first_tokens_of_other_heads(kind, dtype, hq, hk, dim, page):
+    say(f"[sinks heads] {kind} {dtype} {hq}/{hk} x {dim} pages of {page}")
+    for qs, ks in (((1, 1), (1500, 77)), ((80, 2), (600, 400))):
+        c = make(dtype, hq, hk, dim, page, qs=qs, ks=ks, seed=dim)
+        c = packed(c) if kind == "packed" else c
+        weighted(c, window=70, sinks=9)
+
+
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+def test_no_first_tokens_is_the_window(kind):
+    """sinks 0, and sinks without a window, change nothing, bit by bit."""
+    import torch
+
+    for qs, ks in (((1, 1), (1500, 77)), ((80, 2), (600, 400))):
+        c = make(qs=qs, ks=ks)
+        c = packed(c) if kind == "packed" else c
+        assert all(torch.equal(a, b) for a, b in zip(run(c, sinks=8), run(c)))
+        near = run(c, window=64)
+        assert all(torch.equal(a, b) for a, b in zip(run(c, window=64, sinks=0), near))
+        assert not torch.equal(run(c, window=64, sinks=1)[0], near[0])
+
+
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+@pytest.mark.parametrize("page", [1, 8, 16])
+@pytest.mark.parametrize("qs,ks", [((1, 1), (301, 90)), ((3,), (777,)), ((50, 33), (300, 95))])
+def test_pages_between_may_be_gone(kind, page, qs, ks):
+    """Pages between the first tokens and the window are freed: no results
+    change and nothing is reported; a page of the first tokens is."""
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ID
+
+    window, sinks = 37, 5
+    c = make(qs=qs, ks=ks, page=page)
+    c = packed(c) if kind == "packed" else c
+    want = run(c, window=window, sinks=sinks)
+    for b, (ql, kl) in enumerate(zip(qs, ks)):
+        c["table"][b, -(-sinks // page):max(0, kl - ql - window + 1) // page] = -1
+    got = run(c, window=window, sinks=sinks)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    w = torch.zeros(len(ks), c["hk"], max(ks), device="cuda")
+    assert all(torch.equal(a, b) for a, b in zip(run(c, window=window, sinks=sinks, weights=w), want))
+    c["table"][0, (sinks - 1) // page] = -1
+    with pytest.raises(GrandError) as e:
+        run(c, window=window, sinks=sinks)
+    assert e.value.code == E_ID
+
+
+@pytest.mark.parametrize("qs,ks", [((3,), (90,)), ((60,), (190,))])
+def test_first_tokens_hidden_ones_hold_anything(qs, ks):
+    """Between the first tokens and a row's window lie NaN and infinities."""
+    import torch
+
+    c = make(qs=qs, ks=ks, seed=5)
+    window, sinks = 16, 5
+    clean = run(c, window=window, sinks=sinks)
+    for pos, x in ((sinks, math.nan), (sinks + 1, math.inf), (ks[0] - qs[0] - window - 1, -math.inf)):
+        for pool in ("k_pages", "v_pages"):
+            c[pool][int(c["table"][0, pos // 16]), pos % 16] = x
+    out, lse = run(c, window=window, sinks=sinks)
+    assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+    c["v_pages"][int(c["table"][0, 0]), 4] = math.inf            # a first token: every row sees it
+    out, lse = run(c, window=window, sinks=sinks)
+    assert (out == math.inf).all() and torch.equal(lse, clean[1])
+
+
+def test_long_histories_of_first_tokens():
+    """Several splits of the first tokens and of the window."""
+    for qs, ks in (((1, 1), (9000, 5000)), ((20, 70), (5000, 3001))):
+        c = make("f16", 4, 1, 64, 16, qs=qs, ks=ks, seed=1)
+        weighted(c, window=2100, sinks=1500)
+        weighted(packed(c), window=2100, sinks=1500)
