@@ -85,6 +85,8 @@ __device__ __forceinline__ void lds_wave_fence() {
 // read cover all banks.
 template <int DP> constexpr int k_row() { return DP * 2 + 16; }
 template <int DP> constexpr int v_row() { return DP * 2 + ((DP * 2) % 128 == 0 ? 64 : 0); }
+// (values that are unpacked: 16 bytes a lane of eight rows in consecutive lanes, which start 32 bytes apart)
+template <int DP> constexpr int packed_v_row() { return DP * 2 + 32; }
 template <int DP, int KT> constexpr int tile_bytes() { return KT * (k_row<DP>() + v_row<DP>()); }
 
 // Global loads of one tile of KT keys by 256 threads into registers, and
@@ -526,11 +528,12 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
 }
 
 // The end of a kernel whose four waves took different keys of the same 16 NB
-// rows: their sums meet in LDS, and leave as results or as a split's.
+// rows: their sums meet in LDS, and leave as results (direct) or at place
+// part(row of the results, row of the chunk) among the parts.
 template <int DP> constexpr int few_sum() { return DP + 4; }  // floats of a row
-template <class E, int DP, int NB>
+template <class E, int DP, int NB, class Part>
 __device__ __forceinline__ void few_finish(const AttendArgs &a, const Chunk &ch, uint8_t *smem, float2 (*ml)[16], const v4f (*o)[DP / 16],
-                                           const float *m, float *l, uint32_t kvh, uint32_t split, uint32_t r0, uint32_t r1) {
+                                           const float *m, float *l, uint32_t kvh, uint32_t r0, uint32_t r1, bool direct, Part part) {
   constexpr int kSum = few_sum<DP>();
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, c = lane & 15;
   float *sum = (float *)smem;
@@ -562,7 +565,7 @@ __device__ __forceinline__ void few_finish(const AttendArgs &a, const Chunk &ch,
       const bool some = ll > 0.f || ll != ll;
       const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
       const size_t at = (size_t)token * a.q_heads + head;
-      if (a.n_splits == 1) {
+      if (direct) {
         const float inv = some ? 1.f / ll : 0.f;
         typename E::T y[4];
 #pragma unroll
@@ -574,8 +577,9 @@ __device__ __forceinline__ void few_finish(const AttendArgs &a, const Chunk &ch,
           if (a.lse2) a.lse2[at] = z;
         }
       } else {
-        *(v4f *)(a.part + (at * a.n_splits + split) * a.dim + d) = v;
-        if (d == 0) a.part_ml[at * a.n_splits + split] = make_float2(some ? mm : neg_inf(), ll);
+        const size_t to = part(at, r);
+        *(v4f *)(a.part + to * a.dim + d) = v;
+        if (d == 0) a.part_ml[to] = make_float2(some ? mm : neg_inf(), ll);
       }
     }
   }
@@ -609,10 +613,9 @@ __device__ __forceinline__ void few_softmax(const v4f *sc, float c, float &m, fl
 }
 
 // O^T += V^T P^T of a tile of 32 keys in LDS.
-template <class E, int DP, int NB>
+template <class E, int DP, int NB, int VROW>
 __device__ __forceinline__ void few_values(const uint8_t *lt, int g, int c, const typename E::V *p, v4f (*o)[DP / 16]) {
   typedef typename E::V Op;
-  constexpr int VROW = v_row<DP>();
 #pragma unroll
   for (int d = 0; d < DP / 16; d++) {
     typedef __attribute__((address_space(3))) v4s *P;
@@ -819,7 +822,7 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
         }
         few_softmax<E, DP>(sc[nb], a.c, m[nb], l[nb], o[nb], p[nb]);
       }
-      few_values<E, DP, NB>(lt, g, c, p, o);
+      few_values<E, DP, NB, VROW>(lt, g, c, p, o);
     }
     if (__ballot(odd)) {  // as add_non_finite
       for (uint32_t k0 = begin + wave * 32; k0 < end; k0 += kKeysStep)
@@ -844,7 +847,57 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
         }
     }
   }
-  few_finish<E, DP, NB>(a, ch, smem, ml, o, m, l, kvh, split, r0, r1);
+  few_finish<E, DP, NB>(a, ch, smem, ml, o, m, l, kvh, r0, r1, a.n_splits == 1, [&](size_t at, uint32_t) { return at * a.n_splits + split; });
+}
+
+// Shares of the work of few rows: the keys that a sequence's rows see, in steps of
+// kKeysStep, one sequence after the other, are one line of `total` steps, and
+// unit u takes those from u * per on.  Lengths lie on the GPU, so every
+// workgroup adds them up itself.
+struct Share {
+  uint32_t total, per;
+  uint32_t seq, before;  // a sequence, and the steps before it
+};
+__device__ __forceinline__ uint32_t steps_of(const AttendArgs &a, uint32_t b) {
+  const Chunk ch = chunk_of(a.s, b, a.err);
+  if (!ch.ql) return 0;
+  const KeyLine<Sinks> line(a, ch, 0, ch.ql - 1);
+  return max((line.hi - line.lo + kKeysStep - 1) / kKeysStep, 1u);
+}
+// The sequence that has step find(per) of the line, or that is find(per).
+template <class F>
+__device__ __forceinline__ Share share_of(const AttendArgs &a, bool by_step, F find) {
+  Share s{};
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t steps = 0, sum = 0;
+  for (uint32_t b0 = 0; b0 < a.s.n_seq; b0 += 64) {
+    steps = b0 + lane < a.s.n_seq ? steps_of(a, b0 + lane) : 0;
+    sum += steps;
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) sum += (uint32_t)__shfl_xor((int)sum, j, 64);
+  s.total = (uint32_t)__builtin_amdgcn_readfirstlane((int)sum);
+  s.per = (uint32_t)__builtin_amdgcn_readfirstlane((int)max((sum + a.units - 1) / a.units, 1u));
+  const uint32_t want = find(s.per);
+  uint32_t base = 0;
+  for (uint32_t b0 = 0; b0 < a.s.n_seq; b0 += 64) {
+    if (a.s.n_seq > 64) steps = b0 + lane < a.s.n_seq ? steps_of(a, b0 + lane) : 0;
+    uint32_t x = steps;
+#pragma unroll
+    for (int j = 1; j < 64; j <<= 1) {
+      const uint32_t y = (uint32_t)__shfl_up((int)x, j, 64);
+      if ((int)lane >= j) x += y;
+    }
+    const uint64_t at = __ballot(by_step ? base + x > want && base + x - steps <= want : b0 + lane == want);
+    if (at) {
+      const int l = __ffsll((unsigned long long)at) - 1;
+      s.seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)b0 + l);
+      s.before = base + (uint32_t)__builtin_amdgcn_readlane((int)(x - steps), l);
+      break;
+    }
+    base += (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+  }
+  return s;
 }
 
 // The same over packed pages.  A row's codes are a quarter of its bytes, so a
@@ -852,194 +905,299 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
 // (c, g) holds block g of key c, 32 elements with one scale, which are the
 // operands of four steps (queries are read in that order of elements).  No
 // LDS for the keys; values pass through it as 16 bits for their transposition.
-// The next tile's 4 KB are in flight while one is computed.
-template <class E, int DP, int NB>
-__global__ __launch_bounds__(256, DP > 128 ? (NB > 1 ? 1 : 2) : NB > 1 ? 2 : 3) void k_attend_few_packed(AttendArgs a) {
+// A wave takes tiles of 32 keys; the next one (4 KB at 128 elements) is in flight
+// while one is computed (with the one after it, too, 69.8 us become 78).
+// WIDE: pages of 16 slots or more, and whole rows of DP elements whose scales are
+// aligned.  Sixteen keys of a tile then lie in one page: a lane's part of an address
+// never changes, a wave looks up the places of 64 such runs at once, and the
+// scales of 64 keys are one load, a row a lane.
+// A workgroup takes a split of one sequence's keys, or (a.units) a share of all
+// sequences' keys, which lie behind each other.
+template <class E, int DP, int NB, bool WIDE>
+__global__ __launch_bounds__(256, packed_groups(DP, NB)) void k_attend_few_packed(AttendArgs a) {
   typedef typename E::V Op;
+  constexpr int KT = 32, R = 2, STEP = kKeysStep;  // keys of a tile, runs of 16 of them
   constexpr int W = DP == 64 ? 2 : 4, LD = DP / 32 / W;  // words of eight codes a load, loads of a row's share
-  constexpr int VROW = v_row<DP>(), ROWS = 16 * NB;
-  constexpr int kTiles = 4 * 32 * VROW, kSums = 4 * 16 * few_sum<DP>() * 4;
+  constexpr int VROW = packed_v_row<DP>(), ROWS = 16 * NB;
+  constexpr int kTiles = 4 * KT * VROW, kSums = 4 * 16 * few_sum<DP>() * 4;
   typedef uint32_t vw __attribute__((ext_vector_type(W)));
   __shared__ __align__(16) uint8_t smem[kTiles > kSums ? kTiles : kSums];
   __shared__ float2 ml[4][16];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, c = lane & 15;
   // (as k_attend_few's)
   const uint32_t unit = blockIdx.x / (8 * a.kv_heads) * 8 + blockIdx.x % 8, kvh = blockIdx.x / 8 % a.kv_heads;
-  const uint32_t b = unit % a.s.n_seq, rt = unit / a.s.n_seq % a.row_tiles, split = unit / a.s.n_seq / a.row_tiles;
-  if (split >= a.n_splits) return;
-  const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
-  uint32_t page[2];
-  auto pages = [&](uint32_t key0) {
-#pragma unroll
-    for (int kb = 0; kb < 2; kb++) page[kb] = table[min((key0 + kb * 16 + c) >> a.pg.shift, a.s.max_pages - 1)];
-  };
-  if (a.s.max_pages) pages(split * a.split + wave * 32);
-  const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t rows = ch.ql * a.group, r0 = rt * ROWS;
-  if (r0 >= rows) return;
-  const uint32_t r1 = min(rows, r0 + ROWS) - 1;
-  const KeyLine<Packed> line(a, ch, r0 / a.group, r1 / a.group);
-  const uint32_t begin = line.lo + split * a.split, end = min(line.hi, begin + a.split);
-  if (split && begin >= line.hi) return;
-  if (line.gap) pages(line.key(a, begin + wave * 32));
-
-  Op q[NB][DP / 32];
-  int first[NB], last[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; nb++) {
-    const uint32_t r = min(r0 + nb * 16 + c, r1), tok = r / a.group;
-    const uint8_t *p = a.q.p + (int64_t)(ch.r0 + tok) * a.q.token + (int64_t)(kvh * a.group + r % a.group) * a.q.head;
-#pragma unroll
-    for (int s = 0; s < DP / 32; s++) {
-      const int at = ((s / W * 4 + g) * W + s % W) * 8;
-      v4u x{0, 0, 0, 0};
-      if (at < (int)a.dim) x = *(const v4u *)(p + at * 2);
-      q[nb][s] = __builtin_bit_cast(Op, x);
-    }
-    const int pos = ch.p0 + (int)tok;
-    last[nb] = a.causal ? min(pos, (int)ch.kl - 1) : (int)ch.kl - 1;
-    first[nb] = a.window ? pos - (int)a.window + 1 : 0;
+  uint32_t b, rt = 0, split = 0, pos, left;  // the sequence, the segment's first step and the steps that are left
+  if (a.units) {
+    if (unit >= a.units) return;
+    const Share s = share_of(a, true, [&](uint32_t per) { return unit * per; });
+    if (unit * s.per >= s.total) return;
+    b = s.seq;
+    pos = unit * s.per - s.before;
+    left = min(s.per, s.total - unit * s.per);
+  } else {
+    b = unit % a.s.n_seq, rt = unit / a.s.n_seq % a.row_tiles, split = unit / a.s.n_seq / a.row_tiles;
+    if (split >= a.n_splits) return;
+    pos = split * (a.split / STEP);
+    left = a.n_splits > 1 ? a.split / STEP : ~0u;
   }
-  // every row sees the keys from all0 to all1
-  const int all0 = a.window ? ch.p0 + (int)(r1 / a.group) - (int)a.window + 1 : 0;
-  const int all1 = a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
-  const int sinks = (int)a.sinks;
-
-  v4f o[NB][DP / 16];
-  float m[NB], l[NB];
+  const uint32_t mask = (1u << a.pg.shift) - 1;
+  const int blocks = ((int)a.dim + 31) / 32;
+  // bytes from a slot's row to the lane's blocks and their scales (past a row's
+  // last block that one again: its elements meet zeros of the queries, or are
+  // not written)
+  uint32_t in_row[LD], in_scales[LD];
 #pragma unroll
-  for (int nb = 0; nb < NB; nb++) {
-    m[nb] = neg_inf();
-    l[nb] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DP / 16; d++) o[nb][d] = v4f{0, 0, 0, 0};
+  for (int j = 0; j < LD; j++) {
+    const int block = (j * 4 + g) * W / 4;
+    in_row[j] = kvh * a.pg.head + (block < blocks ? (j * 4 + g) * W * 4 : (blocks - 1) * 16);
+    in_scales[j] = kvh * a.sc.head + min(block, blocks - 1);
+    if constexpr (WIDE) in_row[j] += c * a.pg.slot;
   }
-  // a lane's blocks of keys c and 16 + c of a tile and of their values; a key
-  // at or past the end reads some slot of the pool and is hidden
-  struct Tile {
-    vw k[2][LD], v[2][LD];
-    uint32_t ks[2][LD], vs[2][LD];
-  } next;
-  auto block = [&](int j) { return (j * 4 + g) * W / 4; };
-  auto load = [&](uint32_t at) {
-    const uint32_t key0 = line.key(a, at), tile_end = line.end_of(a, at, end), mask = (1u << a.pg.shift) - 1;
-    bool bad = false;
-#pragma unroll
-    for (int kb = 0; kb < 2; kb++) {
-      const uint32_t key = key0 + kb * 16 + c;
-      bad |= page[kb] >= a.pg.n_pages && key < tile_end && (key >= line.seen || (int)key < sinks);
-      const uint64_t pg = min(page[kb], a.pg.n_pages - 1);
-      const uint64_t off = pg * a.pg.page + ((key & mask) * a.pg.slot + kvh * a.pg.head + g * W * 4);
-      const uint64_t sc = pg * a.sc.page + ((key & mask) * a.sc.slot + kvh * a.sc.head);
-#pragma unroll
-      for (int j = 0; j < LD; j++) {
-        const bool in = block(j) * 32 < (int)a.dim;
-        next.k[kb][j] = next.v[kb][j] = vw(0);
-        next.ks[kb][j] = next.vs[kb][j] = 127;
-        if (in) {
-          next.k[kb][j] = __builtin_nontemporal_load((const vw *)(a.pg.k + off + j * 64));
-          next.v[kb][j] = __builtin_nontemporal_load((const vw *)(a.pg.v + off + j * 64));
-          next.ks[kb][j] = a.sc.k[sc + block(j)];
-          next.vs[kb][j] = a.sc.v[sc + block(j)];
-        }
-      }
-    }
-    if (bad) cache_err(a.err, kCachePage, b);
-  };
-  bool odd = false;
+  if constexpr (WIDE) in_scales[0] = kvh * a.sc.head + c * a.sc.slot;  // a whole row: of key, or value, `lane`
   uint8_t *lt = smem + wave * (kTiles / 4);
-  uint32_t at0 = begin + wave * 32;
-  if (at0 < end) {
-    load(at0);
-    pages(line.key(a, at0 + kKeysStep));
-    for (; at0 < end; at0 += kKeysStep) {
-      const uint32_t key0 = line.key(a, at0);
-      const int tile_end = (int)line.end_of(a, at0, end);
-      const bool masked = (int)key0 < all0 || (int)key0 + 31 > min(all1, tile_end - 1);
-      Tile x = next;
-      if (at0 + kKeysStep < end) {
-        load(at0 + kKeysStep);
-        pages(line.key(a, at0 + 2 * kKeysStep));
+  const int sinks = (int)a.sinks;
+  // Codes of consecutive keys side by side pass by the caches; where other heads'
+  // lie between them, a line is several workgroups' (64 single tokens over up to
+  // 8,192, two over 131,072 with weights: side by side 69.8 us past the caches, 74.3
+  // through them, slots of all heads 87.9 and 83.0, 114 and 100.5).
+  const bool stream = DP >= 128 && a.pg.slot == DP / 2;
+
+  for (bool first_seg = true; left && b < a.s.n_seq; first_seg = false) {
+    const uint32_t *table = a.s.table + (int64_t)b * a.s.table_stride;
+    const Chunk ch = chunk_of(a.s, b, a.err);
+    const uint32_t rows = ch.ql * a.group, r0 = rt * ROWS;
+    if (r0 >= rows) {
+      if (!a.units) return;
+      b++;
+      continue;
+    }
+    const uint32_t r1 = min(rows, r0 + ROWS) - 1;
+    const KeyLine<Packed> line(a, ch, r0 / a.group, r1 / a.group);
+    const uint32_t steps = (uint32_t)__builtin_amdgcn_readfirstlane((int)max((line.hi - line.lo + STEP - 1) / STEP, 1u));
+    const uint32_t n = min(steps - min(pos, steps), left);
+    if (!a.units && split && !n) return;
+    const uint32_t begin = line.lo + pos * STEP, end = min(line.hi, begin + n * STEP);
+    // Where runs of 16 keys lie, in bytes of codes and of scales: WIDE lane r % R of
+    // tile r / R from here on; else keys c of the next tile's runs.
+    constexpr int P = WIDE ? 1 : R;
+    uint64_t code_at[P], scale_at[P];
+    auto places = [&](uint32_t at) {
+      bool bad = false;
+#pragma unroll
+      for (int r = 0; r < P; r++) {
+        const uint32_t from = WIDE ? at + lane / R * STEP + lane % R * 16 : at, to = from + (WIDE ? 0 : r * 16 + c);
+        const uint32_t key = line.key(a, from) + (to - from), run = line.end_of(a, from, end);
+        const uint32_t id = table[min(key >> a.pg.shift, a.s.max_pages - 1)];
+        bad |= id >= a.pg.n_pages && from < end && key < run && (key + (WIDE ? 16 : 1) > line.seen || (int)key < sinks);
+        const uint64_t pg = min(id, a.pg.n_pages - 1);
+        code_at[r] = pg * a.pg.page + (key & mask) * a.pg.slot;
+        scale_at[r] = pg * a.sc.page + (key & mask) * a.sc.slot;
       }
-      v4f sc[NB][2];
+      if (bad) cache_err(a.err, kCachePage, b);
+    };
+    uint32_t at0 = begin + wave * KT, tile = 0;
+    if (at0 < end) places(at0);
+
+    Op q[NB][DP / 32];
+    int first[NB], last[NB];
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) {
+    for (int nb = 0; nb < NB; nb++) {
+      const uint32_t r = min(r0 + nb * 16 + c, r1), tok = r / a.group;
+      const uint8_t *p = a.q.p + (int64_t)(ch.r0 + tok) * a.q.token + (int64_t)(kvh * a.group + r % a.group) * a.q.head;
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++) sc[nb][kb] = v4f{0, 0, 0, 0};
+      for (int s = 0; s < DP / 32; s++) {
+        const int at = ((s / W * 4 + g) * W + s % W) * 8;
+        v4u x{0, 0, 0, 0};
+        if (at < (int)a.dim) x = *(const v4u *)(p + at * 2);
+        q[nb][s] = __builtin_bit_cast(Op, x);
+      }
+      const int p0 = ch.p0 + (int)tok;
+      last[nb] = a.causal ? min(p0, (int)ch.kl - 1) : (int)ch.kl - 1;
+      first[nb] = a.window ? p0 - (int)a.window + 1 : 0;
+    }
+    // every row sees the keys from all0 to all1
+    const int all0 = a.window ? ch.p0 + (int)(r1 / a.group) - (int)a.window + 1 : 0;
+    const int all1 = a.causal ? min(ch.p0 + (int)(r0 / a.group), (int)ch.kl - 1) : (int)ch.kl - 1;
+
+    v4f o[NB][DP / 16];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; nb++) {
+      m[nb] = neg_inf();
+      l[nb] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) o[nb][d] = v4f{0, 0, 0, 0};
+    }
+    // A lane's blocks of the keys c of a tile's runs and of their values; a key
+    // at or past the end reads some slot of the pool and is hidden.
+    constexpr int S = WIDE ? 1 : 2 * R;  // scales: WIDE a row, else of each run's keys and values
+    struct Tile {
+      vw k[R][LD], v[R][LD];
+      uint32_t s[S][LD];
+    } next;
+    auto load = [&](uint32_t i) {  // i: the tile among those whose places are known
+#pragma unroll
+      for (int r = 0; r < R; r++) {
+        uint64_t at;
+        if constexpr (WIDE) {
+          const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)code_at[0], R * i + r);
+          const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(code_at[0] >> 32), R * i + r);
+          at = (uint64_t)hi << 32 | lo;
+        } else {
+          at = code_at[r];
+        }
 #pragma unroll
         for (int j = 0; j < LD; j++) {
-          const float f = pack_factor<E>(x.ks[kb][j]);
-#pragma unroll
-          for (int w = 0; w < W; w++) {
-            const Op k = __builtin_bit_cast(Op, unpack8<E>(x.k[kb][j][w], f));
-#pragma unroll
-            for (int nb = 0; nb < NB; nb++) sc[nb][kb] = E::mul16(k, q[nb][j * W + w], sc[nb][kb]);
+          const vw *k = (const vw *)(a.pg.k + at + in_row[j]), *v = (const vw *)(a.pg.v + at + in_row[j]);
+          if (stream) {
+            next.k[r][j] = __builtin_nontemporal_load(k);
+            next.v[r][j] = __builtin_nontemporal_load(v);
+          } else {
+            next.k[r][j] = *k;
+            next.v[r][j] = *v;
+          }
+          if constexpr (!WIDE) {
+            next.s[r][j] = a.sc.k[scale_at[r] + in_scales[j]];
+            next.s[R + r][j] = a.sc.v[scale_at[r] + in_scales[j]];
           }
         }
       }
-      if (masked) {
+      if constexpr (WIDE) {
+        // the lower lanes keys, the upper ones values
+        const int from = (R * (int)i + g % R) * 4;
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)scale_at[0]);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)(scale_at[0] >> 32));
+        const uint8_t *p = (g >= R ? a.sc.v : a.sc.k) + (((uint64_t)hi << 32 | lo) + in_scales[0]);
+        if constexpr (DP == 64) {
+          next.s[0][0] = *(const uint16_t *)p;
+        } else {
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
+          for (int j = 0; j < LD; j++) next.s[0][j] = *(const uint32_t *)(p + j * 4);
+        }
+      }
+    };
+    bool odd = false;
+    if (at0 < end) {
+      load(0);
+      if constexpr (!WIDE) places(at0 + STEP);
+      for (; at0 < end; at0 += STEP) {
+        const uint32_t key0 = line.key(a, at0);
+        const int tile_end = (int)line.end_of(a, at0, end);
+        const bool masked = (int)key0 < all0 || (int)key0 + KT - 1 > min(all1, tile_end - 1);
+        Tile x = next;
+        if (at0 + STEP < end) {
+          if constexpr (WIDE) {
+            tile = (tile + 1) % (64 / R);
+            if (tile == 0) places(at0 + STEP);
+          }
+          load(tile);
+          if constexpr (!WIDE) places(at0 + 2 * STEP);
+        }
+        // the scales of the lane's blocks of the runs' keys, and values
+        uint32_t scale[2 * R][LD];
+#pragma unroll
+        for (int y = 0; y < 2 * R; y++)
 #pragma unroll
           for (int j = 0; j < LD; j++)
-            if (x.vs[kb][j] > (uint32_t)E::kMaxScale) {  // a block of NaN becomes zeros
-              odd |= (int)key0 + kb * 16 + c < tile_end;
-              x.v[kb][j] = vw(0);
-              x.vs[kb][j] = 127;
-            }
-      }
-      lds_wave_fence();
+            scale[y][j] = WIDE ? (uint32_t)__builtin_amdgcn_ds_bpermute((y * 16 + c) * 4, (int)x.s[0][j]) : x.s[y][j];
+        if constexpr (WIDE) {
+          // all on their way before the first is waited for
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++)
+          for (int y = 0; y < 2 * R; y++)
 #pragma unroll
-        for (int j = 0; j < LD; j++) {
-          const float f = pack_factor<E>(x.vs[kb][j]);
-#pragma unroll
-          for (int w = 0; w < W; w++)
-            *(v4u *)(lt + (kb * 16 + c) * VROW + ((j * 4 + g) * W + w) * 16) = unpack8<E>(x.v[kb][j][w], f);
+            for (int j = 0; j < LD; j++) scale[y][j] = scale[y][j] >> (DP == 64 ? g / 2 * 8 : g * 8) & 255;
         }
-      lds_wave_fence();
-      if (masked) {
-        uint32_t k0 = key0;
-        asm volatile("" : "+s"(k0));
+        if (masked) {
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++)
+          for (int r = 0; r < R; r++)
 #pragma unroll
-          for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-              const int key = (int)k0 + kb * 16 + g * 4 + i;
-              if ((key < first[nb] && key >= sinks) || key > min(last[nb], tile_end - 1)) sc[nb][kb][i] = neg_inf();
-            }
-      }
-      Op p[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; nb++) {
-        if (a.scores && r0 + nb * 16 + c <= r1) {
-          float *to = a.scores + (((size_t)b * a.kv_heads + kvh) * a.score_rows + r0 + nb * 16 + c) * a.score_keys + key0 + g * 4;
-          *(v4f *)to = sc[nb][0] * a.c;
-          *(v4f *)(to + 16) = sc[nb][1] * a.c;
+            for (int j = 0; j < LD; j++)
+              if (scale[R + r][j] > (uint32_t)E::kMaxScale) {  // a block of NaN becomes zeros
+                odd |= (int)key0 + r * 16 + c < tile_end;
+                x.v[r][j] = vw(0);
+                scale[R + r][j] = 127;
+              }
         }
-        few_softmax<E, DP>(sc[nb], a.c, m[nb], l[nb], o[nb], p[nb]);
+        v4f sc[NB][R];
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+#pragma unroll
+          for (int nb = 0; nb < NB; nb++) sc[nb][r] = v4f{0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < LD; j++) {
+            const float f = pack_factor<E>(scale[r][j]);
+#pragma unroll
+            for (int w = 0; w < W; w++) {
+              const Op k = __builtin_bit_cast(Op, unpack8<E>(x.k[r][j][w], f));
+#pragma unroll
+              for (int nb = 0; nb < NB; nb++) sc[nb][r] = E::mul16(k, q[nb][j * W + w], sc[nb][r]);
+            }
+          }
+        }
+        lds_wave_fence();
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+          for (int j = 0; j < LD; j++) {
+            const float f = pack_factor<E>(scale[R + r][j]);
+#pragma unroll
+            for (int w = 0; w < W; w++) *(v4u *)(lt + (r * 16 + c) * VROW + ((j * 4 + g) * W + w) * 16) = unpack8<E>(x.v[r][j][w], f);
+          }
+        lds_wave_fence();
+        if (masked) {
+          uint32_t k0 = key0;
+          asm volatile("" : "+s"(k0));
+#pragma unroll
+          for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+              for (int i = 0; i < 4; i++) {
+                const int key = (int)k0 + r * 16 + g * 4 + i;
+                if ((key < first[nb] && key >= sinks) || key > min(last[nb], tile_end - 1)) sc[nb][r][i] = neg_inf();
+              }
+        }
+        Op p[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; nb++) {
+          if (a.scores && r0 + nb * 16 + c <= r1) {
+            float *to = a.scores + (((size_t)b * a.kv_heads + kvh) * a.score_rows + r0 + nb * 16 + c) * a.score_keys + key0 + g * 4;
+            *(v4f *)to = sc[nb][0] * a.c;
+            *(v4f *)(to + 16) = sc[nb][1] * a.c;
+          }
+          few_softmax<E, DP>(sc[nb], a.c, m[nb], l[nb], o[nb], p[nb]);
+        }
+        few_values<E, DP, NB, VROW>(lt, g, c, p, o);
       }
-      few_values<E, DP, NB>(lt, g, c, p, o);
+      if (__ballot(odd)) {  // as add_non_finite
+        for (uint32_t k0 = begin + wave * KT; k0 < end; k0 += STEP)
+          for (uint32_t at1 = k0; at1 < min(k0 + KT, end); at1++) {
+            const uint32_t key = line.key(a, at1), pg = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & mask;
+            const uint8_t *p = a.sc.v + (uint64_t)pg * a.sc.page + (slot * a.sc.slot + kvh * a.sc.head);
+#pragma unroll
+            for (int d = 0; d < DP / 16; d++)
+              if (d * 16 < (int)a.dim && p[d / 2] > E::kMaxScale) {
+#pragma unroll
+                for (int nb = 0; nb < NB; nb++)
+                  if (((int)key >= first[nb] || (int)key < sinks) && (int)key <= last[nb]) o[nb][d] += __builtin_nanf("");
+              }
+          }
+      }
     }
-    if (__ballot(odd)) {  // as add_non_finite
-      for (uint32_t k0 = begin + wave * 32; k0 < end; k0 += kKeysStep)
-        for (uint32_t at1 = k0; at1 < min(k0 + 32, end); at1++) {
-          const uint32_t key = line.key(a, at1), pg = min(table[key >> a.pg.shift], a.pg.n_pages - 1), slot = key & ((1u << a.pg.shift) - 1);
-          const uint8_t *p = a.sc.v + (uint64_t)pg * a.sc.page + (slot * a.sc.slot + kvh * a.sc.head);
-#pragma unroll
-          for (int d = 0; d < DP / 16; d++)
-            if (d * 16 < (int)a.dim && p[d / 2] > E::kMaxScale) {
-#pragma unroll
-              for (int nb = 0; nb < NB; nb++)
-                if (((int)key >= first[nb] || (int)key < sinks) && (int)key <= last[nb]) o[nb][d] += __builtin_nanf("");
-            }
-        }
+    if (a.units) {
+      // a unit's parts: the one that it begins with, and the one that it ends with
+      const size_t to = (((size_t)unit * 2 + (first_seg ? 0 : 1)) * a.kv_heads + kvh) * ROWS;
+      few_finish<E, DP, NB>(a, ch, smem, ml, o, m, l, kvh, r0, r1, n == steps, [&](size_t, uint32_t r) { return to + r; });
+    } else {
+      few_finish<E, DP, NB>(a, ch, smem, ml, o, m, l, kvh, r0, r1, a.n_splits == 1, [&](size_t at, uint32_t) { return at * a.n_splits + split; });
+      return;
     }
+    left -= n;
+    pos = 0;
+    b++;
+    __syncthreads();  // the waves' sums have been read
   }
-  few_finish<E, DP, NB>(a, ch, smem, ml, o, m, l, kvh, split, r0, r1);
 }
 
 // Weights from scores computed again: a wave keeps 64 keys in registers, the
@@ -1239,11 +1397,15 @@ hipError_t rows_dim(const AttendArgs &a, hipStream_t st) {
 
 template <class E, int DP, class V>
 hipError_t few_dim(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
-  const uint32_t units = (a.row_tiles * a.n_splits * a.s.n_seq + 7) / 8 * 8;
+  const uint32_t units = ((a.units ? a.units : a.row_tiles * a.n_splits * a.s.n_seq) + 7) / 8 * 8;
   const dim3 grid(units * a.kv_heads);
   if constexpr (V::kPacked) {
-    if (tile_rows == 16) k_attend_few_packed<E, DP, 1><<<grid, 256, 0, st>>>(a);
-    else k_attend_few_packed<E, DP, 2><<<grid, 256, 0, st>>>(a);
+    const uint32_t row = DP / 32;  // a row's scales
+    const bool wide = a.pg.shift >= 4 && a.dim > DP - 32 && ((uintptr_t)a.sc.k | (uintptr_t)a.sc.v | a.sc.page | a.sc.slot | a.sc.head) % row == 0;
+    if (tile_rows == 16 && wide) k_attend_few_packed<E, DP, 1, true><<<grid, 256, 0, st>>>(a);
+    else if (tile_rows == 16) k_attend_few_packed<E, DP, 1, false><<<grid, 256, 0, st>>>(a);
+    else if (wide) k_attend_few_packed<E, DP, 2, true><<<grid, 256, 0, st>>>(a);
+    else k_attend_few_packed<E, DP, 2, false><<<grid, 256, 0, st>>>(a);
   } else {
     if (tile_rows == 16) k_attend_few<E, DP, 1, V><<<grid, 256, 0, st>>>(a);
     else k_attend_few<E, DP, 2, V><<<grid, 256, 0, st>>>(a);

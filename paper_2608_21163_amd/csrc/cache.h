@@ -67,6 +67,7 @@ struct AttendArgs {
   uint32_t row_tiles;        // row tiles of the longest chunk
   uint32_t split;            // keys of one split (a multiple of the keys a workgroup takes at once)
   uint32_t n_splits;         // most splits a row tile has; 1: results are written directly
+  uint32_t units;            // packed pages, few rows: shares of all sequences' keys; 0: splits of each
   float *part;               // partial sums: (token x q_heads x n_splits) x dim
   float2 *part_ml;           // their running maxima (log2 units) and sums
   float *lse2;               // log2-unit lse of every row, for the weights
@@ -185,6 +186,10 @@ constexpr uint32_t kEvictSmall = 8192, kEvictTile = 2048;
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.
 constexpr uint32_t kFewRows = 32, kManyRows = 128;
+// Packed pages, few rows: workgroups of a CU.  64 single tokens over up to 8,192 of 128 elements, 307 MB, heads outside
+// slots and inside: two workgroups 69.8 us and 87.9, three 70.6 and 96.6, four 86.2 and
+// 128.8 (their registers spill); two with tiles of 64 keys a wave 74.4 and 97.4.
+constexpr int packed_groups(int dp, int nb) { return dp > 128 && nb > 1 ? 1 : dp == 64 && nb == 1 ? 3 : 2; }
 // keys of a tile of many rows
 constexpr uint32_t rows_tile(uint32_t dim) { return dim > 128 ? 32 : 64; }
 constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again

@@ -220,14 +220,22 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   if (span <= split) a.n_splits = 1, split = span + 31;
   a.split = (uint32_t)split;
-  const uint64_t groups = few ? (base * a.n_splits + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;
+  // Packed pages, few rows: equal shares of all sequences' keys that fill the chip
+  // once, not splits of each (64 single tokens over up to 8,192: 70 us, splits of 1,024
+  // keys 81).  Up to 512 keys are one launch without parts; every workgroup
+  // adds up all lengths, 64 at a time.
+  if (is_packed && few && span > 512 && s->n_seq <= 1024 && s->n_seq * (span / kKeysStep + 2) < 1u << 31) {
+    const uint32_t groups_of_cu = packed_groups(p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256, tile_rows / 16);
+    a.units = std::max(1u, 256 * groups_of_cu / p.kv_heads);
+  }
+  const uint64_t groups = few ? ((a.units ? (uint64_t)p.kv_heads * a.units : base * a.n_splits) + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;
   if (groups >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "too many sequences, heads and new tokens for one call");
   if (weights_out && ((uint64_t)s->max_k / kAgainKeys + 1) * p.kv_heads * 32 >= kMostGroups) return fail(h, GRAND_E_CAPACITY, "max_k is too large");
 
   Parts w;
   const uint64_t all_rows = (uint64_t)s->n_tokens * p.q_heads;
-  const int w_part = a.n_splits > 1 ? w.add(all_rows * a.n_splits * p.head_dim * 4) : -1;
-  const int w_ml = a.n_splits > 1 ? w.add(all_rows * a.n_splits * 8) : -1;
+  const uint64_t parts = a.units ? 2ull * a.units * p.kv_heads * tile_rows : a.n_splits > 1 ? all_rows * a.n_splits : 0;
+  const int w_part = parts ? w.add(parts * p.head_dim * 4) : -1, w_ml = parts ? w.add(parts * 8) : -1;
   int w_lse = -1, w_scores = -1, w_sums = -1;
   a.row_splits = 1;
   if (weights_out) {
@@ -261,7 +269,7 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   const bool f16 = p.dtype == GRAND_F16;
   if (s->n_tokens && s->max_q) {
     HCHK(h, launch_attend(tile_rows, f16, a, h->stream));
-    if (a.n_splits > 1) HCHK(h, launch_attend_join(f16, a, tile_rows, h->stream));
+    if (parts) HCHK(h, launch_attend_join(f16, a, tile_rows, h->stream));
   }
   if (weights_out && s->max_k) HCHK(h, launch_attend_weights(f16, a, h->stream));
   return GRAND_OK;

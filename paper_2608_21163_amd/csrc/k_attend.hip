@@ -126,6 +126,137 @@ __global__ __launch_bounds__(256) void k_attend_join_short(AttendArgs a, uint32_
   }
 }
 
+// Where part s of a sequence's row lies (share_of): the first unit may have begun
+// with an earlier sequence, the others begin with this one.
+__device__ __forceinline__ size_t unit_part(const AttendArgs &a, const Share &sh, uint32_t u0, uint32_t s, uint32_t kvh, uint32_t r, uint32_t tile_rows) {
+  return (((size_t)(u0 + s) * 2 + (s == 0 && u0 * sh.per != sh.before ? 1 : 0)) * a.kv_heads + kvh) * tile_rows + r;
+}
+
+// The same for shares of all sequences' keys (share_of): a sequence whose keys
+// lie in one unit's share has its results already.
+template <class E, int LQ>
+__global__ __launch_bounds__(256) void k_attend_join_units(AttendArgs a, uint32_t tile_rows) {
+  constexpr int G = 256 / LQ, CHUNK = 1024;
+  __shared__ float2 ml[4];
+  __shared__ float factor[CHUNK];
+  __shared__ v4f acc[256];
+  const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, r = blockIdx.x / a.kv_heads;
+  const Chunk ch = chunk_of(a.s, b, a.err);
+  if (r >= ch.ql * a.group) return;
+  const Share sh = share_of(a, false, [&](uint32_t) { return b; });
+  const uint32_t u0 = sh.before / sh.per, u1 = (sh.before + steps_of(a, b) - 1) / sh.per, n = u1 - u0 + 1;
+  if (n == 1) return;
+  const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
+  const size_t row = (size_t)token * a.q_heads + head;
+  auto place = [&](uint32_t s) { return unit_part(a, sh, u0, s, kvh, r, tile_rows); };
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  float m = neg_inf(), l = 0.f;
+  for (uint32_t s = t; s < n; s += 256) {
+    const float2 x = a.part_ml[place(s)];
+    const float mn = fmaxf(m, x.x);
+    l = (m == neg_inf() ? l : l * ex2(m - mn)) + (x.x == neg_inf() ? x.y : x.y * ex2(x.x - mn));
+    m = mn;
+  }
+#pragma unroll
+  for (int j = 32; j; j >>= 1) {
+    const float m2 = __shfl_xor(m, j, 64), l2 = __shfl_xor(l, j, 64), mn = fmaxf(m, m2);
+    l = (m == neg_inf() ? l : l * ex2(m - mn)) + (m2 == neg_inf() ? l2 : l2 * ex2(m2 - mn));
+    m = mn;
+  }
+  if (lane == 0) ml[wave] = make_float2(m, l);
+  __syncthreads();
+  m = neg_inf(), l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; w++) m = fmaxf(m, ml[w].x);
+#pragma unroll
+  for (int w = 0; w < 4; w++) l += ml[w].x == neg_inf() ? ml[w].y : ml[w].y * ex2(ml[w].x - m);
+  v4f o{0, 0, 0, 0};
+  const int g = t / LQ, c = t % LQ;
+  for (uint32_t s0 = 0; s0 < n; s0 += CHUNK) {
+    const uint32_t m1 = min(n - s0, (uint32_t)CHUNK);
+    if (s0) __syncthreads();
+    for (uint32_t s = t; s < m1; s += 256) {
+      const float x = a.part_ml[place(s0 + s)].x;
+      factor[s] = x == neg_inf() ? 1.f : ex2(x - m);
+    }
+    __syncthreads();
+    if (c * 4 < (int)a.dim) {
+#pragma unroll 4
+      for (uint32_t s = g; s < m1; s += G) o += *(const v4f *)(a.part + place(s0 + s) * a.dim + c * 4) * factor[s];
+    }
+  }
+  acc[t] = o;
+  __syncthreads();
+  const bool some = l > 0.f || l != l;
+  if (t < LQ && t * 4 < (int)a.dim) {
+    for (int i = 1; i < G; i++) o += acc[i * LQ + t];
+    const float inv = some ? 1.f / l : 0.f;
+    typename E::T y[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = (typename E::T)(o[j] * inv);
+    *(uint2 *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + t * 8) = *(uint2 *)y;
+  }
+  if (t == 0) {
+    const float z = some ? m + lg2(l) : neg_inf();
+    if (a.lse) a.lse[row] = z * kLn2;
+    if (a.lse2) a.lse2[row] = z;
+  }
+}
+
+// For few parts a sequence: LQ lanes a row, eight parts at a time.
+template <class E, int LQ>
+__global__ __launch_bounds__(256) void k_attend_join_units_short(AttendArgs a, uint32_t tile_rows) {
+  const uint32_t b = blockIdx.y;
+  const Chunk ch = chunk_of(a.s, b, a.err);
+  const uint32_t x = blockIdx.x * (256 / LQ) + threadIdx.x / LQ, c = threadIdx.x % LQ;
+  const uint32_t kvh = x % a.kv_heads, r = x / a.kv_heads;
+  const Share sh = share_of(a, false, [&](uint32_t) { return b; });
+  const uint32_t u0 = sh.before / sh.per, u1 = (sh.before + steps_of(a, b) - 1) / sh.per, n = u1 - u0 + 1;
+  if (n == 1 || r >= ch.ql * a.group || c * 4 >= a.dim) return;
+  const uint32_t token = ch.r0 + r / a.group, head = kvh * a.group + r % a.group;
+  const size_t row = (size_t)token * a.q_heads + head;
+  float m = neg_inf(), l = 0.f;
+  v4f o{0, 0, 0, 0};
+  for (uint32_t s0 = 0; s0 < n; s0 += kShortSplits) {
+    float2 ml[kShortSplits];
+    v4f part[kShortSplits];
+    float top = m;
+#pragma unroll
+    for (uint32_t s = 0; s < kShortSplits; s++) {
+      ml[s] = make_float2(neg_inf(), 0.f);
+      part[s] = v4f{0, 0, 0, 0};
+      if (s0 + s < n) {
+        const size_t at = unit_part(a, sh, u0, s0 + s, kvh, r, tile_rows);
+        ml[s] = a.part_ml[at];
+        part[s] = *(const v4f *)(a.part + at * a.dim + c * 4);
+      }
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kShortSplits; s++) top = fmaxf(top, ml[s].x);
+    const float f0 = m == neg_inf() ? 1.f : ex2(m - top);
+    l *= f0;
+    o *= f0;
+#pragma unroll
+    for (uint32_t s = 0; s < kShortSplits; s++) {
+      const float f = ml[s].x == neg_inf() ? 1.f : ex2(ml[s].x - top);
+      l += ml[s].y * f;
+      o += part[s] * f;
+    }
+    m = top;
+  }
+  const bool some = l > 0.f || l != l;
+  const float inv = some ? 1.f / l : 0.f;
+  typename E::T y[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) y[j] = (typename E::T)(o[j] * inv);
+  *(uint2 *)(a.out.p + (int64_t)token * a.out.token + (int64_t)head * a.out.head + c * 8) = *(uint2 *)y;
+  if (c == 0) {
+    const float z = some ? m + lg2(l) : neg_inf();
+    if (a.lse) a.lse[row] = z * kLn2;
+    if (a.lse2) a.lse2[row] = z;
+  }
+}
+
 // Weights from stored scores: a thread sums four keys' weights over the rows.
 // 50 MB of scores and weights in 12 us; computing the scores again would read
 // half of the cache.
@@ -190,6 +321,19 @@ hipError_t launch_attend(uint32_t tile_rows, bool f16, const AttendArgs &a, hipS
 template <class E>
 static hipError_t join_type(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
   const uint32_t rows = a.s.max_q * a.q_heads;
+  if (a.units && a.units <= 4 * a.s.n_seq) {  // some sequences may have more than eight parts, few have
+    if (a.dim <= 64) k_attend_join_units_short<E, 16><<<dim3((rows + 15) / 16, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    else if (a.dim <= 128) k_attend_join_units_short<E, 32><<<dim3((rows + 7) / 8, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    else k_attend_join_units_short<E, 64><<<dim3((rows + 3) / 4, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
+    return hipGetLastError();
+  }
+  if (a.units) {
+    const dim3 grid(rows, a.s.n_seq);
+    if (a.dim <= 64) k_attend_join_units<E, 16><<<grid, 256, 0, st>>>(a, tile_rows);
+    else if (a.dim <= 128) k_attend_join_units<E, 32><<<grid, 256, 0, st>>>(a, tile_rows);
+    else k_attend_join_units<E, 64><<<grid, 256, 0, st>>>(a, tile_rows);
+    return hipGetLastError();
+  }
   if (a.n_splits <= kShortSplits) {
     if (a.dim <= 64) k_attend_join_short<E, 16><<<dim3((rows + 15) / 16, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
     else if (a.dim <= 128) k_attend_join_short<E, 32><<<dim3((rows + 7) / 8, a.s.n_seq), 256, 0, st>>>(a, tile_rows);
