@@ -13,6 +13,7 @@
 #pragma once
 #include "cache.h"
 #include "packed.h"
+#include "wave.h"
 
 namespace gr {
 namespace {
@@ -1207,7 +1208,7 @@ __global__ __launch_bounds__(256, packed_groups(DP, NB)) void k_attend_few_packe
 // of 32 heads over 32,768: 0.60 to 0.65 ms (beside 0.65 to 0.70 in the same
 // runs: 32 keys a wave 0.80, tiles of 32 rows 0.70 to 0.75).
 // Where that gives too few workgroups the rows are split, and their sums are
-// added by another launch.
+// added by another launch (which a window needs too, for the tiles without rows).
 struct AgainRows {
   uint32_t lo, hi, per, n;  // rows that see a key of the tile, rows of a split, splits that have any
 };
@@ -1225,22 +1226,33 @@ __device__ __forceinline__ AgainRows again_rows(const AttendArgs &a, const Chunk
   return r;
 }
 
+// The keys of workgroup i's tile.  With a window only the tiles that it reaches
+// from some row, and those of the first tokens, have workgroups (again_tiles):
+// seven chunks of up to 300 tokens, 12 heads of 64 elements, windows of 1,000 over up to
+// 5,000, 1,300 workgroups instead of 3,400, 40 us -> 38.
+template <class V>
+__device__ __forceinline__ uint32_t again_key(const AttendArgs &a, const Chunk &ch, uint32_t i) {
+  if (!a.window) return i * kAgainKeys;
+  const uint32_t front = ((uint32_t)sinks_of<V>(a) + kAgainKeys - 1) / kAgainKeys, base = (uint32_t)max(0, ch.p0 - (int)a.window + 1) / kAgainKeys;
+  return (i < front || base <= front ? i : base + i - front) * kAgainKeys;
+}
+
 template <class E, int DP, class V>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendArgs a) {
+__global__ __launch_bounds__(256, DP > 128 ? 1 : DP > 64 ? 2 : 3) void k_weights_again(AttendArgs a) {
   constexpr int kStride = DP * 2 + 16, RT = DP > 128 ? 32 : 64;  // rows of a tile
   __shared__ __align__(16) uint8_t lq[2][RT * kStride];
   __shared__ float lz[2][RT];
   __shared__ float total[kAgainKeys];
   const uint32_t b = blockIdx.y, kvh = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const uint32_t part = rest % a.row_splits, kt = rest / a.row_splits;
+  const uint32_t part = rest % a.row_splits;
   const Chunk ch = chunk_of(a.s, b, a.err);
-  const uint32_t key0 = kt * kAgainKeys;
+  const uint32_t key0 = again_key<V>(a, ch, rest / a.row_splits);
   if (key0 >= ch.kl) return;
   const AgainRows range = again_rows<V>(a, ch, key0);
   const float *win = a.win.p + (int64_t)b * a.win.seq + (int64_t)kvh * a.win.head;
   float *wout = a.wout.p + (int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head;
   if (part >= range.n) {
-    if (a.row_splits == 1 && key0 + threadIdx.x < ch.kl) wout[key0 + threadIdx.x] = win[key0 + threadIdx.x];
+    if (!a.row_sums && key0 + threadIdx.x < ch.kl) wout[key0 + threadIdx.x] = win[key0 + threadIdx.x];
     return;
   }
   const uint32_t r_lo = range.lo + part * range.per, r_hi = min(range.hi, r_lo + range.per);
@@ -1334,8 +1346,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
     const int p_lo = ch.p0 + (int)first_tok, p_hi = p_lo + (int)((RT - 1) / a.group) + 1;
     // (rows past the last are zeros, which an infinite key makes NaN of)
     const bool masked = (a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window) || r0 + RT > r_hi;
+    // (no row sees a key of the wave: most of a tile of first tokens)
+    const bool none = (a.causal && wkey > p_hi) || (a.window && wkey + 63 <= p_lo - (int)a.window && wkey >= sinks_of<V>(a));
 #pragma unroll
-    for (int rb = 0; rb < RT / 32; rb++) {
+    for (int rb = 0; rb < RT / 32 && !none; rb++) {
       v16f s[2] = {v16f{}, v16f{}};
 #pragma unroll
       for (int x = 0; x < DP / 16; x++) {
@@ -1371,19 +1385,28 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_weights_again(AttendA
       first_tok++;
     }
   }
+  // Sums over the 32 columns of 32 values, each half of the wave its own: at every
+  // step a lane hands on the half of its values that it does not keep, and ends
+  // with the sum of value `col` (all sums by themselves: 160 trips through LDS, 9 us).
+  float y[16];
 #pragma unroll
-  for (int kb = 0; kb < 2; kb++)
+  for (int i = 0; i < 16; i++) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[0][i]), __float_as_uint(acc[1][i]), false, false);
+    y[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      float x = acc[kb][i];
+  for (int j = 8; j; j >>= 1)
 #pragma unroll
-      for (int j = 16; j; j >>= 1) x += __shfl_xor(x, j, 64);
-      if (col == 0) total[wave * 64 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4] = x;
+    for (int i = 0; i < j; i++) {
+      const bool upper = lane & j;
+      const float keep = upper ? y[i + j] : y[i], give = upper ? y[i] : y[i + j];
+      y[i] = keep + xshfl(give, j);
     }
+  total[wave * 64 + col / 16 * 32 + (col % 16 / 4) * 8 + half * 4 + col % 4] = y[0];
   __syncthreads();
   const uint32_t key = key0 + t;
   if (key < ch.kl) {
-    if (a.row_splits == 1) wout[key] = win[key] + total[t];
+    if (!a.row_sums) wout[key] = win[key] + total[t];
     else a.row_sums[(((size_t)part * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key] = total[t];
   }
 }
@@ -1432,8 +1455,7 @@ hipError_t attend_type(uint32_t tile_rows, const AttendArgs &a, hipStream_t st) 
 
 template <class E, class V>
 hipError_t weights_type(const AttendArgs &a, hipStream_t st) {
-  const uint32_t tiles = (a.s.max_k + kAgainKeys - 1) / kAgainKeys;
-  const dim3 grid(tiles * a.row_splits * a.kv_heads, a.s.n_seq);
+  const dim3 grid(again_tiles(a) * a.row_splits * a.kv_heads, a.s.n_seq);
   if (a.dim <= 64) k_weights_again<E, 64, V><<<grid, 256, 0, st>>>(a);
   else if (a.dim <= 96) k_weights_again<E, 96, V><<<grid, 256, 0, st>>>(a);
   else if (a.dim <= 128) k_weights_again<E, 128, V><<<grid, 256, 0, st>>>(a);

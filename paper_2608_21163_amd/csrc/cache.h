@@ -74,7 +74,7 @@ struct AttendArgs {
   float *scores;             // log2-unit scores by (sequence, key/value head, row, key); null: recomputed
   uint32_t score_rows, score_keys;
   uint32_t row_splits;       // where they are recomputed: splits of the rows, whose sums are
-  float *row_sums;           // by (split, sequence, key/value head, key) if there is more than one
+  float *row_sums;           // by (split, sequence, key/value head, key) if there is more than one, or a window
   CacheErr *err;
 };
 
@@ -193,6 +193,12 @@ constexpr int packed_groups(int dp, int nb) { return dp > 128 && nb > 1 ? 1 : dp
 // keys of a tile of many rows
 constexpr uint32_t rows_tile(uint32_t dim) { return dim > 128 ? 32 : 64; }
 constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again
+// Tiles of keys that some row of a sequence may see.
+inline uint32_t again_tiles(const AttendArgs &a) {
+  const uint64_t all = ((uint64_t)a.s.max_k + kAgainKeys - 1) / kAgainKeys;
+  const uint64_t seen = ((uint64_t)a.sinks + kAgainKeys - 1) / kAgainKeys + ((uint64_t)a.window + a.s.max_q) / kAgainKeys + 2;
+  return (uint32_t)(a.window && seen < all ? seen : all);
+}
 constexpr uint32_t kKeysStep = 128;  // keys that a workgroup of few rows takes at once (four waves of 32)
 
 // (16-bit pages without first tokens; the others are called from there)

@@ -357,7 +357,7 @@ hipError_t launch_attend_weights(bool f16, const AttendArgs &a, hipStream_t st) 
   }
   const hipError_t e = a.sc.k ? launch_weights_packed(f16, a, st) : a.sinks ? launch_weights_sinks(f16, a, st)
                        : f16 ? weights_type<F16, Whole>(a, st) : weights_type<Bf16, Whole>(a, st);
-  if (e != hipSuccess || a.row_splits == 1) return e;
+  if (e != hipSuccess || !a.row_sums) return e;
   k_weights_add<<<dim3((a.s.max_k + kAgainKeys - 1) / kAgainKeys * a.kv_heads, a.s.n_seq), 256, 0, st>>>(a);
   return hipGetLastError();
 }
