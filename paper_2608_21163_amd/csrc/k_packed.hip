@@ -18,20 +18,20 @@ struct Bf16 : PackBf16 {
   typedef __bf16 T;
   // the fp32 bits of the magnitude with these 15 bits
   static __device__ __forceinline__ uint32_t magnitude(uint32_t u) { return u << 16; }
+  // two products and a sum, in 32 bits
+  static __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, a), __builtin_bit_cast(v2bf, b), c, false);
+  }
 };
 struct F16 : PackF16 {
   typedef _Float16 T;
   static __device__ __forceinline__ uint32_t magnitude(uint32_t u) {
     return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)u));
   }
-};
-template <class E> __device__ __forceinline__ void widen8(v4u x, float *f) {
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    f[2 * i] = (float)__builtin_bit_cast(typename E::T, (uint16_t)x[i]);
-    f[2 * i + 1] = (float)__builtin_bit_cast(typename E::T, (uint16_t)(x[i] >> 16));
+  static __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b), c, false);
   }
-}
+};
 // 32 codes as fp32 values.
 template <class E> __device__ __forceinline__ void unpack32(v4u x, float factor, float *f) {
 #pragma unroll
@@ -129,24 +129,29 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 // (m, l) of two parts of a softmax, in log2 units; m may be -inf (nothing).
 __device__ __forceinline__ float part_scale(float m, float top) { return m == neg_inf() ? 1.f : ex2(m - top); }
 
-// Attention over listed slots, as for 16-bit pages: a workgroup per (sequence, query
-// head), here a lane per block of a row, so that DP / 32 lanes read one.
-template <class E, int DP>
+// Attention over listed slots, as for 16-bit pages, here a lane per block of a row, so
+// that DP / 32 lanes read one.  WAVES share a (sequence, query head)'s list: four, or
+// one where there are many lists that would not fill a workgroup's first loads, as the start and
+// the end of a list then count for more than its rows (256 x 32 lists of 64 ids: 45 us, with
+// four waves 82; of 256 ids 158 and 149; 64 x 32 of 64: 17 and 26).  Rows of 64
+// bytes that lie anywhere are bound by their number: 256 x 32 lists of 256 take
+// 152, 158 and 170 us at 64, 128 and 256 elements, in a pool of 4,096 slots 52;
+// keys and values are two places each, codes and scales.
+template <class E, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
-  constexpr int LPR = DP / 32, GROUPS = 64 / LPR, U = 4;
+  constexpr int LPR = DP / 32, GROUPS = 64 / LPR, U = 4, STEP = WAVES * GROUPS;
   __shared__ float2 sml[4];
   __shared__ float sacc[4][DP];
-  const uint32_t b = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads, kvh = head / a.group;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane / LPR, c = lane % LPR;
+  const int t = threadIdx.x, lane = t & 63, wave = t / 64 % WAVES, g = lane / LPR, c = lane % LPR;
+  const uint32_t list = blockIdx.x * (4 / WAVES) + __builtin_amdgcn_readfirstlane(t / 64 / WAVES);
+  if (list >= a.n_seq * a.q_heads) return;
+  const uint32_t b = list / a.q_heads, head = list % a.q_heads, kvh = head / a.group;
   const bool in = c * 32 < (int)a.dim;
-  float q[32];
+  v4u q[4];
 #pragma unroll
   for (int w = 0; w < 4; w++) {
-    v4u x{0, 0, 0, 0};
-    if (c * 32 + w * 8 < (int)a.dim) x = *(const v4u *)(a.q.p + (int64_t)b * a.q.token + (int64_t)head * a.q.head + c * 64 + w * 16);
-    widen8<E>(x, q + 8 * w);
-#pragma unroll
-    for (int i = 0; i < 8; i++) q[8 * w + i] *= a.c;
+    q[w] = v4u{0, 0, 0, 0};
+    if (c * 32 + w * 8 < (int)a.dim) q[w] = *(const v4u *)(a.q.p + (int64_t)b * a.q.token + (int64_t)head * a.q.head + c * 64 + w * 16);
   }
   const uint32_t *ids = a.ids + (int64_t)b * a.ids_seq + (int64_t)head * a.ids_head;
   const uint64_t slots = (uint64_t)a.pg.n_pages << a.pg.shift;
@@ -154,13 +159,16 @@ __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
   float m = neg_inf(), l = 0.f, acc[32];
 #pragma unroll
   for (int i = 0; i < 32; i++) acc[i] = 0.f;
-  for (uint32_t j0 = wave * GROUPS + g; j0 < a.k; j0 += 4 * GROUPS * U) {
+  const uint32_t j0 = wave * GROUPS + g;
+  uint32_t next[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) next[u] = j0 + u * STEP < a.k ? ids[j0 + u * STEP] : kInvalid;
+  for (uint32_t j1 = 0; j1 < a.k; j1 += STEP * U) {
     uint32_t id[U], ks[U], vs[U];
     v4u kx[U], vx[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const uint32_t j = j0 + u * 4 * GROUPS;
-      id[u] = j < a.k ? ids[j] : kInvalid;
+      id[u] = next[u];
       if (id[u] != kInvalid && id[u] >= slots) {
         cache_err(a.err, kCacheId, b);
         id[u] = kInvalid;
@@ -180,20 +188,25 @@ __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
         vs[u] = a.sc.v[sc];
       }
     }
+#pragma unroll
+    for (int u = 0; u < U; u++) next[u] = j1 + j0 + (U + u) * STEP < a.k ? ids[j1 + j0 + (U + u) * STEP] : kInvalid;
     float s[U], top = m;
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      float f[32], x = 0.f, y = 0.f;
-      unpack32<E>(kx[u], pack_factor<E>(ks[u]), f);
+      float x = 0.f, y = 0.f;
+      const float f = pack_factor<E>(ks[u]);
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        x = __builtin_fmaf(f[i], q[i], x);
-        y = __builtin_fmaf(f[i + 1], q[i + 1], y);
+      for (int w = 0; w < 4; w++) {
+        const v4u k = unpack8<E>(kx[u][w], f);
+        x = E::dot2(k[0], q[w][0], x);
+        y = E::dot2(k[1], q[w][1], y);
+        x = E::dot2(k[2], q[w][2], x);
+        y = E::dot2(k[3], q[w][3], y);
       }
       x += y;
 #pragma unroll
       for (int j = LPR / 2; j; j >>= 1) x += xshfl(x, j);
-      s[u] = id[u] == kInvalid ? neg_inf() : x;
+      s[u] = id[u] == kInvalid ? neg_inf() : x * a.c;
       top = fmaxf(top, s[u]);
     }
     const float base = top == neg_inf() ? 0.f : top, scale = m == neg_inf() ? 1.f : ex2(m - base);
@@ -220,31 +233,61 @@ __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
 #pragma unroll
   for (int i = 0; i < 32; i++) acc[i] *= f;
 #pragma unroll
-  for (int j = LPR; j < 64; j <<= 1) {
-    l += xshfl(l, j);
+  for (int j = LPR; j < 64; j <<= 1) l += xshfl(l, j);
+  // at every step a lane hands on the half of its values that it does not keep,
+  // and ends with the wave's sums of 32 / GROUPS elements of its block
 #pragma unroll
-    for (int i = 0; i < 32; i++) acc[i] += xshfl(acc[i], j);
+  for (int i = 0; i < 16; i++) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i]), __float_as_uint(acc[i + 16]), false, false);
+    acc[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
-  if (g == 0) {
 #pragma unroll
-    for (int i = 0; i < 32; i++) sacc[wave][c * 32 + i] = acc[i];
+  for (int i = 0; i < 8; i++) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i]), __float_as_uint(acc[i + 8]), false, false);
+    acc[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
-  if (lane == 0) sml[wave] = make_float2(top, l);
+  int first = lane / 32 * 16 + lane / 16 % 2 * 8;
+#pragma unroll
+  for (int j = 8, n = 4; j >= LPR; j >>= 1, n >>= 1) {
+    const bool upper = lane & j;
+    if (upper) first += n;
+#pragma unroll
+    for (int i = 0; i < n; i++) {
+      const float keep = upper ? acc[i + n] : acc[i], give = upper ? acc[i] : acc[i + n];
+      acc[i] = keep + xshfl(give, j);
+    }
+  }
   const size_t row = (size_t)b * a.q_heads + head;
-  // read before the barrier: lse may be the same memory, and one thread writes it
+  const uint8_t *prior = a.prior.p + (int64_t)b * a.prior.token + (int64_t)head * a.prior.head;
+  typename E::T *out = (typename E::T *)(a.out.p + (int64_t)b * a.out.token + (int64_t)head * a.out.head);
+  // the earlier result stands for one row of weight 1 at its lse
+  // (read before a barrier, or by the wave that writes: lse may be the same memory)
   const float z0 = a.prior.p ? a.prior_lse[row] * (1.f / kLn2) : neg_inf();
+  if constexpr (WAVES == 1) {
+    const float mm = fmaxf(top, z0), w0 = z0 == neg_inf() ? 0.f : ex2(z0 - mm), w = part_scale(top, mm), sum = w0 + l * w;
+    const bool some = sum > 0.f || sum != sum;
+#pragma unroll
+    for (int i = 0; i < 32 / GROUPS; i++) {
+      const int at = c * 32 + first + i;
+      if (at < (int)a.dim) {
+        const float o0 = a.prior.p ? (float)((const typename E::T *)prior)[at] : 0.f;
+        const float o = (w0 == 0.f ? 0.f : w0 * o0) + acc[i] * w;
+        out[at] = (typename E::T)(some ? o / sum : 0.f);
+      }
+    }
+    if (lane == 0 && a.lse) a.lse[row] = some ? (mm + lg2(sum)) * kLn2 : neg_inf();
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 32 / GROUPS; i++) sacc[wave][c * 32 + first + i] = acc[i];
+  if (lane == 0) sml[wave] = make_float2(top, l);
   __syncthreads();
   if (t >= DP) return;
-  float o0 = 0.f;
-  if (a.prior.p) {
-    if (t < (int)a.dim)
-      o0 = (float)*(const typename E::T *)(a.prior.p + (int64_t)b * a.prior.token + (int64_t)head * a.prior.head + t * 2);
-  }
+  const float o0 = a.prior.p && t < (int)a.dim ? (float)((const typename E::T *)prior)[t] : 0.f;
   float mm = z0;
 #pragma unroll
   for (int w = 0; w < 4; w++) mm = fmaxf(mm, sml[w].x);
-  // the earlier result stands for one row of weight 1 at its lse
-  float w0 = z0 == neg_inf() ? 0.f : ex2(z0 - mm);
+  const float w0 = z0 == neg_inf() ? 0.f : ex2(z0 - mm);
   float sum = w0, o = w0 == 0.f ? 0.f : w0 * o0;
 #pragma unroll
   for (int w = 0; w < 4; w++) {
@@ -253,25 +296,26 @@ __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
     o += sacc[w][t] * s;
   }
   const bool some = sum > 0.f || sum != sum;
-  if (t < (int)a.dim)
-    *(typename E::T *)(a.out.p + (int64_t)b * a.out.token + (int64_t)head * a.out.head + t * 2) =
-        (typename E::T)(some ? o / sum : 0.f);
+  if (t < (int)a.dim) out[t] = (typename E::T)(some ? o / sum : 0.f);
   if (t == 0 && a.lse) a.lse[row] = some ? (mm + lg2(sum)) * kLn2 : neg_inf();
 }
 
-template <class E>
+template <class E, int WAVES>
 hipError_t ids_type(const IdsArgs &a, hipStream_t st) {
-  const dim3 grid(a.n_seq * a.q_heads);
-  if (a.dim <= 64) k_ids_packed<E, 64><<<grid, 256, 0, st>>>(a);
-  else if (a.dim <= 128) k_ids_packed<E, 128><<<grid, 256, 0, st>>>(a);
-  else k_ids_packed<E, 256><<<grid, 256, 0, st>>>(a);
+  const uint32_t lists = a.n_seq * a.q_heads;
+  const dim3 grid((lists + 4 / WAVES - 1) / (4 / WAVES));
+  if (a.dim <= 64) k_ids_packed<E, 64, WAVES><<<grid, 256, 0, st>>>(a);
+  else if (a.dim <= 128) k_ids_packed<E, 128, WAVES><<<grid, 256, 0, st>>>(a);
+  else k_ids_packed<E, 256, WAVES><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_ids_packed(bool f16, const IdsArgs &a, hipStream_t st) {
-  return f16 ? ids_type<F16>(a, st) : ids_type<Bf16>(a, st);
+  const uint32_t pass = a.dim <= 64 ? 512 : a.dim <= 128 ? 256 : 128;  // ids that four waves ask for at once
+  if (a.n_seq * a.q_heads >= 2048 && a.k < pass) return f16 ? ids_type<F16, 1>(a, st) : ids_type<Bf16, 1>(a, st);
+  return f16 ? ids_type<F16, 4>(a, st) : ids_type<Bf16, 4>(a, st);
 }
 
 hipError_t launch_append_packed(const AppendArgs &a, hipStream_t st) {

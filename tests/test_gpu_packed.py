@@ -427,3 +427,46 @@ def test_long_histories_of_first_tokens():
         c = make("f16", 4, 1, 64, 16, qs=qs, ks=ks, seed=1)
         weighted(c, window=2100, sinks=1500)
         weighted(packed(c), window=2100, sinks=1500)
+
+
+@pytest.mark.parametrize("dim,n", [(64, 70), (128, 255), (128, 256), (128, 300), (256, 60)])
+def test_many_lists(dim, n):
+    """Enough lists for a wave each, in place over an earlier result, some lists empty."""
+    import torch
+
+    say(f"[packed ids] 300 x 8 lists of {n}, {dim}")
+    c = packed(make("bf16", 8, 2, dim, 16, qs=(1,), ks=(600,), seed=n))
+    r = np.random.default_rng(n)
+    slots = np.array([int(c["table"][0, p // 16]) * 16 + p % 16 for p in range(600)])
+    b = 300
+    q = torch.from_numpy(r.standard_normal((b, 8, dim)) * 2).to(c["q"].dtype)
+    ids = slots[r.integers(0, 600, (b, 8, n))].astype(np.uint32)
+    ids[7], ids[9, 3, 5:], ids[r.random(ids.shape) < 0.05] = INVALID, INVALID, INVALID
+    po, pz = torch.from_numpy(r.standard_normal((b, 8, dim))).to(q.dtype), torch.from_numpy(r.standard_normal((b, 8))).float()
+    pz[7, 2] = -math.inf
+    out, lse = po.cuda(), pz.cuda()
+    cache = cache_for(c)
+    cache.attend_ids(q.cuda(), c["k_pages"], c["v_pages"], torch.from_numpy(ids.astype(np.int32)).cuda(), prior=(out, lse), out=out, lse=lse)
+    cache.check()
+    cache.close()
+    total = c["k_pages"].codes.shape[0] * 16
+    flat = [np.zeros((total, 2, dim)) for _ in range(2)]
+    for x, rows in zip(flat, (c["keys"], c["vals"])):
+        x[slots] = rows[0].numpy()
+    some = [0, 7, 9, 133, 299]
+    want, z, bound, z_err = ids_ref(q[some].double().numpy(), *flat, ids[some], dim ** -0.5, (po[some].double().numpy(), pz[some].double().numpy()))
+    o, l = out.double().cpu().numpy()[some], lse.double().cpu().numpy()[some]
+    assert (np.abs(o - want) <= bound("bf16")).all()
+    empty = np.isneginf(z)
+    assert np.array_equal(np.isneginf(l), empty) and empty.any()
+    assert (np.abs(np.where(empty, 0, l) - np.where(empty, 0, z)) <= z_err + 1e-30).all()
+    with_ids = ids.astype(np.int32)
+    with_ids[11, 2, 1] = total          # a slot outside the pool: passed over, and reported
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ID
+    cache = cache_for(c)
+    cache.attend_ids(q.cuda(), c["k_pages"], c["v_pages"], torch.from_numpy(with_ids).cuda())
+    with pytest.raises(GrandError) as e:
+        cache.check()
+    assert e.value.code == E_ID
+    cache.close()
