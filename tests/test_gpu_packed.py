@@ -339,6 +339,41 @@ def test_listed_slots(dtype, layout, hq, hk, dim, page, n, prior):
     assert (np.abs(np.where(empty, 0, l) - np.where(empty, 0, z)) <= z_err + 1e-30).all()
 
 
+def ragged(n, most_q, longest, seed, empty=0.2):
+    """n sequences, some of no new tokens, some of no tokens at all."""
+    r = np.random.default_rng(seed)
+    qs = np.where(r.random(n) < empty, 0, r.integers(1, most_q + 1, n))
+    ks = np.where(r.random(n) < empty, qs, qs + r.integers(0, longest, n))
+    qs[n // 3], qs[-1] = 1, 1
+    ks[n // 3], ks[-1] = 1, longest
+    return tuple(qs.tolist()), tuple(ks.tolist())
+
+
+MANY = [(70, 1, 900), (129, 4, 700), (1024, 1, 520), (1025, 1, 520), (3, 2, 20_000)]
+
+
+@pytest.mark.parametrize("n,most_q,longest", MANY)
+@pytest.mark.parametrize("dtype,hq,hk,dim,window,sinks", [("bf16", 4, 2, 128, 0, 0), ("f16", 4, 1, 64, 0, 0), ("bf16", 2, 2, 64, 300, 40)])
+def test_many_sequences(n, most_q, longest, dtype, hq, hk, dim, window, sinks):
+    """Few rows of many sequences share the card by their keys: empty and short ones among long ones, and one long one last."""
+    say(f"[packed many] {n} of up to {most_q} tokens and {longest} keys, {dtype} {hq}/{hk} x {dim}, window {window} {sinks}")
+    qs, ks = ragged(n, most_q, longest, n + most_q)
+    c = packed(make(dtype, hq, hk, dim, 16, qs=qs, ks=ks, seed=n))
+    weighted(c, window=window, sinks=sinks)
+    compare(c, *run(c, max_q=most_q + 1, max_k=c["table"].shape[1] * 16, window=window, sinks=sinks), window=window, sinks=sinks)
+
+
+def test_one_long_sequence_among_short_ones():
+    """... and alone, in one page order after the other."""
+    for qs, ks in (((1,) * 64, (3,) * 40 + (12_000,) + (2,) * 23), ((1,), (30_001,)), ((0,) * 63 + (1,), (0,) * 63 + (9000,)),
+                   ((0,) * 5, (700,) * 5)):
+        c = packed(make("bf16", 8, 2, 128, 16, qs=qs, ks=ks, seed=len(qs)))
+        if sum(qs):
+            weighted(c)
+        else:
+            run(c)
+
+
 # ------------------------------------------------------------ first tokens
 @pytest.mark.parametrize("kind", ["whole", "packed"])
 @pytest.mark.parametrize("window,sinks", [(1, 1), (7, 4), (32, 32), (33, 64), (100, 5), (40, 65), (100000, 3), (40, 100000)])
@@ -427,6 +462,27 @@ def test_long_histories_of_first_tokens():
         c = make("f16", 4, 1, 64, 16, qs=qs, ks=ks, seed=1)
         weighted(c, window=2100, sinks=1500)
         weighted(packed(c), window=2100, sinks=1500)
+
+
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+@pytest.mark.parametrize("qs,ks,window,sinks", [((70, 1, 33), (4000, 700, 33), 200, 10), ((40,), (5000,), 64, 300), ((64, 64), (2500, 1000), 1, 257),
+                                                ((300,), (3500,), 500, 0), ((40, 40), (1800, 1800), 1700, 3)])
+def test_weights_far_from_the_window(kind, qs, ks, window, sinks):
+    """Keys that no row of a chunk sees lie between the first tokens and the windows: their weights stay."""
+    say(f"[weights] {kind} {qs} {ks} window {window} {sinks}")
+    for dtype, hq, hk, dim in (("bf16", 4, 2, 64), ("f16", 5, 1, 128)):
+        c = make(dtype, hq, hk, dim, qs=qs, ks=ks, seed=window)
+        weighted(packed(c) if kind == "packed" else c, window=window, sinks=sinks)
+        weighted(packed(c) if kind == "packed" else c, window=window, sinks=sinks, causal=False)
+
+
+@pytest.mark.parametrize("n,most_q", [(127, 1), (128, 1), (130, 3)])
+def test_first_tokens_of_many_sequences(n, most_q):
+    """A workgroup a sequence and head where there are enough of them."""
+    qs, ks = ragged(n, most_q, 1500, n)
+    for dtype, hq, hk, dim in (("bf16", 4, 2, 64), ("f16", 2, 2, 128)):
+        c = make(dtype, hq, hk, dim, qs=qs, ks=ks, seed=n)
+        weighted(c, window=600, sinks=30)
 
 
 @pytest.mark.parametrize("dim,n", [(64, 70), (128, 255), (128, 256), (128, 300), (256, 60)])
