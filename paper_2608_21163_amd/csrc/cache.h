@@ -161,10 +161,12 @@ struct RefArgs {
   uint32_t *blk;             // set bits by block of kRefPages pages
   uint32_t *rank, *total;    // compact: a moving page's place in the lists; pages in use
   uint32_t *need;            // grow: pages a sequence needs, bit 31: one of them for a copy
-  uint64_t *start;           // grow: pages that the sequences before it need
+  uint32_t *at;              // grow: the place in its row of the first page that a sequence gets
+  uint32_t *start;           // grow: pages that the sequences before it need (more than kFewSeqs)
   CacheErr *err;
 };
 constexpr uint32_t kRefPages = 2048;  // pages of a workgroup
+constexpr uint32_t kFewSeqs = 2048;   // sequences whose needs every workgroup adds up
 
 struct CopyArgs {
   PagesView pg;

@@ -147,105 +147,94 @@ __global__ __launch_bounds__(256) void k_grow_need(RefArgs a) {
   if (b >= a.s.n_seq) return;
   const GrowSeq g = grow_seq(a, b);
   if (!g.fits) cache_err(a.err, kCacheLen, b);
-  uint32_t need = g.n1 - g.n0;
+  uint32_t need = g.n1 - g.n0, from = kInvalid;
   if (g.fits && a.n_new[b] && (g.len & ((1u << a.shift) - 1))) {
     const uint32_t id = a.s.table[(int64_t)b * a.s.table_stride + g.n0 - 1];
     if (id >= a.n_pages) cache_err(a.err, kCachePage, b);
-    else if (a.refs_in[id] > 1) need = (need + 1) | kOneCopy;
+    else if (a.refs_in[id] > 1) need = (need + 1) | kOneCopy, from = id;
   }
   a.need[b] = need;
+  a.at[b] = g.n0 - (need & kOneCopy ? 1 : 0);
+  a.src[b] = from;
 }
 
-// Where each sequence's pages begin among the free ones.
-__global__ __launch_bounds__(1024) void k_grow_start(RefArgs a) {
-  __shared__ uint64_t sum[16];
-  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  uint64_t base = 0;
-  for (uint32_t b0 = 0; b0 < a.s.n_seq; b0 += 1024) {
-    const uint32_t b = b0 + t;
-    const uint64_t n = b < a.s.n_seq ? a.need[b] & ~kOneCopy : 0;
-    uint64_t s = n;
+// Sums that stay at 2^32 - 1.
+__device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return x + y < x ? ~0u : x + y; }
+__device__ __forceinline__ uint32_t wave_scan_sat(uint32_t x, int lane) {
 #pragma unroll
-    for (int j = 1; j < 64; j <<= 1) {
-      const uint64_t x = __shfl_up((unsigned long long)s, j, 64);
-      if ((int)lane >= j) s += x;
-    }
+  for (int j = 1; j < 64; j <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_up((int)x, j, 64);
+    if (lane >= j) x = add_sat(x, y);
+  }
+  return x;
+}
+
+// Where each sequence's pages begin among the free ones: start[b], and their
+// number at start[n_seq].  A workgroup of NT threads.
+template <int NT>
+__device__ __forceinline__ void grow_starts(const RefArgs &a, uint32_t *start) {
+  __shared__ uint32_t sum[NT / 64];
+  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  uint32_t base = 0;
+  for (uint32_t b0 = 0; b0 < a.s.n_seq; b0 += NT) {
+    const uint32_t b = b0 + t, n = b < a.s.n_seq ? a.need[b] & ~kOneCopy : 0, s = wave_scan_sat(n, lane);
     if (lane == 63) sum[wave] = s;
     __syncthreads();
-    uint64_t before = base;
-    for (uint32_t w = 0; w < 16; w++) {
-      if (w < wave) before += sum[w];
-      base += sum[w];
+    uint32_t before = base;
+    for (uint32_t w = 0; w < NT / 64; w++) {
+      if (w < wave) before = add_sat(before, sum[w]);
+      base = add_sat(base, sum[w]);
     }
-    if (b < a.s.n_seq) a.start[b] = before + s - n;
+    const uint32_t up = (uint32_t)__shfl_up((int)s, 1, 64);
+    if (b < a.s.n_seq) start[b] = add_sat(before, lane ? up : 0);
     __syncthreads();
   }
+  if (t == 0) start[a.s.n_seq] = base;
+  __syncthreads();
 }
+__global__ __launch_bounds__(1024) void k_grow_start(RefArgs a) { grow_starts<1024>(a, a.start); }
 
+// Up to kFewSeqs sequences every workgroup adds up the needs itself: a launch less.
+template <bool FEW>
 __global__ __launch_bounds__(256) void k_grow_give(RefArgs a) {
+  __shared__ uint32_t own[FEW ? kFewSeqs + 1 : 1];
   const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + kRefPages - 1) / kRefPages);
   uint32_t before, all;
   blk_sums(a, blocks, min(blockIdx.x, blocks), before, all);
-  uint32_t *table = a.out_table;
+  if constexpr (FEW) grow_starts<256>(a, own);
+  const uint32_t *start = FEW ? own : a.start;
   if (blockIdx.x < blocks) {
-    const uint64_t wanted = a.start[a.s.n_seq - 1] + (a.need[a.s.n_seq - 1] & ~kOneCopy);
+    const uint32_t wanted = start[a.s.n_seq];
     if (before >= wanted) return;
     each_bit(a, blockIdx.x, [&](uint32_t p, bool free, uint32_t rank) {
-      const uint64_t r = before + rank;
+      const uint32_t r = before + rank;
       if (!free || r >= wanted) return;
       // the last sequence that starts at r or before it
       uint32_t lo = 0, hi = a.s.n_seq;
       while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
-        if (a.start[mid] <= r) lo = mid;
+        if (start[mid] <= r) lo = mid;
         else hi = mid;
       }
-      const uint32_t b = lo, need = a.need[b];
-      if (a.start[b] + (need & ~kOneCopy) > all) return;
-      const uint32_t j = (uint32_t)(r - a.start[b]);
-      uint32_t n0 = (uint32_t)(((uint64_t)min(a.s.lens[b], a.s.max_k) + (1u << a.shift) - 1) >> a.shift);
-      if (need & kOneCopy) {
-        n0--;
-        // (the page before it is left by its thread below, which reads it first)
-        if (j == 0) {
-          a.dst[b] = p;
-          a.refs_out[p] = 1;
-          return;
-        }
-      }
+      const uint32_t need = a.need[lo], j = r - start[lo];
+      if (add_sat(start[lo], need & ~kOneCopy) > all) return;
+      if ((need & kOneCopy) && j == 0) a.dst[lo] = p;
       a.refs_out[p] = 1;
-      table[(int64_t)b * a.s.table_stride + n0 + j] = p;
+      a.out_table[(int64_t)lo * a.s.table_stride + a.at[lo] + j] = p;
     });
     return;
   }
   const uint32_t b = (blockIdx.x - blocks) * 256 + threadIdx.x;
   if (b >= a.s.n_seq) return;
   const uint32_t need = a.need[b];
-  const bool served = (need & ~kOneCopy) == 0 || a.start[b] + (need & ~kOneCopy) <= all;
-  if (!served) cache_err(a.err, kCacheFull, b);
-  uint32_t from = kInvalid;
-  if (served && (need & kOneCopy)) {
-    const uint32_t n0 = (uint32_t)(((uint64_t)min(a.s.lens[b], a.s.max_k) + (1u << a.shift) - 1) >> a.shift);
-    from = a.s.table[(int64_t)b * a.s.table_stride + n0 - 1];
-    atomicSub(&a.refs_out[from], 1u);
-  } else {
-    a.dst[b] = kInvalid;
+  if ((need & ~kOneCopy) && add_sat(start[b], need & ~kOneCopy) > all) {
+    cache_err(a.err, kCacheFull, b);
+    a.src[b] = a.dst[b] = kInvalid;
+    return;
   }
-  a.src[b] = from;
-}
-
-// The last step, once every page is given: copies' places in the table, lengths.
-__global__ __launch_bounds__(256) void k_grow_end(RefArgs a) {
-  const uint32_t blocks = (uint32_t)(((uint64_t)a.n_pages + kRefPages - 1) / kRefPages);
-  uint32_t before, all;
-  blk_sums(a, blocks, 0, before, all);
-  const uint32_t b = blockIdx.x * 256 + threadIdx.x;
-  if (b >= a.s.n_seq) return;
-  const uint32_t need = a.need[b];
-  const bool served = (need & ~kOneCopy) == 0 || a.start[b] + (need & ~kOneCopy) <= all;
-  if (!served) return;
+  if (need & kOneCopy) atomicSub(&a.refs_out[a.src[b]], 1u);
+  else a.dst[b] = kInvalid;
   const GrowSeq g = grow_seq(a, b);
-  if (need & kOneCopy) a.out_table[(int64_t)b * a.s.table_stride + g.n0 - 1] = a.dst[b];
   if (g.fits) a.lens[b] = g.len + a.n_new[b];
 }
 
@@ -428,9 +417,12 @@ hipError_t launch_grow(const RefArgs &a, hipStream_t st) {
     return hipGetLastError();
   }
   k_grow_need<<<blocks + seqs, 256, 0, st>>>(a);
-  k_grow_start<<<1, 1024, 0, st>>>(a);
-  k_grow_give<<<blocks + seqs, 256, 0, st>>>(a);
-  k_grow_end<<<seqs, 256, 0, st>>>(a);
+  if (a.s.n_seq <= kFewSeqs) {
+    k_grow_give<true><<<blocks + seqs, 256, 0, st>>>(a);
+  } else {
+    k_grow_start<<<1, 1024, 0, st>>>(a);
+    k_grow_give<false><<<blocks + seqs, 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -141,12 +141,14 @@ grand_status grand_pages_grow(grand_cache *h, const grand_seqs *s, const uint32_
   }
   Parts w;
   const uint32_t blocks = blocks_of(n_pages);
-  const int w_bits = w.add(blocks * (kRefPages / 8ull)), w_blk = w.add(blocks * 4ull), w_need = w.add(n_seq * 4ull), w_start = w.add(n_seq * 8ull);
+  const int w_bits = w.add(blocks * (kRefPages / 8ull)), w_blk = w.add(blocks * 4ull), w_need = w.add(n_seq * 4ull), w_at = w.add(n_seq * 4ull);
+  const int w_start = w.add(n_seq > kFewSeqs ? (n_seq + 1) * 4ull : 0);
   TRY(ensure_ws(h, w.total));
   a.bits = (uint64_t *)(h->ws + w.at[w_bits]);
   a.blk = (uint32_t *)(h->ws + w.at[w_blk]);
   a.need = (uint32_t *)(h->ws + w.at[w_need]);
-  a.start = (uint64_t *)(h->ws + w.at[w_start]);
+  a.at = (uint32_t *)(h->ws + w.at[w_at]);
+  a.start = (uint32_t *)(h->ws + w.at[w_start]);
   a.n_new = n_new;
   a.out_table = table;
   a.lens = lens;

@@ -546,21 +546,23 @@ class Cache:
     def _packed(self, k, v):
         if not isinstance(v, Packed):
             raise ValueError("k_pages and v_pages must both be Packed")
-        g, u8 = self._args["packed"], self._torch.uint8
-        for what, a, b, shape in (("codes", k.codes, v.codes, self._code_shape), ("scales", k.scales, v.scales, self._scale_shape)):
-            if (a.dtype != u8 or b.dtype != u8 or a.shape != b.shape or a.shape[1:] != shape or not a.is_cuda or not b.is_cuda
-                    or (shape[2] > 1 and (a.stride(3) != 1 or b.stride(3) != 1))):
-                raise ValueError(f"{what} of k_pages and v_pages must be (pages, {', '.join(map(str, shape))}) uint8 on the GPU, contiguous "
-                                 "along their last axis")
-            if a.stride() != b.stride() and any(n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride())):
-                raise ValueError(f"{what} of k_pages and v_pages must have the same strides")
-        if k.codes.shape[0] != k.scales.shape[0]:
+        g = self._args["packed"]
+        g.k, g.v, pages, (g.page_stride, g.slot_stride, g.head_stride) = self._packed_part("codes", k.codes, v.codes, self._code_shape)
+        g.k_scales, g.v_scales, g.n_pages, (g.scale_page_stride, g.scale_slot_stride, g.scale_head_stride) = self._packed_part(
+            "scales", k.scales, v.scales, self._scale_shape)
+        if pages != g.n_pages:
             raise ValueError("codes and scales must have as many pages")
-        g.k, g.v, g.k_scales, g.v_scales = k.codes.data_ptr(), v.codes.data_ptr(), k.scales.data_ptr(), v.scales.data_ptr()
-        g.n_pages = k.codes.shape[0]
-        g.page_stride, g.slot_stride, g.head_stride = k.codes.stride()[:3]
-        g.scale_page_stride, g.scale_slot_stride, g.scale_head_stride = k.scales.stride()[:3]
         return self._refs["packed"]
+
+    def _packed_part(self, what, k, v, want):
+        shape, stride, u8 = k.shape, k.stride(), self._torch.uint8
+        if (k.dtype != u8 or v.dtype != u8 or shape[1:] != want or v.shape != shape or not k.is_cuda or not v.is_cuda
+                or (want[2] > 1 and (stride[3] != 1 or v.stride(3) != 1))):
+            raise ValueError(f"{what} of k_pages and v_pages must be (pages, {', '.join(map(str, want))}) uint8 on the GPU, contiguous "
+                             "along their last axis")
+        if v.stride() != stride and any(n > 1 and a != b for n, a, b in zip(shape, stride, v.stride())):
+            raise ValueError(f"{what} of k_pages and v_pages must have the same strides")
+        return k.data_ptr(), v.data_ptr(), shape[0], stride[:3]
 
     def _pages(self, k, v):
         if isinstance(v, Packed):

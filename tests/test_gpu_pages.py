@@ -125,6 +125,40 @@ def test_grow(n_seq, page, n_pages, width, in_place, most):
     cache.close()
 
 
+@pytest.mark.parametrize("n_seq", [255, 256, 257, 2047, 2048, 2049, 5000])
+@pytest.mark.parametrize("short", [0, 1, 700])
+def test_grow_of_many_sequences(n_seq, short):
+    """Some wait for pages where the pool is `short` of them."""
+    from paper_2608_21163_amd import GrandError
+
+    r = np.random.default_rng(n_seq + short)
+    page = 4
+    lens = r.integers(0, 17, n_seq)
+    held = -(-lens // page)
+    new = r.integers(0, 9, n_seq)
+    want_pages = int((-(-(lens + new) // page) - held).sum())
+    n_pages = int(held.sum()) + max(0, want_pages - short)
+    order = r.permutation(n_pages)
+    table, at = np.full((n_seq, 7), INVALID, np.uint32), 0
+    for b in range(n_seq):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+    lens, new = lens.astype(np.uint32), new.astype(np.uint32)
+    refs = names(table, lens, page, n_pages)
+    want = grow_ref(table, lens, page, new, refs)
+    assert bool(want[5]) == bool(short)
+    cache = cache_of(page)
+    t, l, c = ints(table), ints(lens), ints(refs)
+    got = cache.grow(cache.sequences(t, l), ints(new), c)
+    for g, w in zip((t, l, c, got[2], got[3]), want):
+        equal(g, w)
+    if short:
+        with pytest.raises(GrandError):
+            cache.check()
+    cache.check()
+    cache.close()
+
+
 def test_grow_when_pages_run_out():
     """In order: what does not fit stays as it was, and so does what comes after it and needs a page."""
     from paper_2608_21163_amd import GrandError
