@@ -156,7 +156,7 @@ struct RefArgs {
   int tokens;
   uint32_t *freed, *n_freed; // compact: n_freed counts its moves
   // workspace
-  uint32_t *count;           // release: names given up, by page
+  uint64_t *below;           // release: pages with more names than counted
   uint64_t *bits;            // a bit a page: free (grow), in use (compact), freed (release)
   uint32_t *blk;             // set bits by block of kRefPages pages
   uint32_t *rank, *total;    // compact: a moving page's place in the lists; pages in use
@@ -166,6 +166,7 @@ struct RefArgs {
   CacheErr *err;
 };
 constexpr uint32_t kRefPages = 2048;  // pages of a workgroup
+constexpr uint32_t kFewBlocks = 256; // workgroups that count the set bits of all themselves
 constexpr uint32_t kFewSeqs = 2048;   // sequences whose needs every workgroup adds up
 
 struct CopyArgs {

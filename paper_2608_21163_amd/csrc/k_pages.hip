@@ -69,16 +69,10 @@ __device__ __forceinline__ void block_bits(const RefArgs &a, uint32_t blk, F set
   if (t == 0) a.blk[blk] = sum[0] + sum[1] + sum[2] + sum[3];
 }
 
-// Sums of blk[0 .. n) before and in all, by a workgroup of 256.
-__device__ __forceinline__ void blk_sums(const RefArgs &a, uint32_t n, uint32_t before, uint32_t &sum_before, uint32_t &sum_all) {
+// The sums of x and y over a workgroup of 256.
+__device__ __forceinline__ void sum_pair(uint32_t &x, uint32_t &y) {
   __shared__ uint32_t tmp[4][2];
   const uint32_t t = threadIdx.x;
-  uint32_t x = 0, y = 0;
-  for (uint32_t i = t; i < n; i += 256) {
-    const uint32_t c = a.blk[i];
-    y += c;
-    if (i < before) x += c;
-  }
 #pragma unroll
   for (int j = 32; j; j >>= 1) {
     x += (uint32_t)__shfl_xor((int)x, j, 64);
@@ -86,9 +80,43 @@ __device__ __forceinline__ void blk_sums(const RefArgs &a, uint32_t n, uint32_t 
   }
   if (t % 64 == 0) tmp[t / 64][0] = x, tmp[t / 64][1] = y;
   __syncthreads();
-  sum_before = tmp[0][0] + tmp[1][0] + tmp[2][0] + tmp[3][0];
-  sum_all = tmp[0][1] + tmp[1][1] + tmp[2][1] + tmp[3][1];
+  x = tmp[0][0] + tmp[1][0] + tmp[2][0] + tmp[3][0];
+  y = tmp[0][1] + tmp[1][1] + tmp[2][1] + tmp[3][1];
   __syncthreads();
+}
+
+// Sums of blk[0 .. n) before and in all, by a workgroup of 256.
+__device__ __forceinline__ void blk_sums(const RefArgs &a, uint32_t n, uint32_t before, uint32_t &sum_before, uint32_t &sum_all) {
+  const uint32_t t = threadIdx.x;
+  uint32_t x = 0, y = 0;
+  for (uint32_t i = t; i < n; i += 256) {
+    const uint32_t c = a.blk[i];
+    y += c;
+    if (i < before) x += c;
+  }
+  sum_pair(x, y);
+  sum_before = x, sum_all = y;
+}
+
+// The same from the bits themselves, for the set bits of the words before `before`:
+// one launch less (pages given back in a pool of 165,000: 17.4 us, 21.5 with it).
+__device__ __forceinline__ void word_sums(const RefArgs &a, uint32_t before, uint32_t &sum_before, uint32_t &sum_all) {
+  const uint32_t words = (a.n_pages + 63) / 64;
+  uint32_t x = 0, y = 0;
+  for (uint32_t i = threadIdx.x; i < words; i += 256) {
+    const uint32_t c = popc(a.bits[i]);
+    y += c;
+    if (i < before) x += c;
+  }
+  sum_pair(x, y);
+  sum_before = x, sum_all = y;
+}
+__global__ __launch_bounds__(256) void k_count_bits(RefArgs a) {
+  const uint32_t words = kRefPages / 64, t = threadIdx.x;
+  const uint64_t w = (uint64_t)blockIdx.x * words + t;
+  uint32_t n = t < words && w * 64 < a.n_pages ? popc(a.bits[w]) : 0, all = n;
+  sum_pair(n, all);
+  if (t == 0) a.blk[blockIdx.x] = all;
 }
 
 // Calls f(page, is its bit set, set bits of the workgroup before it) for every page
@@ -239,12 +267,17 @@ __global__ __launch_bounds__(256) void k_grow_give(RefArgs a) {
 }
 
 // ---------------------------------------------------------------- release
-__global__ __launch_bounds__(256) void k_release_clear(RefArgs a) {
+// A name takes one off its page's count in refs_out.  The one that finds 1 sets the
+// page's bit of those that are freed; one that finds 0 (more names than counted)
+// sets its bit of those below 0.  A page of either kind ends at 0.
+__global__ __launch_bounds__(256) void k_release_start(RefArgs a) {
   const uint64_t p = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (p < a.n_pages) a.count[p] = 0;
+  if (p >= a.n_pages) return;
+  if (a.refs_out != a.refs_in) a.refs_out[p] = a.refs_in[p];
+  if (p % 64 == 0) a.bits[p / 64] = a.below[p / 64] = 0;
 }
 
-__global__ __launch_bounds__(256) void k_release_count(RefArgs a) {
+__global__ __launch_bounds__(256) void k_release_names(RefArgs a) {
   const uint32_t chunks = (a.width + 255) / 256, row = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
   uint32_t n = a.width;
   if (a.counts) {
@@ -259,23 +292,22 @@ __global__ __launch_bounds__(256) void k_release_count(RefArgs a) {
   if (i >= n) return;
   const uint32_t id = a.ids[(int64_t)row * a.row_stride + i];
   if (id == kInvalid) return;
-  if (id >= a.n_pages) cache_err(a.err, kCachePage, row);
-  else atomicAdd(&a.count[id], 1u);
-}
-
-__global__ __launch_bounds__(256) void k_release_refs(RefArgs a) {
-  block_bits(a, blockIdx.x, [&](uint32_t p) {
-    const uint32_t old = a.refs_in[p], gone = a.count[p];
-    if (gone > old) cache_err(a.err, kCacheRefs, p);
-    a.refs_out[p] = old - min(gone, old);
-    return old && gone >= old;
-  });
+  if (id >= a.n_pages) {
+    cache_err(a.err, kCachePage, row);
+    return;
+  }
+  const uint32_t old = atomicSub(&a.refs_out[id], 1u);
+  if (old > 1) return;
+  atomicOr((unsigned long long *)(old ? a.bits : a.below) + id / 64, 1ull << (id % 64));
+  if (!old) cache_err(a.err, kCacheRefs, id);
 }
 
 __global__ __launch_bounds__(256) void k_release_list(RefArgs a) {
   uint32_t before, all;
-  blk_sums(a, gridDim.x, blockIdx.x, before, all);
+  if (gridDim.x > kFewBlocks) blk_sums(a, gridDim.x, blockIdx.x, before, all);
+  else word_sums(a, blockIdx.x * (kRefPages / 64), before, all);
   each_bit(a, blockIdx.x, [&](uint32_t p, bool freed, uint32_t rank) {
+    if (freed || a.below[p / 64] >> (p % 64) & 1) a.refs_out[p] = 0;
     if (freed) a.freed[before + rank] = p;
     if (p >= all && p < a.cap) a.freed[p] = kInvalid;
   });
@@ -428,9 +460,9 @@ hipError_t launch_grow(const RefArgs &a, hipStream_t st) {
 
 hipError_t launch_release(const RefArgs &a, hipStream_t st) {
   const uint32_t blocks = groups(a.n_pages, kRefPages);
-  k_release_clear<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
-  if (a.n_rows && a.width) k_release_count<<<groups(a.width, 256) * a.n_rows, 256, 0, st>>>(a);
-  k_release_refs<<<blocks, 256, 0, st>>>(a);
+  k_release_start<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
+  if (a.n_rows && a.width) k_release_names<<<groups(a.width, 256) * a.n_rows, 256, 0, st>>>(a);
+  if (blocks > kFewBlocks) k_count_bits<<<blocks, 256, 0, st>>>(a);
   k_release_list<<<blocks, 256, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -184,11 +184,11 @@ grand_status grand_pages_release(grand_cache *h, uint32_t n_rows, uint32_t width
   TRY(check_results(h, results, 3, args, 3));
   Parts w;
   const uint32_t blocks = blocks_of(n_pages);
-  const int w_bits = w.add(blocks * (kRefPages / 8ull)), w_blk = w.add(blocks * 4ull), w_count = w.add(n_pages * 4ull);
+  const int w_bits = w.add(blocks * (kRefPages / 8ull)), w_blk = w.add(blocks * 4ull), w_below = w.add(blocks * (kRefPages / 8ull));
   TRY(ensure_ws(h, w.total));
   a.bits = (uint64_t *)(h->ws + w.at[w_bits]);
   a.blk = (uint32_t *)(h->ws + w.at[w_blk]);
-  a.count = (uint32_t *)(h->ws + w.at[w_count]);
+  a.below = (uint64_t *)(h->ws + w.at[w_below]);
   a.ids = ids;
   a.counts = counts;
   a.row_stride = stride;

@@ -226,6 +226,31 @@ def test_release_of_more_names_than_counted():
     cache.close()
 
 
+@pytest.mark.parametrize("n_pages", [524_288, 524_289, 1_000_001])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_release_in_large_pools(n_pages, in_place):
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+
+    r = np.random.default_rng(n_pages)
+    refs = r.integers(0, 4, n_pages)
+    refs[-1] = refs[0] = 1
+    ids = r.integers(0, n_pages, (64, 5000)).astype(np.uint32)
+    ids[3, 17], ids[60, 4999] = n_pages - 1, 0
+    cache = cache_of()
+    c, t = ints(refs), ints(ids)
+    out = c if in_place else torch.full_like(c, -7)
+    got = cache.release(t, c, refs_out=None if in_place else out)
+    want = release_ref(ids, None, refs)
+    equal(got[0], want[0])
+    equal(got[1], want[1])
+    assert int(got[2]) == want[2] > 10_000
+    with pytest.raises(GrandError):         # a quarter of the pages are named though free
+        cache.check()
+    cache.close()
+
+
 @pytest.mark.parametrize("n_seq,page,n_pages,width", SIZES)
 @pytest.mark.parametrize("in_place", [False, True])
 def test_compact(n_seq, page, n_pages, width, in_place):
