@@ -220,8 +220,9 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   a.n_splits = (uint32_t)std::max<uint64_t>(1, (span + 31 + split - 1) / split);
   // (beside first tokens every long sequence's window is as long: one workgroup each as soon
   // as that is one a CU.  Windows of 1,024, 8 heads, 16, 32, 48, 64 and 96 single tokens:
-  // 18.6 us, 23.5, 38.2, 45.6, 66.7; split 17.0, 26.8, 39.9, 51.2, 73.9)
-  if (span <= split || (a.sinks && !is_packed && few && base >= 256)) a.n_splits = 1, split = span + 31;
+  // 18.6 us, 23.5, 38.2, 45.6, 66.7; split 17.0, 26.8, 39.9, 51.2, 73.9.  Long windows
+  // gain little, 64 of 4,000 143 and 151 us, and where few sequences reach them they are split)
+  if (span <= split || (a.sinks && !is_packed && few && base >= 256 && span <= 2048)) a.n_splits = 1, split = span + 31;
   a.split = (uint32_t)split;
   // Packed pages, few rows: equal shares of all sequences' keys that fill the chip
   // once, not splits of each (64 single tokens over up to 8,192: 70 us, splits of 1,024
