@@ -131,12 +131,13 @@ __device__ __forceinline__ float part_scale(float m, float top) { return m == ne
 
 // Attention over listed slots, as for 16-bit pages, here a lane per block of a row, so
 // that DP / 32 lanes read one.  WAVES share a (sequence, query head)'s list: four, or
-// one where there are many lists that would not fill a workgroup's first loads, as the start and
-// the end of a list then count for more than its rows (256 x 32 lists of 64 ids: 45 us, with
-// four waves 82; of 256 ids 158 and 149; 64 x 32 of 64: 17 and 26).  Rows of 64
-// bytes that lie anywhere are bound by their number: 256 x 32 lists of 256 take
-// 152, 158 and 170 us at 64, 128 and 256 elements, in a pool of 4,096 slots 52;
-// keys and values are two places each, codes and scales.
+// one where there are many lists that would not fill a workgroup's first loads, or whose
+// pool the caches hold: the start and the end of a list then count for more than its
+// rows.  256 x 32 lists, one wave and four: of 64 ids 45 us, 82; of 256 in a pool
+// of 16,384 slots of eight heads (18 MB) 58, 88; of 65,536 106, 113; of 131,072 129, 129; of 262,144 159, 150.
+// Rows in a pool above the caches are bound by their number: 155, 150 and
+// 159 us at 64, 128 and 256 elements, 57 lines a ns (keys and values are two
+// places each, codes and scales), and as long with rows asked for ahead of the sums.
 template <class E, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_ids_packed(IdsArgs a) {
   constexpr int LPR = DP / 32, GROUPS = 64 / LPR, U = 4, STEP = WAVES * GROUPS;
@@ -314,7 +315,8 @@ hipError_t ids_type(const IdsArgs &a, hipStream_t st) {
 
 hipError_t launch_ids_packed(bool f16, const IdsArgs &a, hipStream_t st) {
   const uint32_t pass = a.dim <= 64 ? 512 : a.dim <= 128 ? 256 : 128;  // ids that four waves ask for at once
-  if (a.n_seq * a.q_heads >= 2048 && a.k < pass) return f16 ? ids_type<F16, 1>(a, st) : ids_type<Bf16, 1>(a, st);
+  const bool held = a.pg.bytes <= 64u << 20;                       // keys' codes; as much again for the values'
+  if (a.n_seq * a.q_heads >= 2048 && (a.k < pass || held)) return f16 ? ids_type<F16, 1>(a, st) : ids_type<Bf16, 1>(a, st);
   return f16 ? ids_type<F16, 4>(a, st) : ids_type<Bf16, 4>(a, st);
 }
 
