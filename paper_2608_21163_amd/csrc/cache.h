@@ -189,10 +189,9 @@ constexpr uint32_t kEvictSmall = 8192, kEvictTile = 2048;
 // Rows of a workgroup's tile: 16 or 32, its waves taking different keys, or
 // 128, its waves taking different rows.
 constexpr uint32_t kFewRows = 32, kManyRows = 128;
-// Packed pages, few rows: workgroups of a CU.  64 single tokens over up to 8,192 of 128 elements, 307 MB, heads outside
-// slots and inside: two workgroups 69.8 us and 87.9, three 70.6 and 96.6, four 86.2 and
-// 128.8 (their registers spill); two with tiles of 64 keys a wave 74.4 and 97.4.
-constexpr int packed_groups(int dp, int nb) { return dp > 128 && nb > 1 ? 1 : dp == 64 && nb == 1 ? 3 : 2; }
+// Packed pages, few rows: workgroups that a CU's registers hold (a fourth of 128 elements
+// spills: 64 single tokens over up to 8,192 86 us instead of 70; tiles of 64 keys a wave 74).
+constexpr int packed_groups(int dp, int nb) { return dp > 128 ? (nb > 1 ? 1 : 2) : nb == 1 ? 3 : 2; }
 // keys of a tile of many rows
 constexpr uint32_t rows_tile(uint32_t dim) { return dim > 128 ? 32 : 64; }
 constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again

@@ -227,9 +227,14 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   // Packed pages, few rows: equal shares of all sequences' keys that fill the chip
   // once, not splits of each (64 single tokens over up to 8,192: 70 us, splits of 1,024
   // keys 81).  Up to 512 keys are one launch without parts; every workgroup
-  // adds up all lengths, 64 at a time.
+  // adds up all lengths, 64 at a time.  Three workgroups a CU rather than two where registers
+  // allow it (64 over up to 1,024: 23.5 us, 26.6; 256: 55, 60; 96 elements 69, 75), but two for long
+  // shares of slots of all heads (64 over up to 2,048, 4,096 and 8,192: 34.2, 45.4, 84.8, three
+  // 33.1, 46.7, 86.3).
   if (is_packed && few && span > 512 && s->n_seq <= 1024 && s->n_seq * (span / kKeysStep + 2) < 1u << 31) {
-    const uint32_t groups_of_cu = packed_groups(p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256, tile_rows / 16);
+    uint32_t groups_of_cu = packed_groups(p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256, tile_rows / 16);
+    const bool beside = a.pg.slot == (p.head_dim + 31) / 32 * 16;  // a head's slots
+    if (!beside && groups_of_cu == 3 && p.head_dim > 64 && s->n_seq * span * p.kv_heads > 2048 * 512) groups_of_cu = 2;
     a.units = std::max(1u, 256 * groups_of_cu / p.kv_heads);
   }
   const uint64_t groups = few ? ((a.units ? (uint64_t)p.kv_heads * a.units : base * a.n_splits) + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;
