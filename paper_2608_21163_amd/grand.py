@@ -660,6 +660,8 @@ class Cache:
         (out, lse), and with weights (sequences, kv_heads, at least max_k)
         also weights_out (weights itself if not given).  With a window every
         row sees the first `sinks` tokens too."""
+        if not 0 <= sinks < 1 << 32:
+            raise ValueError("sinks must be a number of tokens")
         n, ref = self._tokens(seqs, q)
         rq = self._rows("q", q, self._q, n)
         if out is None:

@@ -374,6 +374,59 @@ def test_one_long_sequence_among_short_ones():
             run(c)
 
 
+@pytest.mark.parametrize("n,longest", [(9, 3000), (70, 900)])
+def test_captured_steps_of_changing_lengths(n, longest):
+    """Shares follow the lengths of a replay, not those of the capture; two graphs take turns in one workspace."""
+    import torch
+
+    from paper_2608_21163_amd import Cache
+
+    stream = torch.cuda.Stream()
+    r = np.random.default_rng(n)
+    c = packed(make("bf16", 4, 2, 128, 16, qs=(1,) * n, ks=(longest,) * n, seed=n))
+    cache = Cache(c["dtype"], c["hq"], c["hk"], c["dim"], c["page"], stream=stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        q, lens = c["q"].cuda(), c["lens"].clone()
+        s = cache.sequences(c["table"], lens, max_k=longest)
+        weights = torch.zeros(n, 2, longest, device="cuda")
+        calls = [lambda: cache.attend(s, q, c["k_pages"], c["v_pages"]),
+                 lambda: cache.attend(s, q, c["k_pages"], c["v_pages"], window=700, sinks=20, weights=weights, weights_out=torch.empty_like(weights))]
+        for call in calls:
+            call()
+        stream.synchronize()
+        graphs = []
+        for call in calls:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                res = call()
+            graphs.append((g, res))
+        for i in range(8):
+            kl = r.integers(0, longest + 1, n)
+            kl[r.integers(0, n)] = longest
+            lens.copy_(torch.from_numpy(kl.astype(np.int32)))
+            weights.copy_(torch.rand(weights.shape))
+            for (g, got), call in zip(graphs, calls):
+                g.replay()
+                got = [x.clone() for x in got]
+                want = call()
+                seen = torch.arange(longest, device="cuda") < torch.from_numpy(kl).cuda()[:, None, None]
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+                assert len(got) < 3 or torch.equal(*(torch.where(seen, x[2], 0.0) for x in (got, want))), i
+    cache.check()
+    cache.close()
+
+
+def test_refusals_of_the_binding():
+    c = packed(make(qs=(1,), ks=(40,)))
+    whole = make(qs=(1,), ks=(40,))
+    for kw in (dict(sinks=-1), dict(sinks=1 << 32)):
+        with pytest.raises(ValueError):
+            run(c, window=4, **kw)
+    for k, v in ((c["k_pages"], whole["v_pages"]), (whole["k_pages"], c["v_pages"])):
+        with pytest.raises(ValueError):
+            run(dict(c, k_pages=k, v_pages=v))
+
+
 # ------------------------------------------------------------ first tokens
 @pytest.mark.parametrize("kind", ["whole", "packed"])
 @pytest.mark.parametrize("window,sinks", [(1, 1), (7, 4), (32, 32), (33, 64), (100, 5), (40, 65), (100000, 3), (40, 100000)])
