@@ -542,3 +542,29 @@ def test_calls_on_another_stream():
     assert np.array_equal(rows[0][0].double().cpu().numpy(), c["keys"][0][0].numpy())
     cache.check()
     cache.close()
+
+
+def test_calls_that_the_binding_does_not_make():
+    """Keys or values read alone, and attention without its log-sum-exps."""
+    import torch
+
+    k = packed(make(qs=(1, 1), ks=(90, 700)))
+    cache = cache_for(k)
+    slots = ints([int(k["table"][1, p // 16]) * 16 + p % 16 for p in (0, 77, 699)])
+    both = cache.read(slots, k["k_pages"], k["v_pages"])
+    pages = cache._packed(k["k_pages"], k["v_pages"])
+    for i, name in enumerate(("k", "v")):
+        x = torch.empty_like(both[0])
+        r = cache._rows(name, x, k["hk"], 3)
+        cache._check(cache.lib.grand_packed_read(cache.h, 3, slots.data_ptr(), pages, r if i == 0 else None, r if i == 1 else None))
+        cache.check()
+        assert torch.equal(x, both[i])
+    q, s = k["q"].cuda(), seqs_for(cache, k)
+    out, lse = cache.attend(s, q, k["k_pages"], k["v_pages"])
+    alone = torch.full_like(out, 7)
+    n, ref = cache._tokens(s, q)
+    cache._check(cache.lib.grand_cache_attend_packed(cache.h, ref, cache._rows("q", q, k["hq"], n), pages, k["dim"] ** -0.5, 1, 0, 0,
+                                                     cache._rows("out", alone, k["hq"], n), None, None, None))
+    cache.check()
+    assert torch.equal(alone, out)
+    cache.close()
