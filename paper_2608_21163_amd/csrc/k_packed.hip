@@ -122,8 +122,17 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
     if (a.k.p) k = unpack8<E>(*(const uint32_t *)(a.pg.k + at), pack_factor<E>(a.sc.k[sc]));
     if (a.v.p) v = unpack8<E>(*(const uint32_t *)(a.pg.v + at), pack_factor<E>(a.sc.v[sc]));
   }
-  if (a.k.p) *(v4u *)(a.k.p + (int64_t)i * a.k.token + (int64_t)head * a.k.head + c * 16) = k;
-  if (a.v.p) *(v4u *)(a.v.p + (int64_t)i * a.v.token + (int64_t)head * a.v.head + c * 16) = v;
+  v4u *to_k = (v4u *)(a.k.p + (int64_t)i * a.k.token + (int64_t)head * a.k.head + c * 16);
+  v4u *to_v = (v4u *)(a.v.p + (int64_t)i * a.v.token + (int64_t)head * a.v.head + c * 16);
+  // more than the caches could keep for who takes them: past them (67 MB of keys and as much of values,
+  // written by an append and read back, 58 us, through them 68; 17 MB 22 both ways)
+  if ((uint64_t)a.n * a.kv_heads * a.dim >= 1 << 24) {
+    if (a.k.p) __builtin_nontemporal_store(k, to_k);
+    if (a.v.p) __builtin_nontemporal_store(v, to_v);
+  } else {
+    if (a.k.p) *to_k = k;
+    if (a.v.p) *to_v = v;
+  }
 }
 
 // (m, l) of two parts of a softmax, in log2 units; m may be -inf (nothing).

@@ -388,7 +388,8 @@ __global__ __launch_bounds__(256) void k_compact_apply(RefArgs a) {
 
 // ---------------------------------------------------------------- copies
 // 16 bytes a thread and step, keys first, then values; small pages share a
-// workgroup, large ones are several workgroups'.
+// workgroup, large ones are several workgroups'.  Written past the caches: 185 MB of pages
+// in 61 us, 6.1 TB/s of reads and writes; through them 78, read past them too 70.
 __global__ __launch_bounds__(256) void k_copy_pages(CopyArgs a, uint32_t per, uint32_t chunks) {
   const uint32_t both = 2 * a.pieces, t = threadIdx.x;
   const uint64_t wg = blockIdx.x;
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(256) void k_copy_pages(CopyArgs a, uint32_t per, ui
   }
 #pragma unroll
   for (uint32_t j = 0; j < 4; j++)
-    if (j < n) *(v4u *)(const_cast<uint8_t *>(first + j * 256 < a.pieces ? a.pg.k : a.pg.v) + to + at[j]) = x[j];
+    if (j < n) __builtin_nontemporal_store(x[j], (v4u *)(const_cast<uint8_t *>(first + j * 256 < a.pieces ? a.pg.k : a.pg.v) + to + at[j]));
   if (!a.sc.k) return;
   // scales: the entry's first threads, a byte at a time
   const uint32_t bytes = a.slots * a.heads * a.scale_row, step = per > 1 ? both : 256;
