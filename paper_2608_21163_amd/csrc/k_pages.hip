@@ -387,48 +387,59 @@ __global__ __launch_bounds__(256) void k_compact_apply(RefArgs a) {
 }
 
 // ---------------------------------------------------------------- copies
-// 16 bytes a thread and step, keys first, then values; small pages share a
-// workgroup, large ones are several workgroups'.  Written past the caches: 185 MB of pages
-// in 61 us, 6.1 TB/s of reads and writes; through them 78, read past them too 70.
+// 1,024 pieces of 16 bytes a workgroup, of each entry the keys' first, then the values':
+// `per` small pages, or a part of a large one.  Written past the caches: 185 MB of pages
+// in 61 us, 6.1 TB/s of reads and writes; through them 78, read past them too 70.  (Pages of
+// one slot, 4 KB of both, several a workgroup: half of a pool compacted in 97 us, a workgroup each 115;
+// of two slots a workgroup each is better, 86 and 95.)
+template <bool SMALL>
 __global__ __launch_bounds__(256) void k_copy_pages(CopyArgs a, uint32_t per, uint32_t chunks) {
-  const uint32_t both = 2 * a.pieces, t = threadIdx.x;
-  const uint64_t wg = blockIdx.x;
-  const uint64_t i = per > 1 ? wg * per + t / both : wg / chunks;
-  if (i >= a.n || (per > 1 && t >= per * both)) return;
-  const uint32_t s = a.src[i], d = a.dst[i];
-  if (s == kInvalid || d == kInvalid) return;
-  if (s >= a.pg.n_pages || d >= a.pg.n_pages) {
-    cache_err(a.err, kCacheList, (uint32_t)i);
+  const uint32_t both = 2 * a.pieces, t = threadIdx.x, line = a.row / 16;
+  const uint32_t chunk = SMALL ? 0 : blockIdx.x % chunks;
+  const uint64_t first = SMALL ? (uint64_t)blockIdx.x * per : blockIdx.x / chunks;
+  const uint32_t n = SMALL ? (uint32_t)min((uint64_t)per, a.n - first) : 1;
+  auto there = [&](uint32_t s, uint32_t d) { return s < a.pg.n_pages && d < a.pg.n_pages; };
+  v4u x[4];
+  uint32_t s[4], d[4], at[4];
+  bool some[4], key[4];
+#pragma unroll
+  for (uint32_t j = 0; j < (SMALL ? 4 : 1); j++) {
+    const uint32_t e = SMALL ? min((t + j * 256) / both, n - 1) : 0;
+    s[j] = a.src[first + e], d[j] = a.dst[first + e];
+  }
+  if (!SMALL && !there(s[0], d[0])) {
+    if (s[0] != kInvalid && d[0] != kInvalid) cache_err(a.err, kCacheList, (uint32_t)first);
     return;
   }
-  const uint64_t from = (uint64_t)s * a.pg.page, to = (uint64_t)d * a.pg.page;
-  const uint32_t first = per > 1 ? t % both : wg % chunks * 1024 + t;
-  v4u x[4];
-  uint64_t at[4];
-  uint32_t n = 0;
-  const uint32_t most = per > 1 ? 1 : 4, line = a.row / 16;
 #pragma unroll
   for (uint32_t j = 0; j < 4; j++) {
-    const uint32_t y = first + j * 256;
-    if (j < most && y < both) {
-      const uint32_t z = y < a.pieces ? y : y - a.pieces;
-      at[j] = a.flat ? z * 16u : (uint64_t)(z / line / a.heads) * a.pg.slot + (uint64_t)(z / line % a.heads) * a.pg.head + z % line * 16;
-      x[j] = *(const v4u *)((y < a.pieces ? a.pg.k : a.pg.v) + from + at[j]);
-      n = j + 1;
-    }
+    const uint32_t y = t + j * 256, e = SMALL ? y / both : 0, in = SMALL ? y - e * both : chunk * 1024 + y;
+    if (!SMALL) s[j] = s[0], d[j] = d[0];
+    some[j] = SMALL ? e < n && there(s[j], d[j]) : in < both;
+    key[j] = in < a.pieces;
+    const uint32_t z = key[j] ? in : in - a.pieces;
+    at[j] = a.flat ? z * 16u : z / line / a.heads * a.pg.slot + z / line % a.heads * a.pg.head + z % line * 16;
   }
 #pragma unroll
   for (uint32_t j = 0; j < 4; j++)
-    if (j < n) __builtin_nontemporal_store(x[j], (v4u *)(const_cast<uint8_t *>(first + j * 256 < a.pieces ? a.pg.k : a.pg.v) + to + at[j]));
-  if (!a.sc.k) return;
-  // scales: the entry's first threads, a byte at a time
-  const uint32_t bytes = a.slots * a.heads * a.scale_row, step = per > 1 ? both : 256;
-  if (per == 1 && wg % chunks) return;
-  for (uint32_t y = per > 1 ? t % both : t; y < bytes; y += step) {
-    const uint32_t r = y / a.scale_row;
-    const uint64_t off = (uint64_t)(r / a.heads) * a.sc.slot + (uint64_t)(r % a.heads) * a.sc.head + y % a.scale_row;
-    const_cast<uint8_t *>(a.sc.k)[(uint64_t)d * a.sc.page + off] = a.sc.k[(uint64_t)s * a.sc.page + off];
-    const_cast<uint8_t *>(a.sc.v)[(uint64_t)d * a.sc.page + off] = a.sc.v[(uint64_t)s * a.sc.page + off];
+    if (some[j]) x[j] = *(const v4u *)((key[j] ? a.pg.k : a.pg.v) + (uint64_t)s[j] * a.pg.page + at[j]);
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++)
+    if (some[j]) __builtin_nontemporal_store(x[j], (v4u *)(const_cast<uint8_t *>(key[j] ? a.pg.k : a.pg.v) + (uint64_t)d[j] * a.pg.page + at[j]));
+  if (SMALL && t < n) {
+    const uint32_t s0 = a.src[first + t], d0 = a.dst[first + t];
+    if (s0 != kInvalid && d0 != kInvalid && !there(s0, d0)) cache_err(a.err, kCacheList, (uint32_t)(first + t));
+  }
+  if (!a.sc.k || chunk) return;
+  // the entries' scales, a byte at a time
+  const uint32_t bytes = a.slots * a.heads * a.scale_row;
+  for (uint32_t y = t; y < n * bytes; y += 256) {
+    const uint32_t e = y / bytes, in = y - e * bytes, r = in / a.scale_row;
+    const uint32_t s0 = a.src[first + e], d0 = a.dst[first + e];
+    if (!there(s0, d0)) continue;
+    const uint64_t off = (uint64_t)(r / a.heads) * a.sc.slot + (uint64_t)(r % a.heads) * a.sc.head + in % a.scale_row;
+    const_cast<uint8_t *>(a.sc.k)[(uint64_t)d0 * a.sc.page + off] = a.sc.k[(uint64_t)s0 * a.sc.page + off];
+    const_cast<uint8_t *>(a.sc.v)[(uint64_t)d0 * a.sc.page + off] = a.sc.v[(uint64_t)s0 * a.sc.page + off];
   }
 }
 
@@ -477,9 +488,10 @@ hipError_t launch_compact(const RefArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_copy(const CopyArgs &a, hipStream_t st) {
-  const uint32_t both = 2 * a.pieces, per = both < 256 ? 256 / both : 1, chunks = per > 1 ? 1 : groups(both, 1024);
+  const uint32_t both = 2 * a.pieces, per = both < 512 ? 1024 / both : 1, chunks = per > 1 ? 1 : groups(both, 1024);
   const uint64_t wgs = per > 1 ? groups(a.n, per) : (uint64_t)a.n * chunks;
-  k_copy_pages<<<(uint32_t)wgs, 256, 0, st>>>(a, per, chunks);
+  if (per > 1) k_copy_pages<true><<<(uint32_t)wgs, 256, 0, st>>>(a, per, chunks);
+  else k_copy_pages<false><<<(uint32_t)wgs, 256, 0, st>>>(a, per, chunks);
   return hipGetLastError();
 }
 
