@@ -349,7 +349,7 @@ def ragged(n, most_q, longest, seed, empty=0.2):
     return tuple(qs.tolist()), tuple(ks.tolist())
 
 
-MANY = [(70, 1, 900), (129, 4, 700), (1024, 1, 520), (1025, 1, 520), (3, 2, 20_000)]
+MANY = [(70, 1, 900), (129, 4, 700), (1024, 1, 520), (1025, 1, 520), (3, 2, 20_000), (40, 8, 7000)]
 
 
 @pytest.mark.parametrize("n,most_q,longest", MANY)
