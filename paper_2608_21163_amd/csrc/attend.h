@@ -55,6 +55,11 @@ struct Whole { static constexpr bool kSinks = false, kPacked = false; };
 struct Sinks { static constexpr bool kSinks = true, kPacked = false; };
 struct Packed { static constexpr bool kSinks = true, kPacked = true; };
 
+// A key before a row's window that is none of the first tokens.
+template <class V> __device__ __forceinline__ bool before_window(int key, int first, int sinks) {
+  return key < first && (!V::kSinks || key >= sinks);
+}
+
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 constexpr float down(int up) { return 1.f / (float)(1 << up); }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -266,7 +271,7 @@ __device__ __forceinline__ v8s v_operand(const uint8_t *lv, int t, int d, int la
 // One tile of KT keys: scores, running softmax, weighted values.
 // A row sees the keys from first to last, and those before sinks up to last.
 // masked: some key of the tile is hidden from some row of the wave.
-template <class E, int DP, int KT>
+template <class E, int DP, int KT, class V>
 __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk, const uint8_t *lv, float c, uint32_t key0,
                                           bool masked, int sinks, int first, int last, int lane) {
   const int col = lane & 31, half = lane >> 5;
@@ -290,7 +295,7 @@ __device__ __forceinline__ void tile_step(RowState<E, DP> &st, const uint8_t *lk
 #pragma unroll
       for (int i = 0; i < 16; i++) {
         const int key = (int)k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
-        if ((key < first && key >= sinks) || key > last) s[kb][i] = neg_inf();
+        if (before_window<V>(key, first, sinks) || key > last) s[kb][i] = neg_inf();
       }
   }
   float mx = s[0][0];
@@ -517,7 +522,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void k_attend_rows(AttendArg
       }
       lds_barrier();
       const bool masked = (int)key0 < wfirst || (int)key0 + KT - 1 > min(wlast, tile_end - 1);
-      tile_step<E, DP, KT>(st, lk, lv, a.c, key0, masked, sinks, first, min(last, tile_end - 1), lane);
+      tile_step<E, DP, KT, V>(st, lk, lv, a.c, key0, masked, sinks, first, min(last, tile_end - 1), lane);
     }
     if (__syncthreads_or(odd)) add_non_finite<E, DP, V>(a, table, line, kvh, begin, end, first, last, half, st.o);
   }
@@ -810,7 +815,7 @@ __global__ __launch_bounds__(256, DP > 192 || (DP > 128 && NB > 1) ? 1 : DP > 12
 #pragma unroll
             for (int i = 0; i < 4; i++) {
               const int key = (int)k0 + kb * 16 + g * 4 + i;
-              if ((key < first[nb] && key >= sinks) || key > (V::kSinks ? min(last[nb], tile_end - 1) : last[nb])) sc[nb][kb][i] = neg_inf();
+              if (before_window<V>(key, first[nb], sinks) || key > (V::kSinks ? min(last[nb], tile_end - 1) : last[nb])) sc[nb][kb][i] = neg_inf();
             }
       }
       Op p[NB];
@@ -1347,7 +1352,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : DP > 64 ? 2 : 3) void k_weights
     // (rows past the last are zeros, which an infinite key makes NaN of)
     const bool masked = (a.causal && wkey + 63 > p_lo) || (a.window && wkey <= p_hi - (int)a.window) || r0 + RT > r_hi;
     // (no row sees a key of the wave: most of a tile of first tokens)
-    const bool none = (a.causal && wkey > p_hi) || (a.window && wkey + 63 <= p_lo - (int)a.window && wkey >= sinks_of<V>(a));
+    const bool none = V::kSinks && ((a.causal && wkey > p_hi) || (a.window && wkey + 63 <= p_lo - (int)a.window && wkey >= sinks_of<V>(a)));
 #pragma unroll
     for (int rb = 0; rb < RT / 32 && !none; rb++) {
       v16f s[2] = {v16f{}, v16f{}};
@@ -1368,7 +1373,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : DP > 64 ? 2 : 3) void k_weights
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = k0 + kb * 32 + (i / 4) * 8 + half * 4 + i % 4;
-            const bool hidden = row >= r_hi || (a.causal && key > pos) || (a.window && key <= pos - (int)a.window && key >= sinks_of<V>(a));
+            const bool hidden = row >= r_hi || (a.causal && key > pos) || (a.window && before_window<V>(key, pos - (int)a.window + 1, sinks_of<V>(a)));
             acc[kb][i] += hidden ? 0.f : ex2(__builtin_fmaf(s[kb][i], a.c, -z));
           }
       } else {
