@@ -12,6 +12,7 @@
 namespace gr {
 
 constexpr uint32_t kInvalid = 0xFFFFFFFFu;
+constexpr uint32_t kHole = 0xFFFFFFFEu;  // no id, with or without its top bit: capacity is below 2^31 - 1
 constexpr uint32_t kVisit = 0x80000000u;
 constexpr uint32_t kIdMask = 0x7FFFFFFFu;
 
@@ -371,10 +372,10 @@ __device__ __forceinline__ uint64_t rdlane64(uint64_t v, int l) {
 // `keep` are written to the LDS scratch (ld, li: 64*N entries each) and read
 // back in order.  More than kBatchMax survivors take the sort-and-merge path.
 // A list may name an id twice (one that is rewritten while a reader loads
-// it is seen partly old and partly new): equal new keys take that path too.
-// Two at one position would leave the next one unwritten, and what LDS
-// happens to hold there would become an id.  (Looked for beside the loop's
-// chain: dropping them in it made the searches 7% slower.)
+// it is seen partly old and partly new): two equal new keys share a position and
+// leave the next one unwritten.  Such a hole is marked beforehand, and
+// found, those keys take that path too.  (Comparing every new key with the others in
+// the loop below made queries 2% slower, dropping repeats there the searches 7%.)
 constexpr int kBatchMax = 32;
 template <int N>
 __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N], float nd, uint32_t ni, int keep,
@@ -400,12 +401,13 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
 #pragma unroll
   for (int r = 0; r < N; r++) cnt[r] = 0;
   uint32_t ltc = 0, rk = 0;
-  uint64_t live = 0, mm = m, twice = 0;
+  uint64_t live = 0, mm = m;
+#pragma unroll
+  for (int r = 0; r < N; r++) li[r * 64 + ln] = kHole;
   while (mm) {
     const int l = ffs64(mm);
-    const uint64_t xk = rdlane64(nk, l);
     mm &= mm - 1;
-    twice |= ballot(nk == xk) ^ (1ull << l);
+    const uint64_t xk = rdlane64(nk, l);
     bool lt[N];
     int below = 0;
     bool dup = false;
@@ -422,10 +424,6 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
     rk += xk < nk ? 1u : 0u;
     ltc = ln == l ? (uint32_t)below : ltc;
   }
-  if (twice) {
-    wave_merge_new<N>(cd, ci, in ? nd : finf(), in ? ni : kInvalid, keep);
-    return;
-  }
 #pragma unroll
   for (int r = 0; r < N; r++) {
     const int p = r * 64 + ln + (int)cnt[r];
@@ -436,14 +434,24 @@ __device__ __forceinline__ void wave_merge_lds(float (&cd)[N], uint32_t (&ci)[N]
     if (p < keep) { ld[p] = nd; li[p] = ni; }
   }
   __syncthreads();
+  float td[N];
+  uint32_t ti[N];
+  bool hole = false;
 #pragma unroll
   for (int r = 0; r < N; r++) {
     const int e = r * 64 + ln;
     const bool ok = e < keep;
-    cd[r] = ok ? ld[e] : finf();
-    ci[r] = ok ? li[e] : kInvalid;
+    td[r] = ok ? ld[e] : finf();
+    ti[r] = ok ? li[e] : kInvalid;
+    hole |= ti[r] == kHole;
   }
   __syncthreads();
+  if (ballot(hole)) {
+    wave_merge_new<N>(cd, ci, in ? nd : finf(), in ? ni : kInvalid, keep);
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < N; r++) cd[r] = td[r], ci[r] = ti[r];
 }
 
 // The float whose sortable() image is u.
