@@ -247,7 +247,7 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   const int w_part = parts ? w.add(parts * p.head_dim * 4) : -1, w_ml = parts ? w.add(parts * 8) : -1;
   int w_lse = -1, w_scores = -1, w_sums = -1;
   a.row_splits = 1;
-  if (weights_out) {
+  if (weights_out && s->max_k) {
     w_lse = w.add(all_rows * 4);
     // scores of a few rows are kept (4 bytes a row and key, against half of
     // the cache to compute them again)

@@ -579,3 +579,17 @@ def test_many_lists(dim, n):
         cache.check()
     assert e.value.code == E_ID
     cache.close()
+
+
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (10, 4)])
+def test_weights_of_chunks_without_cached_tokens(kind, window, sinks):
+    """max_k 0, and chunks of more rows than a tile's: every row sees nothing."""
+    import torch
+
+    say(f"[no cached tokens] {kind} window {window} {sinks}")
+    c = make("bf16", 8, 2, 64, 16, qs=(40, 70), ks=(0, 0))
+    c = packed(c) if kind == "packed" else c
+    none = torch.empty(2, 2, 0, device="cuda")
+    out, lse, _ = run(c, weights=none, window=window, sinks=sinks)
+    assert not out.any() and torch.isneginf(lse).all()

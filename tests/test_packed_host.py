@@ -279,3 +279,18 @@ def test_copies(built):
         one = More(built, **kw)
         assert built.grand_pages_copy(one.h, 4, one.memory(16), one.memory(16), ctypes.byref(one.pages())) == OK
         assert built.fake_copy_flat() == 1, kw
+
+
+def test_weights_of_chunks_without_cached_tokens(built):
+    """max_k 0 beside a chunk of more rows than one tile's: its rows see nothing, and
+    there are no weights to lay out."""
+    c = More(built, q_heads=8)
+    s, q, out, none = c.seqs(1, max_q=64, max_k=0), c.rows(64), c.rows(64), grand.Weights(None, 0, 0)
+    for window, sinks in ((0, 0), (10, 0), (10, 4)):
+        c.log()
+        assert c.attend(s, q, c.pages(), out, wi=none, wo=none, window=window) == OK, c.error()
+        r = [ctypes.byref(x) for x in (s, q, c.pages(), out, none, none)]
+        assert built.grand_cache_attend_sinks(c.h, *r[:3], 0.125, 1, window, sinks, r[3], None, *r[4:]) == OK, c.error()
+        assert c.attend_packed(s, q, c.packed(), out, window, sinks, none, none) == OK, c.error()
+        launches = [x.split()[0] for x in c.log() if x.split()[0] in ("attend", "join", "weights")]
+        assert launches == ["attend"] * 3
