@@ -558,7 +558,8 @@ grand_status grand_pages_fork(grand_cache *h, const grand_seqs *s, uint32_t n_ou
  * pages are given out in ascending order, to the sequences in order and in a sequence to
  * its tokens in order.  A sequence that needs more pages than are left stays as it was, and so does
  * every later one that needs any (reported by grand_cache_check, and
- * to be seen from lens); so does one whose tokens would not fit max_pages. */
+ * to be seen from lens); so does one whose tokens would not fit max_pages, or
+ * whose length is above max_k before the call (after it, it may be). */
 grand_status grand_pages_grow(grand_cache *h, const grand_seqs *s, const uint32_t *n_new, uint32_t n_pages, const uint32_t *refs_in,
                               uint32_t *refs_out, uint32_t *table, uint32_t *lens, uint32_t *src, uint32_t *dst);
 

@@ -149,13 +149,13 @@ __device__ __forceinline__ void each_bit(const RefArgs &a, uint32_t blk, F f) {
 // ---------------------------------------------------------------- grow
 struct GrowSeq {
   uint32_t len, n0, n1;  // tokens, pages before and after
-  bool fits;
+  bool fits;             // its length is within max_k, and the new one within max_pages
 };
 __device__ __forceinline__ GrowSeq grow_seq(const RefArgs &a, uint32_t b) {
   GrowSeq g;
   g.n0 = row_pages(a, b, g.len);
   const uint64_t after = (uint64_t)g.len + a.n_new[b];
-  g.fits = (after + (1u << a.shift) - 1) >> a.shift <= a.s.max_pages && after <= 0xFFFFFFFFull;
+  g.fits = a.s.lens[b] <= a.s.max_k && (after + (1u << a.shift) - 1) >> a.shift <= a.s.max_pages && after <= 0xFFFFFFFFull;
   g.n1 = g.fits ? (uint32_t)((after + (1u << a.shift) - 1) >> a.shift) : g.n0;
   return g;
 }

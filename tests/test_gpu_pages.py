@@ -568,3 +568,41 @@ def test_calls_that_the_binding_does_not_make():
     cache.check()
     assert torch.equal(alone, out)
     cache.close()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_growth_past_max_k(in_place):
+    """A call may bring a length above max_k. A sequence that has one before the
+    call stays as it was, whatever its row holds there, and is reported; the others grow."""
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ARG
+
+    page = 4
+    table = np.array([[0, 1, 77, 5], [2, INVALID, INVALID, INVALID], [3, 1, INVALID, INVALID]], np.uint32)
+    lens, refs = np.array([8, 4, 7], np.uint32), np.array([1, 2, 1, 1, 0, 0, 0, 0], np.int64)
+    cache = cache_of(page)
+    t, l, c = ints(table), ints(lens), ints(refs)
+    s = cache.sequences(t, l, max_k=7)
+
+    def grow(new, c):
+        out = c if in_place else torch.full_like(c, -7)
+        return cache.grow(s, ints(new), c, refs_out=out)[2:] + (out,)
+    # lengths 8 (above max_k), 4 and 7: pages 4 for the second, 5 for the third's copy
+    src, dst, c = grow([9, 4, 1], c)
+    for g, w in ((t, [table[0], [2, 4, INVALID, INVALID], [3, 5, INVALID, INVALID]]), (l, [8, 8, 8]), (c, [1, 1, 1, 1, 1, 1, 0, 0]),
+                 (src, [INVALID, INVALID, 1]), (dst, [INVALID, INVALID, 5])):
+        equal(g, w)
+    with pytest.raises(GrandError) as e:
+        cache.check()
+    assert e.value.code == E_ARG
+    # all three are above it now
+    before = [x.clone() for x in (t, l, c)]
+    src, dst, c = grow([1, 1, 1], c)
+    assert all(torch.equal(a, b) for a, b in zip((t, l, c), before)) and (src == -1).all() and (dst == -1).all()
+    with pytest.raises(GrandError) as e:
+        cache.check()
+    assert e.value.code == E_ARG
+    cache.check()
+    cache.close()
