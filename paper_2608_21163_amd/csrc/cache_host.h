@@ -241,6 +241,9 @@ bool pools_apart(PoolRows a, PoolRows b) {
   for (int i = 0; i < 3; i++) {
     const auto &x = a.axes[i], &y = b.axes[i];
     if (x.n != y.n || (x.n > 1 && x.s != y.s)) alike = false;
+  }
+  for (int i = 0; i < 3; i++) {
+    const auto &x = a.axes[i], &y = b.axes[i];
     if (alike && x.n > 1 && ra <= d && d + rb <= x.s) return true;
     ra += x.n > 1 ? (x.n - 1) * x.s : 0;
     rb += y.n > 1 ? (y.n - 1) * y.s : 0;

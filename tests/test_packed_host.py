@@ -294,3 +294,19 @@ def test_weights_of_chunks_without_cached_tokens(built):
         assert c.attend_packed(s, q, c.packed(), out, window, sinks, none, none) == OK, c.error()
         launches = [x.split()[0] for x in c.log() if x.split()[0] in ("attend", "join", "weights")]
         assert launches == ["attend"] * 3
+
+
+def test_scales_that_drift_into_codes(built):
+    """Slots of codes leave room for scales beside them, but pages of scales are longer or shorter
+    than the codes': from some page on they lie on codes of other slots."""
+    for heads, slot in ((1, 32), (2, 64)):
+        c = More(built, q_heads=heads, kv_heads=heads, head_dim=32)
+        s, k, v, page = c.seqs(), c.rows(heads=heads), c.rows(heads=heads), 16 * slot
+        at, src, dst = [c.memory(16 * page) for _ in range(4)], c.memory(12), c.memory(12)
+        strides = dict(page_stride=page, slot_stride=slot, head_stride=32, scale_slot_stride=slot, scale_head_stride=32)
+        for scales, want in ((page, OK), (page + 8, ARG), (page - 8, ARG)):
+            for g in (c.packed(k=at[0], k_scales=at[0] + 16, v=at[1], v_scales=at[2], **strides),
+                      c.packed(k=at[0], k_scales=at[1], v=at[2], v_scales=at[2] + 16, **strides)):
+                g.scale_page_stride = scales
+                assert c.append_packed(s, k, v, g) == want, (heads, scales, c.error())
+                assert built.grand_packed_copy(c.h, 3, src, dst, ctypes.byref(g)) == want, (heads, scales)
