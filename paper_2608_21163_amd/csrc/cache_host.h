@@ -232,24 +232,28 @@ bool rows_apart(const PoolRows &r) {
 bool slots_apart(const grand_cache_params &p, const PagesView &g) {
   return rows_apart(pool_rows(p, g.k, p.head_dim * 2, g.n_pages, g.page, g.slot, g.head));
 }
-// Nor do two such pools: one lies behind the other, or with the same strides
-// in the room that one of the axes leaves between its steps.
-bool pools_apart(PoolRows a, PoolRows b) {
-  if (a.p > b.p) std::swap(a, b);
-  uint64_t ra = a.row, rb = b.row, d = b.p - a.p;
-  bool alike = true;
-  for (int i = 0; i < 3; i++) {
-    const auto &x = a.axes[i], &y = b.axes[i];
-    if (x.n != y.n || (x.n > 1 && x.s != y.s)) alike = false;
+// Whether rows of two such pools may share memory, a's first at 0 and b's at d, along the
+// `axes` shortest axes.  Along an axis of the same steps in both only those
+// rows can meet whose steps are as far apart as d is, or one more: what the shorter axes reach
+// lies within a step.  From the first unlike axis on (codes and scales of a page, side by side)
+// the extents are compared.
+bool rows_meet(const PoolRows &a, const PoolRows &b, int axes, int64_t d) {
+  int64_t ra = (int64_t)a.row, rb = (int64_t)b.row;
+  for (int i = 0; i < axes; i++) {
+    ra += (int64_t)((a.axes[i].n - 1) * a.axes[i].s);
+    rb += (int64_t)((b.axes[i].n - 1) * b.axes[i].s);
   }
-  for (int i = 0; i < 3; i++) {
-    const auto &x = a.axes[i], &y = b.axes[i];
-    if (alike && x.n > 1 && ra <= d && d + rb <= x.s) return true;
-    ra += x.n > 1 ? (x.n - 1) * x.s : 0;
-    rb += y.n > 1 ? (y.n - 1) * y.s : 0;
-  }
-  return ra <= d;
+  if (d >= ra || -d >= rb) return false;
+  if (axes == 0) return true;
+  const auto &x = a.axes[axes - 1], &y = b.axes[axes - 1];
+  if (x.n != y.n) return true;
+  if (x.n == 1) return rows_meet(a, b, axes - 1, d);
+  if (x.s != y.s) return true;
+  const int64_t n = (int64_t)x.n, s = (int64_t)x.s, t = floor_div(-d, s);
+  return (t > -n && t < n && rows_meet(a, b, axes - 1, d + t * s)) || (t + 1 > -n && t + 1 < n && rows_meet(a, b, axes - 1, d + (t + 1) * s));
 }
+// (of pools whose own rows are apart)
+bool pools_apart(const PoolRows &a, const PoolRows &b) { return !rows_meet(a, b, 3, (int64_t)(b.p - a.p)); }
 
 // Packed pages: rows of whole blocks, their scales beside them.
 struct PackedBytes { uint64_t codes, scales; };  // up to the last row's last

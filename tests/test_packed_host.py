@@ -4,6 +4,7 @@ import ctypes
 import os
 import subprocess
 
+import numpy as np
 import pytest
 
 from conftest import ROOT
@@ -310,3 +311,83 @@ def test_scales_that_drift_into_codes(built):
                 g.scale_page_stride = scales
                 assert c.append_packed(s, k, v, g) == want, (heads, scales, c.error())
                 assert built.grand_packed_copy(c.h, 3, src, dst, ctypes.byref(g)) == want, (heads, scales)
+
+
+def test_one_buffer_holds_codes_and_scales(built):
+    """Codes and scales take turns, page by page, head by head or slot by slot, keys and
+    values in one buffer or two: attention reads them and appends and copies write them."""
+    c = More(built)                                    # rows of 32 and 2 bytes
+    s, k, v, src, dst = c.seqs(), c.rows(heads=2), c.rows(heads=2), c.memory(12), c.memory(12)
+    q, out = c.rows(), c.rows()
+    page, head, slot = 16 * 2 * 34, 16 * 34 + 16, 2 * 32 + 16
+    layouts = [
+        # a page's codes, then its scales
+        (dict(page_stride=page, slot_stride=64, head_stride=32, scale_page_stride=page, scale_slot_stride=4, scale_head_stride=2), 1024, page),
+        # the same with heads outermost on one side
+        (dict(page_stride=page, slot_stride=32, head_stride=512, scale_page_stride=page, scale_slot_stride=4, scale_head_stride=2), 1024, page),
+        # a head's codes, then its scales
+        (dict(page_stride=2 * head, head_stride=head, slot_stride=32, scale_page_stride=2 * head, scale_head_stride=head, scale_slot_stride=2),
+         512, 2 * head),
+        # a slot's codes, then its scales
+        (dict(page_stride=16 * slot, slot_stride=slot, head_stride=32, scale_page_stride=16 * slot, scale_slot_stride=slot, scale_head_stride=2),
+         64, 16 * slot),
+    ]
+    for strides, behind, size in layouts:
+        # keys' pages, then values' pages; and the pages of both in turn
+        apart = [c.memory(8 * size) for _ in range(2)]
+        pools = [dict(k=apart[0], k_scales=apart[0] + behind, v=apart[1], v_scales=apart[1] + behind, **strides)]
+        both = c.memory(16 * size)
+        turns = dict(strides, page_stride=2 * size, scale_page_stride=2 * size)
+        pools.append(dict(k=both, k_scales=both + behind, v=both + size, v_scales=both + size + behind, **turns))
+        # (values a page further on: between pages of keys, not behind them)
+        longer = c.memory(20 * size)
+        pools.append(dict(k=longer, k_scales=longer + behind, v=longer + 3 * size, v_scales=longer + 3 * size + behind, **turns))
+        for kw in pools:
+            g = c.packed(**kw)
+            assert c.attend_packed(s, q, g, out) == OK, c.error()
+            assert c.append_packed(s, k, v, g) == OK, (strides, c.error())
+            assert built.grand_packed_copy(c.h, 3, src, dst, ctypes.byref(g)) == OK
+            for worse in (dict(k_scales=g.k_scales - 1), dict(v_scales=g.v_scales - 1), dict(k_scales=g.v_scales), dict(v=g.k + 16)):
+                assert c.append_packed(s, k, v, changed(g, **worse)) == ARG, (strides, worse)
+                assert built.grand_packed_copy(c.h, 3, src, dst, ctypes.byref(changed(g, **worse))) == ARG
+
+
+def rows_bytes(at, row, n, strides):
+    """Every byte of a pool's rows; None where two rows share one."""
+    starts = at + sum(np.arange(m).reshape([-1 if i == j else 1 for j in range(3)]) * s for i, (m, s) in enumerate(zip(n, strides)))
+    x = (starts.reshape(-1, 1) + np.arange(row)).ravel()
+    return x if len(np.unique(x)) == len(x) else None
+
+
+def test_pools_share_memory_or_not(built):
+    """Random strides and places: no pools are written that share a byte, and none are
+    refused whose codes and scales have the same steps along every axis."""
+    c = More(built, q_heads=2, kv_heads=2, head_dim=64, page_size=4)
+    s, k, v, r = c.seqs(max_k=12), c.rows(heads=2), c.rows(heads=2), np.random.default_rng(0)
+    n, found = (3, 4, 2), {OK: 0, ARG: 0}
+    far = c.memory(1 << 16)
+    for _ in range(4000):
+        def steps(row, unit):
+            order, at, reach = r.permutation(3), [0, 0, 0], row
+            for i in order:
+                at[i] = -(-(reach + int(r.choice([0, 0, 0, 1, 2, 16, 32, 64, 200]))) // unit) * unit
+                reach += (n[i] - 1) * at[i]
+            return at
+        codes = steps(32, 16)
+        scales = codes if r.random() < 0.6 else steps(2, 1)
+        if r.random() < 0.3:
+            scales = [codes[0] if r.random() < 0.8 else x for x in scales]
+        at = c.memory(1 << 15)
+        place = 4096 + int(r.choice([r.integers(-2000, 2000), r.integers(-200, 200), 32, codes[0] - 4, codes[1] - 4, codes[2] - 4]))
+        g = c.packed(3, k=at + 4096, k_scales=at + place, v=far, v_scales=far + (1 << 15), page_stride=codes[0], slot_stride=codes[1],
+                     head_stride=codes[2], scale_page_stride=scales[0], scale_slot_stride=scales[1], scale_head_stride=scales[2])
+        a, b = rows_bytes(at + 4096, 32, n, codes), rows_bytes(at + place, 2, n, scales)
+        got = c.append_packed(s, k, v, g)
+        assert got in (OK, ARG)
+        found[got] += 1
+        apart = a is not None and b is not None and not len(np.intersect1d(a, b))
+        if got == OK:
+            assert apart, (codes, scales, place)
+        elif scales == codes:
+            assert not apart, (codes, place)
+    assert min(found.values()) > 400, found
