@@ -435,7 +435,7 @@ const char *grand_cache_last_error(const grand_cache *h);
 /* Writes the new tokens' keys and values (n_tokens rows by kv_heads) to their
  * places in the pages: new token i of sequence b is cached token
  * lens[b] - chunk length + i.  No other slot is touched.  No two slots of
- * the pages may share memory. */
+ * the pages may share memory; keys and values may be one pool (and then the same rows). */
 grand_status grand_cache_append(grand_cache *h, const grand_seqs *s, const grand_rows *k, const grand_rows *v,
                                 const grand_pages *pages);
 
@@ -584,7 +584,7 @@ grand_status grand_pages_compact(grand_cache *h, const grand_seqs *s, uint32_t n
 
 /* Copies keys and values of page src[i] to page dst[i], all slots, i < n; entries with
  * GRAND_INVALID in either are passed over.  A page that is named in dst is named there
- * once, and not in src. */
+ * once, and not in src.  No two slots of the pages may share memory; keys and values may be one pool. */
 grand_status grand_pages_copy(grand_cache *h, uint32_t n, const uint32_t *src, const uint32_t *dst, const grand_pages *pages);
 grand_status grand_packed_copy(grand_cache *h, uint32_t n, const uint32_t *src, const uint32_t *dst, const grand_packed *pages);
 

@@ -117,7 +117,7 @@ static grand_status append(grand_cache *h, const grand_seqs *s, const grand_rows
     TRY(check_packed_apart(h, a.pg, a.sc));
   } else {
     TRY(check_pages(h, pages, &a.pg));
-    if (!slots_apart(h->p, a.pg)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
+    TRY(check_pages_apart(h, a.pg));
   }
   TRY(check_rows(h, "k", k, s->n_tokens, h->p.kv_heads, false, &a.k));
   TRY(check_rows(h, "v", v, s->n_tokens, h->p.kv_heads, false, &a.v));

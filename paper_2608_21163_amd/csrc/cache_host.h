@@ -229,9 +229,6 @@ bool rows_apart(const PoolRows &r) {
   }
   return true;
 }
-bool slots_apart(const grand_cache_params &p, const PagesView &g) {
-  return rows_apart(pool_rows(p, g.k, p.head_dim * 2, g.n_pages, g.page, g.slot, g.head));
-}
 // Whether rows of two such pools may share memory, a's first at 0 and b's at d, along the
 // `axes` shortest axes.  Along an axis of the same steps in both only those
 // rows can meet whose steps are as far apart as d is, or one more: what the shorter axes reach
@@ -254,6 +251,14 @@ bool rows_meet(const PoolRows &a, const PoolRows &b, int axes, int64_t d) {
 }
 // (of pools whose own rows are apart)
 bool pools_apart(const PoolRows &a, const PoolRows &b) { return !rows_meet(a, b, 3, (int64_t)(b.p - a.p)); }
+
+// Pages that are written: no row shares memory with another; keys and values may be one pool.
+grand_status check_pages_apart(grand_cache *h, const PagesView &g) {
+  const PoolRows k = pool_rows(h->p, g.k, h->p.head_dim * 2, g.n_pages, g.page, g.slot, g.head);
+  const PoolRows v = pool_rows(h->p, g.v, h->p.head_dim * 2, g.n_pages, g.page, g.slot, g.head);
+  if (!rows_apart(k)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
+  return g.k == g.v || pools_apart(k, v) ? GRAND_OK : fail(h, GRAND_E_ARG, "keys and values overlap");
+}
 
 // Packed pages: rows of whole blocks, their scales beside them.
 struct PackedBytes { uint64_t codes, scales; };  // up to the last row's last

@@ -242,7 +242,7 @@ grand_status grand_pages_copy(grand_cache *h, uint32_t n, const uint32_t *src, c
   HCHK(h, hipSetDevice(h->p.device));
   CopyArgs a{};
   TRY(check_pages(h, pages, &a.pg));
-  if (!slots_apart(h->p, a.pg)) return fail(h, GRAND_E_ARG, "slots of pages overlap");
+  TRY(check_pages_apart(h, a.pg));
   a.row = h->p.head_dim * 2;
   return copy_pages(h, n, src, dst, a);
 }

@@ -391,3 +391,26 @@ def test_pools_share_memory_or_not(built):
         elif scales == codes:
             assert not apart, (codes, place)
     assert min(found.values()) > 400, found
+
+
+def test_keys_and_values_that_partly_overlap(built):
+    """16-bit pages that are written: keys and values are one pool, or share nothing."""
+    c = More(built)
+    s, k, v, g, src, dst = c.seqs(), c.rows(heads=2), c.rows(heads=2), c.pages(), c.memory(40), c.memory(40)
+    size = 16 * 2 * 64 * 2                              # bytes of a page
+
+    def write(g, k=k, v=v):
+        r = [ctypes.byref(x) for x in (s, k, v, g)]
+        return built.grand_cache_append(c.h, *r), built.grand_pages_copy(c.h, 10, src, dst, r[3])
+    assert write(g) == (OK, OK)
+    two = c.memory(2 * 8 * size)
+    for at, want in ((0, OK), (64, ARG), (128, ARG), (size, ARG), (8 * size - 128, ARG), (8 * size, OK)):
+        shared = grand.Pages(two, two + at, 8, g.page_stride, g.slot_stride, g.head_stride)
+        assert c.attend(c.seqs(), c.rows(), shared, c.rows()) == OK, c.error()
+        assert write(shared, k, v if at else k) == (want, want), (at, c.error())
+        if want != OK:
+            assert "overlap" in c.error()
+    # keys and values of a page, of a slot, of a head in turn
+    for strides, at in (((2 * 2048, 128, 64), 2 * 2048), ((2 * 2048, 2 * 128, 64), 2 * 128), ((2 * 2048, 2 * 128, 2 * 64), 2 * 64)):
+        assert write(grand.Pages(two, two + at, 8, *strides)) == (OK, OK), c.error()
+        assert write(grand.Pages(two, two + at - 16, 8, *strides)) == (ARG, ARG)
