@@ -545,7 +545,7 @@ grand_status grand_cache_evict(grand_cache *h, const grand_seqs *s, uint32_t hea
  * packed) names the pages of row parents[i] and then GRAND_INVALID, out_lens[i] is its
  * length, and their refs are counted.  A parent may be named often or never; GRAND_INVALID
  * gives an empty sequence.  drop: the names in s's table are given up in the
- * same call (a step of a beam).  out_table shares no memory with s's table. */
+ * same call (a step of a beam), before the new ones are counted.  out_table shares no memory with s's table. */
 grand_status grand_pages_fork(grand_cache *h, const grand_seqs *s, uint32_t n_out, const uint32_t *parents, int drop,
                               uint32_t n_pages, const uint32_t *refs_in, uint32_t *refs_out, uint32_t *out_table,
                               uint32_t *out_lens);

@@ -29,25 +29,39 @@ __global__ __launch_bounds__(256) void k_copy_refs(RefArgs a) {
   if (p < a.n_pages) a.refs_out[p] = a.refs_in[p];
 }
 
-// A workgroup per 256 entries of a new row (or, behind those, of an old one
-// whose names are dropped).
+// A workgroup per 256 entries of an old row whose names are dropped.  Before the
+// new names are counted, so that whether more are dropped than were counted
+// does not depend on who comes first.  A name that finds nothing left is put back: what is
+// taken off in all is what was there, and the count ends at 0.  (Its own launch is 2.9 us; 64
+// beams' fork, growth and copies 37.4 us, with names dropped and counted in one launch 34.5.)
+__global__ __launch_bounds__(256) void k_fork_drop(RefArgs a) {
+  const uint32_t chunks = max((a.s.max_pages + 255) / 256, 1u), b = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
+  uint32_t len;
+  if (i >= row_pages(a, b, len)) return;
+  const uint32_t id = a.s.table[(int64_t)b * a.s.table_stride + i];
+  if (id >= a.n_pages) {
+    cache_err(a.err, kCachePage, b);
+    return;
+  }
+  const int old = (int)atomicSub(&a.refs_out[id], 1u);
+  if (old > 0) return;
+  atomicAdd(&a.refs_out[id], 1u);
+  cache_err(a.err, kCacheRefs, id);
+}
+
+// A workgroup per 256 entries of a new row.
 __global__ __launch_bounds__(256) void k_fork(RefArgs a) {
   const uint32_t chunks = max((a.s.max_pages + 255) / 256, 1u), row = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
-  uint32_t b = row - a.n_out, len = 0, n = 0;
-  const bool fresh = row < a.n_out;
-  if (fresh) {
-    b = a.parents[row];
-    if (b != kInvalid && b >= a.s.n_seq) cache_err(a.err, kCacheParent, row);
-    if (b < a.s.n_seq) n = row_pages(a, b, len);
-    if (i == 0) a.out_lens[row] = len;
-  } else {
-    n = row_pages(a, b, len);
-  }
+  uint32_t len = 0, n = 0;
+  const uint32_t b = a.parents[row];
+  if (b != kInvalid && b >= a.s.n_seq) cache_err(a.err, kCacheParent, row);
+  if (b < a.s.n_seq) n = row_pages(a, b, len);
+  if (i == 0) a.out_lens[row] = len;
   const uint32_t id = i < n ? a.s.table[(int64_t)b * a.s.table_stride + i] : kInvalid;
-  if (fresh && i < a.s.max_pages) a.out_table[(int64_t)row * a.out_stride + i] = id;
+  if (i < a.s.max_pages) a.out_table[(int64_t)row * a.out_stride + i] = id;
   if (i >= n) return;
   if (id >= a.n_pages) cache_err(a.err, kCachePage, b);
-  else atomicAdd(&a.refs_out[id], fresh ? 1u : 0xFFFFFFFFu);
+  else atomicAdd(&a.refs_out[id], 1u);
 }
 
 // A thread's eight pages of a workgroup's 2,048 are 256 apart, so that a wave's
@@ -449,8 +463,9 @@ static uint32_t groups(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 
 
 hipError_t launch_fork(const RefArgs &a, hipStream_t st) {
   if (a.refs_out != a.refs_in) k_copy_refs<<<groups(a.n_pages, 256), 256, 0, st>>>(a);
-  const uint32_t chunks = a.s.max_pages ? groups(a.s.max_pages, 256) : 1, rows = a.n_out + (a.drop ? a.s.n_seq : 0);
-  if (rows) k_fork<<<chunks * rows, 256, 0, st>>>(a);
+  const uint32_t chunks = a.s.max_pages ? groups(a.s.max_pages, 256) : 1;
+  if (a.drop && a.s.n_seq) k_fork_drop<<<chunks * a.s.n_seq, 256, 0, st>>>(a);
+  if (a.n_out) k_fork<<<chunks * a.n_out, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -606,3 +606,43 @@ def test_growth_past_max_k(in_place):
     assert e.value.code == E_ARG
     cache.check()
     cache.close()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_fork_that_drops_more_names_than_counted(in_place):
+    """Names are dropped before new ones are counted: a count that they would take
+    below 0 is reported and starts from there, in whatever order names come."""
+    import torch
+
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ARG
+
+    say(f"[fork, dropped too often] in place {in_place}")
+    page, n_seq, width = 4, 200, 90
+    r = np.random.default_rng(3)
+    table = r.integers(0, 70, (n_seq, width)).astype(np.uint32)
+    lens = r.integers(0, width * page + 1, n_seq).astype(np.uint32)
+    held = names(table, lens, page, 100)
+    refs = np.where(np.arange(100) % 7 == 0, held // 2, held + np.arange(100) % 3)   # every seventh has too low a count
+    parents = r.integers(0, n_seq, 50).astype(np.uint32)
+    new, new_lens, added = fork_ref(table, lens, page, parents, np.zeros(100, np.int64), False)
+    cache = cache_of(page)
+    t, l = ints(table), ints(lens)
+    for n_out in (50, 0):
+        c = ints(refs)
+        out = c if in_place else torch.full_like(c, -7)
+        got = cache.fork(cache.sequences(t, l), ints(parents[:n_out]), c, drop=True, refs_out=out)
+        equal(got[0], new[:n_out])
+        equal(got[1], new_lens[:n_out])
+        equal(out, np.maximum(refs - held, 0) + (added if n_out else 0))
+        with pytest.raises(GrandError) as e:
+            cache.check()
+        assert e.value.code == E_ARG and "names" in str(e.value)
+    # one page, one name, never counted; the rest of the pool is found as before
+    c = ints([1, 0, 0])
+    cache.fork(cache.sequences(ints([[0, 1]]), ints([8])), ints([]), c, drop=True)
+    equal(c, [0, 0, 0])
+    with pytest.raises(GrandError):
+        cache.check()
+    cache.check()
+    cache.close()
