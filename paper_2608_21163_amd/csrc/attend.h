@@ -1241,6 +1241,14 @@ __device__ __forceinline__ uint32_t again_key(const AttendArgs &a, const Chunk &
   const uint32_t front = ((uint32_t)sinks_of<V>(a) + kAgainKeys - 1) / kAgainKeys, base = (uint32_t)max(0, ch.p0 - (int)a.window + 1) / kAgainKeys;
   return (i < front || base <= front ? i : base + i - front) * kAgainKeys;
 }
+// The other way round, for a tile that some row sees.
+template <class V>
+__device__ __forceinline__ uint32_t again_tile(const AttendArgs &a, const Chunk &ch, uint32_t key0) {
+  const uint32_t i = key0 / kAgainKeys;
+  if (!a.window) return i;
+  const uint32_t front = ((uint32_t)sinks_of<V>(a) + kAgainKeys - 1) / kAgainKeys, base = (uint32_t)max(0, ch.p0 - (int)a.window + 1) / kAgainKeys;
+  return i < front || base <= front ? i : i - base + front;
+}
 
 template <class E, int DP, class V>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : DP > 64 ? 2 : 3) void k_weights_again(AttendArgs a) {
@@ -1412,7 +1420,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : DP > 64 ? 2 : 3) void k_weights
   const uint32_t key = key0 + t;
   if (key < ch.kl) {
     if (!a.row_sums) wout[key] = win[key] + total[t];
-    else a.row_sums[(((size_t)part * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key] = total[t];
+    else a.row_sums[(((size_t)part * a.s.n_seq + b) * a.kv_heads + kvh) * a.sum_keys + rest / a.row_splits * kAgainKeys + t] = total[t];
   }
 }
 

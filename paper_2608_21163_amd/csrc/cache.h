@@ -74,7 +74,8 @@ struct AttendArgs {
   float *scores;             // log2-unit scores by (sequence, key/value head, row, key); null: recomputed
   uint32_t score_rows, score_keys;
   uint32_t row_splits;       // where they are recomputed: splits of the rows, whose sums are
-  float *row_sums;           // by (split, sequence, key/value head, key) if there is more than one, or a window
+  float *row_sums;           // by (split, sequence, key/value head, tile of again_tiles, key) if there is more than one, or a window
+  uint32_t sum_keys;         // keys of those tiles
   CacheErr *err;
 };
 

@@ -261,10 +261,11 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
       // least) where they are too few: six chunks of up to 614 tokens, 8 query
       // heads of 256 elements to one key/value head, over up to 1,904 cached
       // ones take 386 us with 48 workgroups, 172 with splits
-      const uint64_t tiles = (uint64_t)again_tiles(a) * p.kv_heads * s->n_seq;
-      const uint64_t most = std::min<uint64_t>((rows + 255) / 256, std::max<uint64_t>(1, (256ull << 20) / ((uint64_t)s->n_seq * p.kv_heads * keys * 4 + 1)));
+      a.sum_keys = again_tiles(a) * kAgainKeys;
+      const uint64_t tiles = (uint64_t)again_tiles(a) * p.kv_heads * s->n_seq, sums = (uint64_t)s->n_seq * p.kv_heads * a.sum_keys * 4;
+      const uint64_t most = std::min<uint64_t>((rows + 255) / 256, std::max<uint64_t>(1, (256ull << 20) / sums));
       a.row_splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((1024 + tiles - 1) / tiles, std::min<uint64_t>(most, 32)));
-      if (a.row_splits > 1 || a.window) w_sums = w.add((uint64_t)a.row_splits * s->n_seq * p.kv_heads * keys * 4);
+      if (a.row_splits > 1 || a.window) w_sums = w.add(a.row_splits * sums);
     }
     a.score_keys = (uint32_t)keys;
   }

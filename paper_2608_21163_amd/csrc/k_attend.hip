@@ -312,8 +312,12 @@ __global__ __launch_bounds__(256) void k_weights_add(AttendArgs a) {
   const AgainRows range = again_rows<Sinks>(a, ch, key0);
   const float old = a.win.p[(int64_t)b * a.win.seq + (int64_t)kvh * a.win.head + key];
   float sum = 0.f;
+  if (range.n) {
+    const float *at = a.row_sums + ((size_t)b * a.kv_heads + kvh) * a.sum_keys + again_tile<Sinks>(a, ch, key0) * kAgainKeys + threadIdx.x;
+    const size_t part = (size_t)a.s.n_seq * a.kv_heads * a.sum_keys;
 #pragma unroll 4
-  for (uint32_t i = 0; i < range.n; i++) sum += a.row_sums[(((size_t)i * a.s.n_seq + b) * a.kv_heads + kvh) * a.score_keys + key];
+    for (uint32_t i = 0; i < range.n; i++) sum += at[i * part];
+  }
   a.wout.p[(int64_t)b * a.wout.seq + (int64_t)kvh * a.wout.head + key] = old + sum;
 }
 

@@ -23,6 +23,7 @@ uintptr_t next_address;
 int device, capturing;
 hipStream_t captured;
 std::string trace;
+size_t largest;  // of the allocations that the host side made
 
 hipError_t made(const char *call, const char *more = "") {
   trace += std::string(call) + more + " on " + std::to_string(device) + "\n";
@@ -45,7 +46,9 @@ void fake_reset() {
   device = capturing = 0;
   captured = nullptr;
   trace.clear();
+  largest = 0;
 }
+size_t fake_largest() { return largest; }
 uintptr_t fake_memory(size_t size, int on) {
   const uintptr_t p = next_address;
   memory[p] = {size, on};
@@ -80,7 +83,7 @@ hipError_t hipSetDevice(int d) {
 }
 hipError_t hipMalloc(void **p, size_t n) {
   const hipError_t e = made("hipMalloc");
-  if (e == hipSuccess) *p = (void *)fake_memory(n, device);
+  if (e == hipSuccess) *p = (void *)fake_memory(n, device), largest = n > largest ? n : largest;
   return e;
 }
 hipError_t hipFree(void *p) {

@@ -593,3 +593,16 @@ def test_weights_of_chunks_without_cached_tokens(kind, window, sinks):
     none = torch.empty(2, 2, 0, device="cuda")
     out, lse, _ = run(c, weights=none, window=window, sinks=sinks)
     assert not out.any() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("kind", ["whole", "packed"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window,sinks", [(300, 0), (300, 270), (40, 600), (1000, 3), (1, 0)])
+def test_weights_of_windows_in_long_caches(kind, causal, window, sinks):
+    """Tiles of keys that no row sees lie before, between and behind those that have sums,
+    with one split of the rows and with several; a sequence is shorter than its window, one than its chunk."""
+    say(f"[windowed weights] {kind} causal {causal} window {window} {sinks}")
+    for most in (40, 300):                               # rows: one split; three, but for the shorter chunks
+        c = make("f16", 4, 2, 64, 8, qs=(most, 20, 7, 35, 0), ks=(2900, 1500, 200, 30, 700), seed=window + most)
+        c = packed(c) if kind == "packed" else c
+        weighted(c, causal=causal, window=window, sinks=sinks)

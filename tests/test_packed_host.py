@@ -414,3 +414,19 @@ def test_keys_and_values_that_partly_overlap(built):
     for strides, at in (((2 * 2048, 128, 64), 2 * 2048), ((2 * 2048, 2 * 128, 64), 2 * 128), ((2 * 2048, 2 * 128, 2 * 64), 2 * 64)):
         assert write(grand.Pages(two, two + at, 8, *strides)) == (OK, OK), c.error()
         assert write(grand.Pages(two, two + at - 16, 8, *strides)) == (ARG, ARG)
+
+
+def test_workspace_of_windowed_weights(built):
+    """Sums of rows are kept for the keys that a window reaches, not for all that are cached."""
+    built.fake_largest.restype = ctypes.c_size_t
+    n, chunk, length = 64, 64, 131_072
+    for window, sinks in ((1024, 0), (1024, 300)):
+        for packed in (False, True):
+            c = More(built, q_heads=32, kv_heads=8)
+            s, q, out = c.seqs(n, max_q=chunk, max_k=length), c.rows(n * chunk), c.rows(n * chunk)
+            w, pages = c.weights(n, length), c.packed() if packed else c.pages()
+            r = [ctypes.byref(x) for x in (s, q, pages, out, w, w)]
+            call = built.grand_cache_attend_packed if packed else built.grand_cache_attend_sinks
+            assert call(c.h, *r[:3], 0.125, 1, window, sinks, r[3], None, *r[4:]) == OK, c.error()
+            # log-sum-exps of all rows; 256 keys of eight tiles at most for each head, a quarter more when it grows
+            assert built.fake_largest() <= 1.25 * (n * chunk * 32 * 4 + n * 8 * 8 * 256 * 4 + 1024), built.fake_largest()
