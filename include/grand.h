@@ -380,10 +380,12 @@ typedef struct {
  * scale byte s each in `k_scales` and `v_scales`.  A code is a sign (bit 3) and a
  * magnitude of 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0 to 2), elements of even index in a
  * byte's low half; an element is its code times 2^(s - 127).  Blocks with s
- * above 252 (bf16) or 140 (fp16) count as NaN; values below the type's
- * range are rounded to it.  Strides are in bytes: of codes multiples of 16 and
+ * above 252 (bf16) or 140 (fp16) count as NaN.  Elements below the type's
+ * normal range that it holds in part only (no append writes their scales) are
+ * rounded to it, but for the values that grand_cache_attend_ids_packed sums
+ * up, which keep 32 bits.  Strides are in bytes: of codes multiples of 16 and
  * rows aligned to 16, of scales any.  The four arrays may be one buffer's
- * parts (rows whose scales follow their codes). */
+ * parts (rows whose scales follow their codes, pages that hold both). */
 typedef struct {
   uint8_t *k, *v, *k_scales, *v_scales;
   uint32_t n_pages;

@@ -32,7 +32,7 @@ struct F16 : PackF16 {
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b), c, false);
   }
 };
-// 32 codes as fp32 values.
+// 32 codes as fp32 values, small ones that the 16-bit type would round among them.
 template <class E> __device__ __forceinline__ void unpack32(v4u x, float factor, float *f) {
 #pragma unroll
   for (int w = 0; w < 4; w++) {

@@ -35,7 +35,8 @@ struct PackF16 {
   }
 };
 
-// The factor of a scale byte: exponent bits; 255 makes NaN of every code.
+// The factor of a scale byte: exponent bits, which is all that the conversions read
+// (0 is 2^-127, as a test of every byte shows); 255 makes NaN of every code.
 template <class P> __device__ __forceinline__ float pack_factor(uint32_t s) {
   return __uint_as_float((s > (uint32_t)P::kMaxScale ? 255u : s) << 23);
 }

@@ -606,3 +606,83 @@ def test_weights_of_windows_in_long_caches(kind, causal, window, sinks):
         c = make("f16", 4, 2, 64, 8, qs=(most, 20, 7, 35, 0), ks=(2900, 1500, 200, 30, 700), seed=window + most)
         c = packed(c) if kind == "packed" else c
         weighted(c, causal=causal, window=window, sinks=sinks)
+
+
+def rounded(x, dtype):
+    """Values as the 16-bit type holds them, its numbers below the normal range among them."""
+    import torch
+
+    if dtype == "f16":
+        return x.astype(np.float16).astype(np.float64)
+    return torch.from_numpy(x).float().bfloat16().double().numpy()       # (32 bits hold all of them)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_scale_and_code(dtype):
+    """All 256 scales with all 16 codes, those among them that no append writes: rows read back, and
+    what a single cached token gives, by each kernel, are the values rounded to the type."""
+    import torch
+
+    from paper_2608_21163_amd import Cache
+
+    say(f"[every scale] {dtype}")
+    codes = np.tile(np.array([2 * i | (2 * i + 1) << 4 for i in range(8)] * 2, np.uint8), (16, 16, 1, 1))
+    scales = np.arange(256, dtype=np.uint8).reshape(16, 16, 1, 1)
+    want = rounded(unpack(codes, scales, 32, dtype).reshape(256, 32), dtype)
+    cache = Cache(dtype, 1, 1, 32, 16, stream=torch.cuda.current_stream().cuda_stream)
+
+    def ints(x):
+        return torch.tensor(x, dtype=torch.int32, device="cuda")
+    for layout in ("rows", "token"):
+        k, v = (as_packed(codes, scales, layout) for _ in range(2))
+        for x in cache.read(ints(range(256)), k, v):
+            assert np.array_equal(x[:, 0].double().cpu().numpy(), want, equal_nan=True)
+    one = as_packed(codes, np.full_like(scales, 127), "token")
+    q = torch.zeros(256, 1, 32, dtype=cache.torch_dtype, device="cuda")
+    got = [cache.attend_ids(q, one, v, ints(range(256)).view(256, 1, 1))[0]]
+    # sequences of one cached token each: slot 0 of pages of one slot
+    flat = Cache(dtype, 1, 1, 32, 1, stream=torch.cuda.current_stream().cuda_stream)
+    each = [type(x)(*(y.reshape(256, 1, 1, -1) for y in x)) for x in (as_packed(codes, np.full_like(scales, 127), "token"), as_packed(codes, scales, "token"))]
+    got.append(flat.attend(flat.sequences(ints(range(256)).view(256, 1), ints([1] * 256)), q, *each)[0])
+    # (chunks of 40 rows: the last of each sees the token)
+    starts, many = ints(range(0, 257 * 40, 40)), torch.zeros(256 * 40, 1, 32, dtype=cache.torch_dtype, device="cuda")
+    got.append(flat.attend(flat.sequences(ints(range(256)).view(256, 1), ints([1] * 256), starts, max_q=40), many, *each)[0][39::40])
+    cache.check()
+    flat.check()
+    for name, x in zip(("list", "token", "chunk"), got):
+        assert np.array_equal(x[:, 0].double().cpu().numpy(), want, equal_nan=True), name
+    cache.close()
+    flat.close()
+
+
+@pytest.mark.parametrize("dtype,low,power", [("bf16", 0, 124), ("f16", 98, 12)])
+@pytest.mark.parametrize("most_q", [1, 50])
+def test_scales_that_no_append_writes(dtype, low, power, most_q):
+    """Small scales beside each other in the keys (large queries) and in the values: keys, and
+    the values of chunks, are rounded to the type, the values of lists are not."""
+    import torch
+
+    say(f"[small scales] {dtype} up to {most_q} tokens")
+    c = packed(make(dtype, 4, 2, 64, 16, qs=(most_q, 1), ks=(70, 33), seed=most_q))
+    r = np.random.default_rng(most_q)
+    c["q"] = (c["q"].double() / 2 * 2.0 ** power).to(c["q"].dtype)
+    # (bf16 ends at 2^128, fp16 at 2^16: no draw may pass that, as an infinite query gives no value with a key of 0)
+    assert torch.isfinite(c["q"]).all()
+    exact, total = {}, c["k_pages"].codes.shape[0] * 16
+    for pool, name, span in (("k_pages", "keys", 4 if dtype == "bf16" else 10), ("v_pages", "vals", 12)):
+        codes, scales = c[pool + "_np"]
+        scales = r.integers(low, low + span, scales.shape).astype(np.uint8)
+        c[pool] = as_packed(codes, scales, "head")
+        exact[name] = unpack(codes, scales, 64, dtype).reshape(total, 2, 64)
+        table = c["table"].cpu().numpy()
+        slots = [table[b, np.arange(k) // 16] * 16 + np.arange(k) % 16 for b, k in enumerate(c["ks"])]
+        c[name] = [torch.from_numpy(rounded(exact[name][x], dtype)) for x in slots]
+    weighted(c, scale=1.0)
+    ids = r.integers(0, total, (len(c["q"]), 4, 60)).astype(np.uint32)
+    cache = cache_for(c)
+    out, lse = cache.attend_ids(c["q"].cuda(), c["k_pages"], c["v_pages"], torch.from_numpy(ids.astype(np.int32)).cuda(), scale=1.0)
+    cache.check()
+    cache.close()
+    want, z, bound, z_err = ids_ref(c["q"].double().numpy(), rounded(exact["keys"], dtype), exact["vals"], ids, 1.0)
+    assert (np.abs(out.double().cpu().numpy() - want) <= bound(dtype)).all()
+    assert (np.abs(lse.double().cpu().numpy() - z) <= z_err + 1e-30).all()
