@@ -1436,8 +1436,7 @@ hipError_t few_dim(const AttendArgs &a, uint32_t tile_rows, hipStream_t st) {
   const uint32_t units = ((a.units ? a.units : a.row_tiles * a.n_splits * a.s.n_seq) + 7) / 8 * 8;
   const dim3 grid(units * a.kv_heads);
   if constexpr (V::kPacked) {
-    const uint32_t row = DP / 32;  // a row's scales
-    const bool wide = a.pg.shift >= 4 && a.dim > DP - 32 && ((uintptr_t)a.sc.k | (uintptr_t)a.sc.v | a.sc.page | a.sc.slot | a.sc.head) % row == 0;
+    const bool wide = packed_wide(a);
     if (tile_rows == 16 && wide) k_attend_few_packed<E, DP, 1, true><<<grid, 256, 0, st>>>(a);
     else if (tile_rows == 16) k_attend_few_packed<E, DP, 1, false><<<grid, 256, 0, st>>>(a);
     else if (wide) k_attend_few_packed<E, DP, 2, true><<<grid, 256, 0, st>>>(a);

@@ -193,6 +193,13 @@ constexpr uint32_t kFewRows = 32, kManyRows = 128;
 // Packed pages, few rows: workgroups that a CU's registers hold (a fourth of 128 elements
 // spills: 64 single tokens over up to 8,192 86 us instead of 70; tiles of 64 keys a wave 74).
 constexpr int packed_groups(int dp, int nb) { return dp > 128 ? (nb > 1 ? 1 : 2) : nb == 1 ? 3 : 2; }
+// the row length that their kernel is built for, and whether it takes runs of 16 keys that lie
+// in one page, whole rows of scales at once
+constexpr uint32_t packed_row(uint32_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+inline bool packed_wide(const AttendArgs &a) {
+  const uint32_t row = packed_row(a.dim) / 32;  // a row's scales
+  return a.pg.shift >= 4 && (a.dim + 31) / 32 == row && ((uintptr_t)a.sc.k | (uintptr_t)a.sc.v | a.sc.page | a.sc.slot | a.sc.head) % row == 0;
+}
 // keys of a tile of many rows
 constexpr uint32_t rows_tile(uint32_t dim) { return dim > 128 ? 32 : 64; }
 constexpr uint32_t kAgainKeys = 256;  // keys of a workgroup that computes scores again

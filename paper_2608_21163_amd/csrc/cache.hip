@@ -229,12 +229,13 @@ static grand_status attend(grand_cache *h, const grand_seqs *s, const grand_rows
   // keys 81).  Up to 512 keys are one launch without parts; every workgroup
   // adds up all lengths, 64 at a time.  Three workgroups a CU rather than two where registers
   // allow it (64 over up to 1,024: 23.5 us, 26.6; 256: 55, 60; 96 elements 69, 75), but two for long
-  // shares of slots of all heads (64 over up to 2,048, 4,096 and 8,192: 34.2, 45.4, 84.8, three
-  // 33.1, 46.7, 86.3).
+  // shares of slots of all heads whose runs lie in a page (64 over 4,096 and 8,192: 65.4 us, 141,
+  // three 73, 152; over up to 8,192 83.5, 86; up to 4,096 43.3, 41.5; but pages of eight and
+  // rows of 96 elements over up to 8,192 126 and 107, three 103.5 and 89).
   if (is_packed && few && span > 512 && s->n_seq <= 1024 && s->n_seq * (span / kKeysStep + 2) < 1u << 31) {
-    uint32_t groups_of_cu = packed_groups(p.head_dim <= 64 ? 64 : p.head_dim <= 128 ? 128 : 256, tile_rows / 16);
+    uint32_t groups_of_cu = packed_groups(packed_row(p.head_dim), tile_rows / 16);
     const bool beside = a.pg.slot == (p.head_dim + 31) / 32 * 16;  // a head's slots
-    if (!beside && groups_of_cu == 3 && p.head_dim > 64 && s->n_seq * span * p.kv_heads > 2048 * 512) groups_of_cu = 2;
+    if (!beside && groups_of_cu == 3 && p.head_dim > 64 && packed_wide(a) && s->n_seq * span * p.kv_heads > 2048 * 512) groups_of_cu = 2;
     a.units = std::max(1u, 256 * groups_of_cu / p.kv_heads);
   }
   const uint64_t groups = few ? ((a.units ? (uint64_t)p.kv_heads * a.units : base * a.n_splits) + 8 * p.kv_heads) : (uint64_t)p.kv_heads * a.row_tiles * a.n_splits;

@@ -123,10 +123,16 @@ hipError_t hipMemGetAddressRange(hipDeviceptr_t *base, size_t *size, hipDevicept
 }  // extern "C"
 
 namespace gr {
-hipError_t launch_attend(uint32_t, bool, const AttendArgs &, hipStream_t) { return made("attend"); }
+static AttendArgs attended;
+hipError_t launch_attend(uint32_t, bool, const AttendArgs &a, hipStream_t) {
+  attended = a;
+  return made("attend");
+}
 hipError_t launch_attend_join(bool, const AttendArgs &, uint32_t, hipStream_t) { return made("join"); }
 hipError_t launch_attend_weights(bool, const AttendArgs &, hipStream_t) { return made("weights"); }
 hipError_t launch_attend_ids(bool, const IdsArgs &, hipStream_t) { return made("ids"); }
 hipError_t launch_append(const AppendArgs &, hipStream_t) { return made("append"); }
 hipError_t launch_evict(const EvictArgs &, hipStream_t) { return made("evict"); }
 }  // namespace gr
+
+extern "C" uint32_t fake_units() { return gr::attended.units; }

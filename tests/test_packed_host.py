@@ -430,3 +430,21 @@ def test_workspace_of_windowed_weights(built):
             assert call(c.h, *r[:3], 0.125, 1, window, sinks, r[3], None, *r[4:]) == OK, c.error()
             # log-sum-exps of all rows; 256 keys of eight tiles at most for each head, a quarter more when it grows
             assert built.fake_largest() <= 1.25 * (n * chunk * 32 * 4 + n * 8 * 8 * 256 * 4 + 1024), built.fake_largest()
+
+
+def test_shares_of_packed_tokens(built):
+    """Equal shares of all keys fill the chip with three workgroups a CU, with two only where long
+    shares of slots of all heads are read in runs of a page."""
+    for kw, want in ((dict(), 2), (dict(page_size=8), 3), (dict(head_dim=96), 3), (dict(head_dim=104), 2), (dict(head_dim=64), 3),
+                     (dict(head_dim=256), 2), (dict(page_size=64), 2)):
+        c = More(built, **dict(dict(q_heads=32, kv_heads=8, head_dim=128), **kw))
+        s, q, out, g = c.seqs(64, max_k=8192), c.rows(64), c.rows(64), c.packed()
+        assert c.attend_packed(s, q, g, out) == OK and built.fake_units() * 8 == want * 256, kw
+        row, most = 16 * -(-c.p.head_dim // 32), 2 if c.p.head_dim > 128 else 3
+        beside = changed(g, slot_stride=row, head_stride=c.p.page_size * row)       # a head's slots side by side
+        assert c.attend_packed(s, q, beside, out) == OK and built.fake_units() * 8 == most * 256, kw
+        assert c.attend_packed(c.seqs(64, max_k=2048), q, g, out) == OK and built.fake_units() * 8 == most * 256, kw
+    odd = More(built, q_heads=32, kv_heads=8, head_dim=128)
+    g = odd.packed()
+    assert odd.attend_packed(odd.seqs(64, max_k=8192), odd.rows(64), changed(g, k_scales=g.k_scales + 1), odd.rows(64)) == OK
+    assert built.fake_units() * 8 == 3 * 256                                       # scales that are no aligned words
