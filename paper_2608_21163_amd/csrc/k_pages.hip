@@ -29,24 +29,25 @@ __global__ __launch_bounds__(256) void k_copy_refs(RefArgs a) {
   if (p < a.n_pages) a.refs_out[p] = a.refs_in[p];
 }
 
+// Takes a name off a page's count.  One that finds nothing left is put back and reported:
+// what is taken off in all is what was there, and the count ends at 0, whoever comes first.
+__device__ __forceinline__ void drop_name(const RefArgs &a, uint32_t id) {
+  if ((int)atomicSub(&a.refs_out[id], 1u) > 0) return;
+  atomicAdd(&a.refs_out[id], 1u);
+  cache_err(a.err, kCacheRefs, id);
+}
+
 // A workgroup per 256 entries of an old row whose names are dropped.  Before the
 // new names are counted, so that whether more are dropped than were counted
-// does not depend on who comes first.  A name that finds nothing left is put back: what is
-// taken off in all is what was there, and the count ends at 0.  (Its own launch is 2.9 us; 64
+// does not depend on who comes first.  (Its own launch is 2.9 us; 64
 // beams' fork, growth and copies 37.4 us, with names dropped and counted in one launch 34.5.)
 __global__ __launch_bounds__(256) void k_fork_drop(RefArgs a) {
   const uint32_t chunks = max((a.s.max_pages + 255) / 256, 1u), b = blockIdx.x / chunks, i = blockIdx.x % chunks * 256 + threadIdx.x;
   uint32_t len;
   if (i >= row_pages(a, b, len)) return;
   const uint32_t id = a.s.table[(int64_t)b * a.s.table_stride + i];
-  if (id >= a.n_pages) {
-    cache_err(a.err, kCachePage, b);
-    return;
-  }
-  const int old = (int)atomicSub(&a.refs_out[id], 1u);
-  if (old > 0) return;
-  atomicAdd(&a.refs_out[id], 1u);
-  cache_err(a.err, kCacheRefs, id);
+  if (id >= a.n_pages) cache_err(a.err, kCachePage, b);
+  else drop_name(a, id);
 }
 
 // A workgroup per 256 entries of a new row.
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256) void k_grow_give(RefArgs a) {
     a.src[b] = a.dst[b] = kInvalid;
     return;
   }
-  if (need & kOneCopy) atomicSub(&a.refs_out[a.src[b]], 1u);
+  if (need & kOneCopy) drop_name(a, a.src[b]);
   else a.dst[b] = kInvalid;
   const GrowSeq g = grow_seq(a, b);
   if (g.fits) a.lens[b] = g.len + a.n_new[b];

@@ -646,3 +646,30 @@ def test_fork_that_drops_more_names_than_counted(in_place):
         cache.check()
     cache.check()
     cache.close()
+
+
+@pytest.mark.parametrize("n_seq,counted", [(3, 2), (300, 2), (300, 299), (300, 300)])
+def test_growth_of_more_sequences_than_a_page_counts(n_seq, counted):
+    """Every sequence gets its copy of the partly filled page that they share; names
+    beyond its count are reported, and the count ends at 0."""
+    from paper_2608_21163_amd import GrandError
+    from paper_2608_21163_amd.grand import E_ARG
+
+    table, lens = np.zeros((n_seq, 2), np.uint32), np.full(n_seq, 3, np.uint32)
+    refs = np.zeros(n_seq + 5, np.int64)
+    refs[0], refs[1] = counted, 7
+    cache = cache_of(4)
+    t, l, c = ints(table), ints(lens), ints(refs)
+    _, _, src, dst = cache.grow(cache.sequences(t, l), ints(np.ones(n_seq)), c)
+    new = np.arange(2, n_seq + 2)
+    equal(c, np.concatenate([[0, 7], np.ones(n_seq), np.zeros(3)]))
+    equal(t, np.stack([new, 0 * new], 1))
+    equal(l, lens + 1)
+    equal(src, 0 * new)
+    equal(dst, new)
+    if counted < n_seq:
+        with pytest.raises(GrandError) as e:
+            cache.check()
+        assert e.value.code == E_ARG and "names" in str(e.value)
+    cache.check()
+    cache.close()
