@@ -686,3 +686,56 @@ def test_scales_that_no_append_writes(dtype, low, power, most_q):
     want, z, bound, z_err = ids_ref(c["q"].double().numpy(), rounded(exact["keys"], dtype), exact["vals"], ids, 1.0)
     assert (np.abs(out.double().cpu().numpy() - want) <= bound(dtype)).all()
     assert (np.abs(lse.double().cpu().numpy() - z) <= z_err + 1e-30).all()
+
+
+def one_buffer(n, page, hk, blocks, by):
+    """A pool's codes and scales in one buffer: behind each other in every page, head of a
+    page, or slot."""
+    import torch
+
+    from paper_2608_21163_amd import Packed
+
+    row = 16 * blocks
+    inner = {"page": page * hk, "head": page, "slot": hk}[by]
+    outer = page * hk // inner
+    size = -(-inner * (row + blocks) // 16) * 16
+    x = torch.zeros(n, outer, size, dtype=torch.uint8, device="cuda")
+    parts = x[:, :, :inner * row].unflatten(2, (inner, row))
+    scales = x[:, :, inner * row:inner * (row + blocks)].unflatten(2, (inner, blocks))
+    if by == "page":
+        return Packed(parts[:, 0].unflatten(1, (page, hk)), scales[:, 0].unflatten(1, (page, hk)))
+    if by == "head":
+        return Packed(parts.transpose(1, 2), scales.transpose(1, 2))
+    return Packed(parts, scales)
+
+
+@pytest.mark.parametrize("by", ["page", "head", "slot"])
+@pytest.mark.parametrize("hk,dim,page", [(2, 64, 16), (3, 40, 8), (1, 128, 64), (4, 256, 2)])
+def test_codes_and_scales_in_one_buffer(by, hk, dim, page):
+    """Appends, copies, attention and rows read back give what pools of four buffers give, bit by bit."""
+    import torch
+
+    from paper_2608_21163_amd import Packed
+
+    say(f"[one buffer] by {by}, {hk} x {dim}, pages of {page}")
+    c = make("bf16", 2 * hk, hk, dim, page, qs=(90, 20), ks=(90, 33), seed=dim)
+    n, blocks = c["k_pages"].shape[0], -(-dim // 32)
+    cache = cache_for(c)
+    s = seqs_for(cache, c)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(110, hk, dim, device="cuda", generator=g).bfloat16() for _ in range(2))
+    src, dst = c["table"][0, :1].clone(), torch.tensor([n - 1], dtype=torch.int32, device="cuda")
+    used = set(c["table"][c["table"] >= 0].tolist())
+    dst[0] = next(p for p in range(n) if p not in used)
+    both = []
+    for pools in (tuple(one_buffer(n, page, hk, blocks, by) for _ in range(2)),
+                  tuple(Packed(torch.zeros(n, page, hk, 16 * blocks, dtype=torch.uint8, device="cuda"),
+                               torch.zeros(n, page, hk, blocks, dtype=torch.uint8, device="cuda")) for _ in range(2))):
+        cache.append(s, k, v, *pools)
+        cache.copy_pages(*pools, src, dst)
+        out = cache.attend(s, c["q"].cuda(), *pools)
+        rows = cache.read(torch.arange(n * page, dtype=torch.int32, device="cuda"), *pools)
+        cache.check()
+        both.append([x.contiguous() for x in (*out, *rows, *pools[0], *pools[1])])
+    assert all(torch.equal(a, b) for a, b in zip(*both))
+    cache.close()
